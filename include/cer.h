@@ -483,6 +483,109 @@ int cer_stream_copy(void* dst_dev, const void* src_dev, int64_t bytes, void* str
  */
 int cer_stream_read(const void* src_dev, int64_t bytes, void* sink_dev, void* stream);
 
+/*
+ * Operators beside a projection -- what a language model needs next to the product with a compressed, frozen matrix: the norm in front
+ * of it, low-rank adapters next to it (W itself cannot be trained; they can), and the clipping of their gradients.
+ *
+ * Activations are matrices of `tokens` vectors of features (cer_tokens_t), in one of two orders:
+ *   CER_ORDER_ROWS     element (token t, feature i) at data[t * ld + i]
+ *   CER_ORDER_COLUMNS  at data[i * ld + t]: the order of cer_matmul's X and Y (ld = batch); fp32 only
+ * in fp32, bf16 or fp16 (CER_TYPE_F8, e4m3 without infinities, only where said), at any address and leading dimension ld that elements of
+ * the type may have.  An input's ld may be 0 (all tokens the same); an output's is at least the vector's length.  Inputs and outputs
+ * do not overlap, except where one is said to be allowed in another's place (the same data, ld, type and order).
+ *
+ * All pointers but the structs themselves (and grad_clip's list) are device pointers on the current device.  Work is enqueued on
+ * `stream`, nothing is waited for; buffers have to live until the stream has run it.  Arithmetic, sums and norms are in 32 bits or more
+ * whatever the types, and outputs in fewer bits are rounded once (nearest even).  Results do not depend on the order in which
+ * workgroups run.  tokens = 0 is allowed and does what is left of the work (gradients of weights become 0).
+ * Errors: CER_E_INVALID (null pointers, sizes below 1, unknown or unsuitable types and orders, ld too small), CER_E_TOO_LARGE (tokens over 2^28,
+ * features over 65536 for the norm, 2^22 else), CER_E_HIP.
+ */
+enum { CER_TYPE_F32 = 0, CER_TYPE_BF16 = 1, CER_TYPE_F16 = 2, CER_TYPE_F8 = 3 };
+enum { CER_ORDER_ROWS = 0, CER_ORDER_COLUMNS = 1 };
+typedef struct {
+    void* data;
+    int64_t ld;
+    int32_t type, order;
+} cer_tokens_t;
+
+/*
+ * rms_norm -- h = X + residual (NULL: h = X); sum = h (NULL: not written); Y_ti = h_ti . rstd_t . weight_i (NULL: 1), where
+ * rstd_t = 1 / sqrt(mean_i h_ti^2 + eps) comes from the unrounded h.
+ *
+ *   X, residual, sum  the same type (fp32, bf16, fp16) and order; sum may be X's or residual's own place
+ *   Y          fp32, X's type, or CER_TYPE_F8 with a scale per token; either order (columns: fp32; 8 bits: X and Y in rows)
+ *   weight     [n] of weight_type: fp32, bf16 or fp16
+ *   scale      [tokens] fp32, exactly if Y is 8 bits: the element Y_ti stands for Y_ti . scale_t, scale_t = max_i |.| / 448 (1 for a
+ *              token of zeros, at least 2^-126).  A NaN anywhere in a token makes its scale NaN.
+ *   rstd       [tokens] fp32 for the backward pass, or NULL
+ *
+ * Rows to rows is one launch without a temporary; with columns on either side there are two, and a temporary of up to 64 floats a token.
+ */
+int rms_norm(const cer_tokens_t* X, const cer_tokens_t* residual, const cer_tokens_t* sum, const cer_tokens_t* Y, int64_t tokens, int64_t n,
+             const void* weight, int32_t weight_type, float eps, float* scale, float* rstd, void* stream);
+
+/*
+ * rms_norm_backward -- with g = dY . weight and hat = H . rstd:  dX = rstd (g - hat . mean_i(g . hat)) + dsum (NULL: 0), the gradient of X and of
+ * residual alike;  dweight_i = sum_t dY_ti . hat_ti (NULL: not wanted; fp32).
+ *
+ *   H     what rms_norm wrote as sum (or its X); H, dsum, dX: the same type and order; dX may be dY's, H's or dsum's own place (dY's: only
+ *         in H's order)
+ *   dY    fp32 or H's type; rows, or columns (fp32) whichever order H has.  H in columns wants dY in columns.
+ *
+ * Temporaries: up to 512 . n floats for dweight, tokens . n for dY in another order than H, up to 64 a token for columns.
+ */
+int rms_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_tokens_t* dsum, const cer_tokens_t* dX, int64_t tokens, int64_t n,
+                      const float* rstd, const void* weight, int32_t weight_type, float* dweight, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside one projection.  Adapter a of `adapters` has A_a [rank][in], B_a [out][rank], both of `type`, each
+ * row contiguous: element (r, k) of A_a at A[a * stride_a + r * ld_a + k], (o, r) of B_a at B[a * stride_b + o * ld_b + r]; a factor
+ * scales[a] (NULL: 1) and a rank of its own ranks[a] (NULL: rank; what is past it is not read, outside 0 .. rank it counts as the nearer
+ * one).  1 <= rank <= 256, adapters <= 65535.
+ * `index` [tokens] names each token's adapter; tokens with an index outside 0 .. adapters - 1 have none.  Tokens of one adapter need not be
+ * neighbours, but the work is shared best where they are (requests one after the other).
+ * Types: activations and adapters of the same type, or fp32 activations (either order) beside bf16 or fp16 adapters.
+ *
+ * adapter_matmul -- hidden_t = A_a x_t;  Y_t = base_t + scales_a B_a hidden_t (base NULL: 0); Y_t = base_t for a token without an adapter.  base
+ * may be Y's own place (the product of cer_matmul, say).  base, Y: X's type and order.  hidden: [tokens][rank] fp32, without the factor, for the
+ * backward pass, or NULL.  workspace: adapter_workspace_bytes() bytes of device memory, or NULL (a stream-ordered temporary); with it
+ * the call only launches two kernels and may be recorded into a HIP graph after one eager call.
+ *
+ * adapter_backward -- d_t = scales_a B_a^T dY_t;  dX_t = base_t + A_a^T d_t (what the projection sends back; NULL: 0; may be dX's own place);
+ * dA_a = sum over a's tokens of d_t x_t^T;  dB_a = scales_a . sum over a's tokens of dY_t hidden_t^T.  dX, dA, dB: any may be NULL.
+ * dA [adapters][rank][in], dB [adapters][out][rank]: fp32, contiguous, written whole (0 for adapters and ranks that do not occur).
+ */
+typedef struct {
+    const void *A, *B;
+    const float* scales;
+    const int32_t* ranks;
+    int64_t adapters, rank, in, out;
+    int64_t stride_a, ld_a, stride_b, ld_b;
+    int32_t type;
+} cer_adapters_t;
+int64_t adapter_workspace_bytes(int64_t tokens, int64_t rank, int64_t in, int64_t out);
+int adapter_matmul(const cer_adapters_t* w, const int32_t* index, int64_t tokens, const cer_tokens_t* X, const cer_tokens_t* base,
+                   const cer_tokens_t* Y, float* hidden, void* workspace, int64_t workspace_bytes, void* stream);
+int adapter_backward(const cer_adapters_t* w, const int32_t* index, int64_t tokens, const cer_tokens_t* dY, const cer_tokens_t* X,
+                     const float* hidden, const cer_tokens_t* base, const cer_tokens_t* dX, float* dA, float* dB, void* stream);
+
+/*
+ * grad_norm, grad_clip -- norm[0] = sqrt of the sum of the squares of all `count` tensors' elements (added in 64 bits); grad_clip: out =
+ * min(1, max_norm / (norm + 1e-6)) . grad for every one of them.  Each tensor is contiguous, fp32, bf16 or fp16, of any length from 0; out
+ * has its type and may be grad itself (then nothing is written where the factor is 1).  A NaN or an infinity in any of them makes
+ * the norm NaN or infinite, and the factor NaN or 0.  `grads` is a host array, read during the call; max_norm >= 0.
+ * A temporary of 8 KiB per 120 tensors.
+ */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t numbers;
+    int32_t type;
+} cer_gradient_t;
+int grad_norm(const cer_gradient_t* grads, int64_t count, float* norm, void* stream);
+int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float* norm, void* stream);
+
 const char* cer_strerror(int code);
 int cer_last_hip_error(void);
 

@@ -1,7 +1,7 @@
 """Python binding of the C ABI in include/cer.h -- argument marshalling only.
 
 Every function has the name of the C entry point it calls; the product calls (cer_matmul, cser_matmul, cer_matmul_noalloc,
-csr_matmul) are native functions of _cerpy (csrc/pybind.cpp), because a small product takes less time than ctypes does.  Device buffers are passed as torch
+csr_matmul) and the operators beside a projection are native functions of _cerpy (csrc/pybind.cpp), because a small product takes less time than ctypes does.  Device buffers are passed as torch
 tensors (their ``data_ptr()`` is handed to the library) or as raw integer addresses; streams as
 ``torch.cuda.Stream`` objects, raw ``hipStream_t`` integers, or None for the current torch stream.
 No step of the product runs in Python or in torch, and there is no CPU fallback: if the built
@@ -44,6 +44,8 @@ EXPORTS = [
     "cer_decode_device", "cer_trim", "cer_matmul_ex", "cer_matmul_path_ex", "cer_matmul_noalloc", "cer_prepare_strips",
     "cer_matmul_narrow_columns", "cer_matmul_fused_rows", "cer_matmul_tile_columns", "cer_matmul_planes", "cer_encode_sorts_rows",
 ]
+# operators beside a projection
+OPERATOR_EXPORTS = ["rms_norm", "rms_norm_backward", "adapter_workspace_bytes", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip"]
 
 CER_FORMAT_CER, CER_FORMAT_CSER = 0, 1
 
@@ -191,6 +193,10 @@ def lib() -> ctypes.CDLL:
         L.cer_strerror.argtypes = [ctypes.c_int]
         L.cer_last_hip_error.restype = ctypes.c_int
         L.cer_last_hip_error.argtypes = []
+        L.adapter_workspace_bytes.restype = i64
+        L.adapter_workspace_bytes.argtypes = [i64] * 4
+        _cerpy.bind_operators(*(ctypes.cast(getattr(L, f), vp).value
+                                for f in ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip")))
         _cerpy.bind(*(ctypes.cast(getattr(L, f), vp).value
                       for f in ("cer_matmul", "cser_matmul", "cer_matmul_noalloc", "csr_matmul")))
         _lib = L
@@ -224,11 +230,22 @@ if _cerpy is not None:
     # f(h, X, Y, batch, stream=None) -> None
     cer_matmul, cser_matmul = _cerpy.cer_matmul, _cerpy.cser_matmul
     cer_matmul_noalloc, csr_matmul = _cerpy.cer_matmul_noalloc, _cerpy.csr_matmul
+    # Operators beside a projection (csrc/pybind_operators.cpp; include/cer.h says what each computes).  Activations are tensors of
+    # shape (tokens, features): contiguous rows, or, fp32, the transposed view of a contiguous (features, tokens) tensor, which is
+    # how cer_matmul has its X and Y.
+    rms_norm, rms_norm_backward = _cerpy.rms_norm, _cerpy.rms_norm_backward
+    adapter_matmul, adapter_backward = _cerpy.adapter_matmul, _cerpy.adapter_backward
+    grad_norm, grad_clip = _cerpy.grad_norm, _cerpy.grad_clip
 else:
     def cer_matmul(h, X, Y, batch: int, stream=None) -> None:
         lib()  # raises: not built
 
     cser_matmul = cer_matmul_noalloc = csr_matmul = cer_matmul
+
+    def rms_norm(*args, **kwargs) -> None:
+        lib()  # raises: not built
+
+    rms_norm_backward = adapter_matmul = adapter_backward = grad_norm = grad_clip = rms_norm
 
 
 class Handle:
@@ -456,6 +473,14 @@ def cer_free(h: Handle) -> None:
     if h.ptr:
         lib().cer_free(h.ptr)
         h.ptr = None
+
+
+def adapter_workspace_bytes(tokens: int, rank: int, features_in: int, features_out: int) -> int:
+    """Size of the workspace with which adapter_matmul allocates nothing."""
+    v = lib().adapter_workspace_bytes(tokens, rank, features_in, features_out)
+    if v < 0:
+        raise CerError(int(v), "adapter_workspace_bytes")
+    return int(v)
 
 
 def dense_matmul(W, X, Y, m: int, n: int, batch: int, stream=None) -> None:
