@@ -29,7 +29,9 @@ namespace {
 
 using F4 = Vec<float, 4>;
 constexpr int kBlock = 256, kWaves = kBlock / 64;
+constexpr int kShrinkBlock = 512, kOuterBlock = 256;
 constexpr int kMostTile = 64;  // tokens of a workgroup
+constexpr int64_t kFewTokens = 256;
 
 // One side's weights: element (long axis k, rank r) of adapter a at w[a * stride + (kAlong ? r * ld + k : k * ld + r)].
 struct Weights {
@@ -54,7 +56,7 @@ __device__ __forceinline__ int adapter_at(const int32_t* index, int64_t t, int64
 }
 
 // The adapters among a workgroup's tokens, each once, in the order of their first tokens; one wave makes the list for all.
-struct Present {
+struct alignas(16) Present {
     int adapter[kMostTile];  // of each token
     int slot[kMostTile];     // the adapters
     int slots;
@@ -96,6 +98,19 @@ __device__ __forceinline__ Vec<T, N> load_own(const T* p, int64_t left) {
     return v;
 }
 
+// Elements at a wave's own address (a scalar) and a lane's offset in bytes from it.
+template <class T>
+__device__ __forceinline__ const T* at(const T* base, uint32_t bytes) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
+template <class T>
+__device__ __forceinline__ T* at(T* base, uint32_t bytes) { return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes); }
+
+// The same offset, as a number of its own: sums with it are made where they stand, as a scalar and an offset that the load adds up, and not kept in two registers each
+// through the loops around them (32 of those: 64 registers).
+__device__ __forceinline__ uint32_t here(uint32_t bytes) {
+    asm volatile("" : "+v"(bytes));
+    return bytes;
+}
+
 // ---- shrink ---------------------------------------------------------------------------------------------------------------------
 struct ShrinkArgs {
     Weights w;
@@ -108,131 +123,154 @@ struct ShrinkArgs {
     bool scale;    // times s_a
 };
 
-// kTiles * 16 tokens, kRanks * 16 ranks from blockIdx.z on.  Lane (i, g) = (lane % 16, lane / 16) holds of both sides' operands row i's (a rank's, a
-// token's) elements of the long axis that belong to g: 4 of 16 in 32 bits (four instructions of 4, each taking one of every g's), 8 of 32 in 16.
-// The sides agree on which, and that is all that their order has to do.
+// kTiles * 16 tokens, kRanks * 16 ranks from blockIdx.z on; the waves share out the adapters and pieces of the workgroup's part of the long
+// axis.  Lane (i, g) = (lane % 16, lane / 16) holds of both sides' operands row i's (a rank's, a token's) eight elements of 32 of the long axis
+// that belong to g: one 16-bit instruction, or eight 32-bit ones that take one of every g's.  The sides agree on which, and that is all that
+// their order has to do.  Rows of ranks: 16 r + i, or where a rank's elements lie apart (!kAlong) kRanks i + r, neighbours in one load.
 template <class TX, class TW, bool kColumns, bool kAlong, int kTiles, int kRanks>
-__global__ __launch_bounds__(kBlock) void shrink_kernel(ShrinkArgs c) {
+__global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void shrink_kernel(ShrinkArgs c) {
     constexpr bool k16 = sizeof(TX) == 2;
-    constexpr int E = k16 ? 8 : 4, kStep = 4 * E, kTile = 16 * kTiles, kPitch = 16 * kRanks + 4;
-    using Operand = std::conditional_t<k16, Vec<TX, E>, F4>;
+    constexpr int E = 8, kStep = 4 * E, kTile = 16 * kTiles, kPitch = 16 * kRanks + 4, kWaves = kShrinkBlock / 64;
+    using Operand = std::conditional_t<k16, Vec<TX, E>, Vec<float, E>>;
     __shared__ Present present;
-    __shared__ float sums[kWaves][kTile][kPitch];
+    __shared__ float sums[kTile][kPitch];
     const int64_t t0 = (int64_t)blockIdx.x * kTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
     list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
-    const int slots = present.slots;
-    const int abreast = slots >= kWaves ? kWaves : slots >= 2 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
-    // this wave's piece of the long axis
-    const int64_t from = blockIdx.y * c.part, to = from + c.part < c.length ? from + c.part : c.length;
-    const int64_t each = ((to - from + pieces - 1) / pieces + kStep - 1) / kStep * kStep;
-    const int64_t k0 = from + piece * each, k1 = k0 + each < to ? k0 + each : to;
+    const int slots = __builtin_amdgcn_readfirstlane(present.slots);
+    const int abreast = kTiles > 1 ? 1 : slots >= 8 ? 8 : slots >= 4 ? 4 : slots >= 2 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
+    // the workgroup's part of the long axis; its waves take turns, so that together they read neighbouring lines
+    const int from = blockIdx.y * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
+    constexpr int kAhead = k16 && kTiles * kRanks <= 4 ? 4 : kTiles * kRanks <= (kTiles == 1 && !k16 ? 4 : 8) ? 2 : 1;  // steps whose loads are on their way together
+    constexpr int kRun = kAhead * kStep;
     int token[kTiles];  // in the tile
 #pragma unroll
     for (int s = 0; s < kTiles; ++s) token[s] = kColumns ? kTiles * i + s : 16 * s + i;
-    const TX* x[kTiles];
+    const int tokens_left = (int)std::min<int64_t>(c.tokens - t0, kTile), abreast_left = tokens_left - kTiles * i;
+    // a lane's place: the rest of an address is the wave's
+    const TX* x = static_cast<const TX*>(c.x) + (kColumns ? t0 : t0 * c.ldx);
+    uint32_t x_lane[kTiles];
     if (kColumns) {
-        x[0] = static_cast<const TX*>(c.x) + (t0 + kTiles * i < c.tokens ? t0 + kTiles * i : 0);
+        x_lane[0] = (uint32_t)(E * g * c.ldx + (abreast_left > 0 ? kTiles * i : 0)) * sizeof(TX);
     } else {
 #pragma unroll
-        for (int s = 0; s < kTiles; ++s)
-            x[s] = static_cast<const TX*>(c.x) + (t0 + token[s] < c.tokens ? t0 + token[s] : c.tokens - 1) * c.ldx;
+        for (int s = 0; s < kTiles; ++s) x_lane[s] = (uint32_t)(std::min(token[s], tokens_left - 1) * c.ldx + E * g) * sizeof(TX);
     }
-    const int64_t abreast_left = t0 + kTiles * i < c.tokens ? c.tokens - (t0 + kTiles * i) : 0;  // columns: tokens of the lane's vector
-    for (int q = wave % abreast; q < slots; q += abreast) {
-        const int a = __builtin_amdgcn_readfirstlane(present.slot[q]);
-        const int rank = rank_of(c.w, a);
-        if (rank <= r0) continue;
-        const TW* w = static_cast<const TW*>(c.w.w) + a * c.w.stride;
-        const TW* row[kRanks];  // of a rank past the last one: the last one's, its products are not kept
-#pragma unroll
-        for (int r = 0; r < kRanks; ++r) {
-            const int at = r0 + 16 * r + i < rank ? r0 + 16 * r + i : rank - 1;
-            row[r] = kAlong ? w + at * c.w.ld : w + at;
-        }
+    for (int first = 0; first < slots; first += abreast) {
+        const int q = first + wave % abreast;
+        const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
+        const int rank = a >= 0 ? rank_of(c.w, a) : 0;
         F4 acc[kTiles][kRanks];
 #pragma unroll
         for (int s = 0; s < kTiles; ++s)
 #pragma unroll
             for (int r = 0; r < kRanks; ++r) acc[s][r] = 0.f;
-        auto step = [&](int64_t k, auto whole) {  // whole: nothing of the step is past k1
-            constexpr bool kWhole = decltype(whole)::value;
-            const int64_t at = k + E * g, left = kWhole ? E : k1 - at;
-            Operand xs[kTiles], ws[kRanks];
-            if constexpr (kColumns) {
+        if (rank > r0) {
+            const TW* w = static_cast<const TW*>(c.w.w) + a * c.w.stride + (kAlong ? r0 * c.w.ld : r0);
+            uint32_t w_lane[kRanks];  // kAlong: of a rank past the last one: the last one's, its products are not kept
+            if (kAlong) {
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    Vec<float, 4> v = 0.f;
-                    if (kWhole || j < left) {
-                        const TX* p = x[0] + (at + j) * c.ldx;
-                        if constexpr (kTiles == 1) v[0] = abreast_left > 0 ? p[0] : 0.f;
-                        if constexpr (kTiles == 2) {
-                            const Vec<float, 2> u = load_some<TX, 2>(p, abreast_left);
-                            v[0] = u[0], v[1] = u[1];
-                        }
-                        if constexpr (kTiles == 4) v = load_some<TX, 4>(p, abreast_left);
-                    }
-#pragma unroll
-                    for (int s = 0; s < kTiles; ++s) xs[s][j] = v[s];
-                }
+                for (int r = 0; r < kRanks; ++r) w_lane[r] = (uint32_t)(std::min(16 * r + i, rank - r0 - 1) * c.w.ld + E * g) * sizeof(TW);
             } else {
-#pragma unroll
-                for (int s = 0; s < kTiles; ++s) {
-                    if constexpr (k16) xs[s] = load_own<TX, E>(x[s] + at, left);
-                    else xs[s] = load_some<TX, E>(x[s] + at, left);
-                }
+                w_lane[0] = (uint32_t)(E * g * c.w.ld + kRanks * i) * sizeof(TW);
             }
+            const int ranks_left = rank - r0 - kRanks * i;
+            const bool ranks_whole = rank - r0 >= 16 * kRanks;
+            bool here[kTiles];  // rows: tiles in which the adapter occurs (columns: a lane's vector has a token of each)
 #pragma unroll
-            for (int r = 0; r < kRanks; ++r) {
+            for (int s = 0; s < kTiles; ++s) here[s] = kColumns || kTiles == 1 || __any(present.adapter[token[s]] == a);
+            auto step = [&](int k, auto whole) {  // whole: nothing of the step is past the end
+                constexpr bool kWhole = decltype(whole)::value;
+                const int left = kWhole ? E : to - (k + E * g);
+                Operand xs[kTiles], ws[kRanks];
+                if constexpr (kColumns) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        Vec<float, 4> v = 0.f;
+                        if (kWhole || j < left) {
+                            const TX* p = at(x + (k + j) * c.ldx, x_lane[0]);
+                            if constexpr (kTiles == 1) v[0] = p[0];
+                            if constexpr (kTiles == 4) v = load_some<TX, 4>(p, abreast_left);
+                        }
+#pragma unroll
+                        for (int s = 0; s < kTiles; ++s) xs[s][j] = v[s];
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < kTiles; ++s) {
+                        if (!here[s]) continue;
+                        if constexpr (k16) xs[s] = load_own<TX, E>(at(x + k, x_lane[s]), left);
+                        else xs[s] = load_some<TX, E>(at(x + k, x_lane[s]), left);
+                    }
+                }
                 if constexpr (kAlong) {
-                    if constexpr (k16) ws[r] = load_own<TW, E>(row[r] + at, left);
-                    else ws[r] = load_some<TW, E>(row[r] + at, left);
+#pragma unroll
+                    for (int r = 0; r < kRanks; ++r) {
+                        if constexpr (k16) ws[r] = load_own<TW, E>(at(w + k, w_lane[r]), left);
+                        else ws[r] = load_some<TW, E>(at(w + k, w_lane[r]), left);
+                    }
                 } else {
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
-                        TW v = (TW)0.f;
-                        if (kWhole || j < left) v = row[r][(at + j) * c.w.ld];
-                        if constexpr (k16) ws[r][j] = v;
-                        else ws[r][j] = (float)v;
+                        Vec<TW, kRanks> v = (TW)0.f;
+                        const TW* p = at(w + (k + j) * c.w.ld, w_lane[0]);
+                        if (kWhole && ranks_whole) v = load<TW, kRanks>(p);
+                        else if (kWhole || j < left) v = load_own<TW, kRanks>(p, ranks_left);
+#pragma unroll
+                        for (int r = 0; r < kRanks; ++r) {
+                            if constexpr (k16) ws[r][j] = v[r];
+                            else ws[r][j] = (float)v[r];
+                        }
                     }
                 }
+#pragma unroll
+                for (int s = 0; s < kTiles; ++s)
+#pragma unroll
+                    for (int r = 0; r < kRanks; ++r) {
+                        if (!here[s]) continue;
+                        if constexpr (k16) {
+                            acc[s][r] = product(ws[r], xs[s], acc[s][r]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < E; ++j) acc[s][r] = product(ws[r][j], xs[s][j], acc[s][r]);
+                        }
+                    }
+            };
+            int k = from + piece * kRun;
+            for (; k + kRun <= to; k += pieces * kRun)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) step(k + u * kStep, std::true_type());
+            if (k < to) {  // the last run, by the wave whose turn it is
+                const int end = std::min(k + kRun, to);
+                if constexpr (kAhead > 1)
+#pragma unroll 1
+                    for (; k + kStep <= end; k += kStep) step(k, std::true_type());
+                if (k < end) step(k, std::false_type());
             }
+        }
+        // the pieces of an adapter are added up in turn; each token is one adapter's
+        for (int p = 0; p < pieces; ++p) {
+            if (p == piece && rank > r0)
 #pragma unroll
-            for (int s = 0; s < kTiles; ++s)
+                for (int s = 0; s < kTiles; ++s)
+                    if (present.adapter[token[s]] == a)
 #pragma unroll
-                for (int r = 0; r < kRanks; ++r) {
-                    if constexpr (k16) {
-                        acc[s][r] = product(ws[r], xs[s], acc[s][r]);
-                    } else {
+                        for (int r = 0; r < kRanks; ++r)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[s][r] = product(ws[r][j], xs[s][j], acc[s][r]);
-                    }
-                }
-        };
-        int64_t k = k0;
-        constexpr int kAhead = kTiles * kRanks >= 8 ? 2 : 4;  // steps whose loads are on their way together
-        for (; k + kAhead * kStep <= k1; k += kAhead * kStep)
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) step(k + u * kStep, std::true_type());
-        for (; k + kStep <= k1; k += kStep) step(k, std::true_type());
-        if (k < k1) step(k, std::false_type());
-#pragma unroll
-        for (int s = 0; s < kTiles; ++s)
-            if (present.adapter[token[s]] == a)
-#pragma unroll
-                for (int r = 0; r < kRanks; ++r) *reinterpret_cast<F4*>(&sums[piece][token[s]][16 * r + 4 * g]) = acc[s][r];
+                            for (int e = 0; e < 4; ++e) {
+                                float* at = &sums[token[s]][kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r];
+                                *at = p ? *at + acc[s][r][e] : acc[s][r][e];
+                            }
+            __syncthreads();
+        }
     }
-    __syncthreads();
     float* out = c.out + (int64_t)blockIdx.y * c.tokens * c.w.rank;
-    for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kBlock) {
+    for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kShrinkBlock) {
         const int t = e / (16 * kRanks), r = e % (16 * kRanks);
         if (t0 + t >= c.tokens || r0 + r >= c.w.rank) continue;
         const int a = present.adapter[t];
-        float all = 0.f;
-        if (a >= 0 && r0 + r < rank_of(c.w, a)) {
-            for (int p = 0; p < pieces; ++p) all += sums[p][t][r];
-            if (c.scale) all *= scale_of(c.w, a);
-        }
+        float all = a >= 0 && r0 + r < rank_of(c.w, a) ? sums[t][r] : 0.f;
+        if (c.scale && a >= 0) all *= scale_of(c.w, a);
         out[(t0 + t) * c.w.rank + r0 + r] = all;
     }
 }
@@ -261,127 +299,322 @@ struct ExpandArgs {
     void* y;
     int64_t ldbase, ldy;
     uint32_t blocks;    // of 64 elements of the long axis for a workgroup
+    uint32_t groups;    // of such blocks
 };
 
-// kTiles * 16 tokens; a wave takes pairs of adapter and 64 elements of the long axis.  Element o0 + 4 i + j is row (column) i of the tile j of four:
-// the operands' loads have four neighbours in a lane where the weights lie that way, and so do the results: lane (i, g) holds
-// o0 + 16 g .. + 15 of token i (rows), or elements o0 + 4 i + j of tokens 4 g .. + 3 (columns).
-template <class TX, class TW, bool kColumns, bool kAlong, int kTiles>
-__global__ __launch_bounds__(kBlock) void expand_kernel(ExpandArgs c) {
-    constexpr int kTile = 16 * kTiles;
-    extern __shared__ float hidden[];  // [tile][pitch], 0 past the rank and for tokens without an adapter
-    __shared__ Present present;
-    const int64_t t0 = (int64_t)blockIdx.x * kTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+// The 16 tokens from t0 on, `blocks` times 64 elements of the long axis from block `first` on; a wave takes pairs of adapter and 64 elements.
+// Element o0 + 4 i + j is row (column) i of the tile j of four: the operands' loads have four neighbours in a lane where the weights lie
+// that way, and so do the results: lane (i, g) holds o0 + 16 g .. + 15 of token i (rows), or elements o0 + 4 i + j of tokens
+// 4 g .. + 3 (columns).  `room`: LDS of 16 * (the rank's next multiple of 16, + 4) floats.
+template <class TX, class TW, bool kColumns, bool kAlong>
+__device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int first, int blocks, bool tell, Present& present, float* room) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int rank16 = (c.w.rank + 15) / 16 * 16, pitch = rank16 + 4;
-    list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
-    for (int e = threadIdx.x; e < kTile * rank16; e += kBlock) {
-        const int t = e / rank16, r = e % rank16, a = present.adapter[t];
-        float sum = 0.f;
-        if (t0 + t < c.tokens && r < c.w.rank) {
-            const float* p = c.part + (t0 + t) * c.w.rank + r;
-            if (a >= 0 && r < rank_of(c.w, a))
+    list_adapters(present, c.index, t0, 16, c.tokens, c.w.adapters);
+    {  // hidden, 0 past the rank and for tokens without an adapter
+        const int t = threadIdx.x >> 4, a = present.adapter[t];
+        const int rank = a >= 0 ? rank_of(c.w, a) : 0;
+        const float scale = a >= 0 && c.scale ? scale_of(c.w, a) : 1.f;
+        for (int r = threadIdx.x & 15; r < rank16; r += 16) {
+            float sum = 0.f;
+            if (t0 + t < c.tokens && r < c.w.rank) {
+                const float* p = c.part + (t0 + t) * c.w.rank + r;
+                if (r < rank)
 #pragma unroll 8
-                for (uint32_t k = 0; k < c.parts; ++k) sum += p[k * c.tokens * c.w.rank];
-            if (c.hidden && blockIdx.y == 0) c.hidden[(t0 + t) * c.w.rank + r] = sum;
-            if (a >= 0 && c.scale) sum *= scale_of(c.w, a);
+                    for (uint32_t k = 0; k < c.parts; ++k) sum += p[k * c.tokens * c.w.rank];
+                if (c.hidden && tell) c.hidden[(t0 + t) * c.w.rank + r] = sum;
+            }
+            room[t * pitch + r] = sum * scale;
         }
-        hidden[t * pitch + r] = sum;
     }
     __syncthreads();
     const TX* base = static_cast<const TX*>(c.base);
     TX* y = static_cast<TX*>(c.y);
     // tokens without an adapter: a list entry of their own, unless y has what they get already
-    const int slots = present.slots, jobs = slots + (present.none && c.base != c.y ? 1 : 0);
-    const int64_t o_first = (int64_t)blockIdx.y * c.blocks * 64;
-    for (int job = wave; job < jobs * (int)c.blocks; job += kWaves) {
-        const int64_t o0 = o_first + job / jobs * 64;
+    const int slots = __builtin_amdgcn_readfirstlane(present.slots), jobs = slots + (__builtin_amdgcn_readfirstlane(present.none) && c.base != c.y ? 1 : 0);
+    for (int job = wave; job < jobs * blocks; job += kWaves) {
+        const int64_t o0 = (int64_t)(first + job / jobs) * 64;
         if (o0 >= c.length) break;
         const int a = job % jobs < slots ? __builtin_amdgcn_readfirstlane(present.slot[job % jobs]) : -1;
-        const int64_t left = c.length - o0;
-        F4 acc[kTiles][4];  // rows: [tile][j], elements 16 g + 4 (0 .. 3) + j; columns: [tile][j], tokens 4 g + (0 .. 3)
+        const int left = (int)std::min<int64_t>(c.length - o0, 64);
+        F4 acc[4];  // rows: [j], elements 16 g + 4 (0 .. 3) + j; columns: [j], tokens 4 g + (0 .. 3)
+        constexpr int V = 16 / sizeof(TX);
+        const int64_t t = t0 + (kColumns ? 4 * g : i);
+        const bool mine = t0 + i < c.tokens && present.adapter[i] == a;
+        if constexpr (kColumns) {
 #pragma unroll
-        for (int s = 0; s < kTiles; ++s) {
-            if constexpr (kColumns) {
-                const int64_t t = t0 + 16 * s + 4 * g;
+            for (int j = 0; j < 4; ++j)
+                acc[j] = base && 4 * i + j < left && t < c.tokens ? load_some<TX, 4>(base + (o0 + 4 * i + j) * c.ldbase + t, c.tokens - t) : F4(0.f);
+        } else {
+            Vec<float, 16> v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[s][j] = base && 4 * i + j < left && t < c.tokens ? load_some<TX, 4>(base + (o0 + 4 * i + j) * c.ldbase + t, c.tokens - t) : F4(0.f);
-            } else {
-                const int64_t t = t0 + 16 * s + i;
-                const bool mine = base && t < c.tokens && present.adapter[16 * s + i] == a;
-                constexpr int V = 16 / sizeof(TX);
-                Vec<float, 16> v;
+            for (int q = 0; q < 16 / V; ++q) {
+                Vec<float, V> u = 0.f;
+                if (base && mine) u = load_some<TX, V>(base + t * c.ldbase + o0 + 16 * g + V * q, left - 16 * g - V * q);
 #pragma unroll
-                for (int q = 0; q < 16 / V; ++q) {
-                    Vec<float, V> u = 0.f;
-                    if (mine) u = load_some<TX, V>(base + t * c.ldbase + o0 + 16 * g + V * q, left - 16 * g - V * q);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) v[V * q + k] = u[k];
-                }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) acc[s][k % 4][k / 4] = v[k];
+                for (int k = 0; k < V; ++k) v[V * q + k] = u[k];
             }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[k % 4][k / 4] = v[k];
         }
         const int rank = a >= 0 ? rank_of(c.w, a) : 0;
         const TW* w = static_cast<const TW*>(c.w.w) + (a >= 0 ? a * c.w.stride : 0);
         for (int r0 = 0; r0 < rank; r0 += 16) {
-            const int at = r0 + 4 * g;
-            F4 ws[4];  // [j][element at + (0 .. 3)]
+            const int from = r0 + 4 * g;
+            F4 ws[4];  // [j][rank from + (0 .. 3)]
             if constexpr (kAlong) {  // w[r * ld + o]
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     F4 v = 0.f;
-                    if (at + q < rank) v = load_some<TW, 4>(w + (at + q) * c.w.ld + o0 + 4 * i, left - 4 * i);
+                    if (from + q < rank) v = load_some<TW, 4>(w + (from + q) * c.w.ld + o0 + 4 * i, left - 4 * i);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) ws[j][q] = v[j];
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ws[j] = 4 * i + j < left ? load_some<TW, 4>(w + (o0 + 4 * i + j) * c.w.ld + at, rank - at) : F4(0.f);
+                for (int j = 0; j < 4; ++j) ws[j] = 4 * i + j < left ? load_some<TW, 4>(w + (o0 + 4 * i + j) * c.w.ld + from, rank - from) : F4(0.f);
+            }
+            const F4 h = *reinterpret_cast<const F4*>(&room[i * pitch + from]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[j] = kColumns ? product(h[q], ws[j][q], acc[j]) : product(ws[j][q], h[q], acc[j]);
+        }
+        if constexpr (kColumns) {
+            bool own[4], all = true;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                own[k] = t + k < c.tokens && present.adapter[4 * g + k] == a;
+                all &= own[k];
             }
 #pragma unroll
-            for (int s = 0; s < kTiles; ++s) {
-                const F4 h = *reinterpret_cast<const F4*>(&hidden[(16 * s + i) * pitch + at]);
+            for (int j = 0; j < 4; ++j) {
+                if (4 * i + j >= left) continue;
+                TX* p = y + (o0 + 4 * i + j) * c.ldy + t;
+                if (all) {
+                    store_f32<TX, 4>(p, acc[j]);
+                } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                    for (int k = 0; k < 4; ++k)
+                        if (own[k]) p[k] = (TX)acc[j][k];
+                }
+            }
+        } else if (mine) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        acc[s][j] = kColumns ? product(h[q], ws[j][q], acc[s][j]) : product(ws[j][q], h[q], acc[s][j]);
+            for (int q = 0; q < 16 / V; ++q) {
+                Vec<float, V> u;
+#pragma unroll
+                for (int k = 0; k < V; ++k) u[k] = acc[(V * q + k) % 4][(V * q + k) / 4];
+                store_some<TX, V>(y + t * c.ldy + o0 + 16 * g + V * q, u, left - 16 * g - V * q);
             }
         }
+    }
+}
+
+template <class TX, class TW, bool kColumns, bool kAlong>
+__global__ __launch_bounds__(kBlock) void expand_kernel(ExpandArgs c) {
+    extern __shared__ float room[];
+    __shared__ Present present;
+    expand_some<TX, TW, kColumns, kAlong>(c, (int64_t)blockIdx.x * 16, blockIdx.y * c.blocks, c.blocks, blockIdx.y == 0, present, room);
+}
+
+// ---- expand, many tokens --------------------------------------------------------------------------------------------------------
+// A number as bf16 pieces that add up to it, the high bits first: each is cut (the last one rounded), so that none of them is larger
+// than the number and three hold all 24 bits of it down to 2^-133.  Infinities and NaN are their first piece alone.
+template <int kPieces>
+__device__ __forceinline__ void pieces_of(float x, uint16_t (&p)[kPieces]) {
 #pragma unroll
-        for (int s = 0; s < kTiles; ++s) {
-            if constexpr (kColumns) {
-                const int64_t t = t0 + 16 * s + 4 * g;
-                bool mine[4], all = true;
+    for (int k = 0; k < kPieces; ++k) {
+        if (k + 1 < kPieces) {
+            const uint32_t high = __float_as_uint(x) & 0xFFFF0000u;
+            p[k] = (uint16_t)(high >> 16);
+            x -= __uint_as_float(high);
+            x = x == x ? x : 0.f;
+        } else {
+            p[k] = __builtin_bit_cast(uint16_t, (__bf16)x);
+        }
+    }
+}
+template <class T>
+constexpr int kWeightPieces = sizeof(T) == 4 ? 3 : std::is_same_v<T, __bf16> ? 1 : 2;
+
+using Pieces8 = Vec<__bf16, 8>;
+
+// Eight weights as operands, one for each piece.
+template <class TW>
+__device__ __forceinline__ void weight_operands(const Vec<TW, 8> v, Pieces8 (&out)[kWeightPieces<TW>]) {
+    if constexpr (std::is_same_v<TW, __bf16>) {
+        out[0] = v;
+    } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    mine[k] = t + k < c.tokens && present.adapter[16 * s + 4 * g + k] == a;
-                    all &= mine[k];
+        for (int e = 0; e < 8; ++e) {
+            uint16_t p[kWeightPieces<TW>];
+            pieces_of<kWeightPieces<TW>>((float)v[e], p);
+#pragma unroll
+            for (int k = 0; k < kWeightPieces<TW>; ++k) out[k][e] = __builtin_bit_cast(__bf16, p[k]);
+        }
+    }
+}
+
+// 64 tokens.  A wave takes 64 elements of the long axis at a time, with what base has there in registers, and goes through the adapters, each
+// one's weights (ranks up to kChunks * 32; 0: any, loaded again for every tile) in registers.  Element o0 + 4 i + j is row (column) i of
+// tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as bf16 pieces by the weights' pieces in the 16-bit instruction, at an
+// eighth to a fifth of the 32-bit one's time: three pieces where y has 32 bits, two where it has 16 (2^-16 of hidden, an eighth of half a
+// step of y in fp16); products of pieces that are together below that are left out.
+template <class TX, class TW, bool kColumns, bool kAlong, int kChunks>
+__global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
+    constexpr int kTile = 64, kH = sizeof(TX) == 4 ? 3 : 2, kW = kWeightPieces<TW>, kHeld = kChunks ? kChunks : 1;
+    extern __shared__ float room[];
+    __shared__ Present present;
+    // the last workgroups take what the tiles of 64 by 64 leave: the last tokens, and the end of the long axis of the others
+    const int tiles = (int)(c.tokens / 64), blocks = (int)(c.length / 64), all_blocks = (int)((c.length + 63) / 64);
+    const unsigned inner = tiles * c.groups;
+    if (blockIdx.x >= inner) {
+        const int n = blockIdx.x - inner, behind = (int)((c.tokens - 64 * (int64_t)tiles + 15) / 16), each = (all_blocks + 3) / 4;
+        if (n < behind * each) expand_some<TX, TW, kColumns, kAlong>(c, 64 * (int64_t)tiles + n / each * 16, n % each * 4, std::min(4, all_blocks - n % each * 4), n % each == 0, present, room);
+        else expand_some<TX, TW, kColumns, kAlong>(c, (int64_t)(n - behind * each) * 16, blocks, 1, false, present, room);
+        return;
+    }
+    uint16_t* planes = reinterpret_cast<uint16_t*>(room);  // [piece][token][pitch]: hidden, 0 past the rank and for tokens without an adapter
+    const int64_t t0 = (int64_t)(blockIdx.x % tiles) * kTile;
+    const int group = blockIdx.x / tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+    const int rank32 = (c.w.rank + 31) / 32 * 32, pitch = rank32 + 8;
+    list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
+    const int slots = __builtin_amdgcn_readfirstlane(present.slots), jobs = slots + (__builtin_amdgcn_readfirstlane(present.none) && c.base != c.y ? 1 : 0);
+    if (jobs == 0 && !c.hidden) return;
+    {  // four threads for a token, four ranks at a time
+        const int t = threadIdx.x >> 2, a = present.adapter[t];
+        const int rank = a >= 0 ? rank_of(c.w, a) : 0;
+        const float scale = a >= 0 && c.scale ? scale_of(c.w, a) : 1.f;
+        for (int r = (threadIdx.x & 3) * 4; r < rank32; r += 16) {
+            F4 sum = 0.f;
+            const float* p = c.part + (t0 + t) * c.w.rank + r;
+#pragma unroll 4
+            for (uint32_t k = 0; k < c.parts; ++k) sum += load_some<float, 4>(p + k * c.tokens * c.w.rank, rank - r);
+            if (c.hidden && group == 0) store_some<float, 4>(c.hidden + (t0 + t) * c.w.rank + r, sum, c.w.rank - r);
+            sum *= scale;
+            uint16_t h[4][kH];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pieces_of<kH>(sum[e], h[e]);
+#pragma unroll
+            for (int k = 0; k < kH; ++k) {
+                const Vec<uint16_t, 4> v = {h[0][k], h[1][k], h[2][k], h[3][k]};
+                *reinterpret_cast<Vec<uint16_t, 4>*>(&planes[(k * kTile + t) * pitch + r]) = v;
+            }
+        }
+    }
+    __syncthreads();
+    const TX* base = static_cast<const TX*>(c.base);
+    TX* y = static_cast<TX*>(c.y);
+    const int first = group * c.blocks, last = std::min(first + (int)c.blocks, blocks);
+    // a lane's place: the rest of an address is the wave's
+    const uint32_t base_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldbase + 4 * i) * sizeof(TX), y_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldy + 4 * i) * sizeof(TX);
+    const uint32_t w_lane = (uint32_t)(kAlong ? 4 * i : 4 * i * c.w.ld) * sizeof(TW);
+    for (int block = first + wave; block < last; block += kWaves) {
+        const int64_t o0 = (int64_t)block * 64;
+        // A quarter of base, 64 x 64.  rows: [e], elements 4 i .. + 3 of token 16 u + 4 g + e; columns: [e], tokens 4 i .. + 3 of element
+        // 16 g + 4 e + u.  Sixteen neighbouring lanes have neighbouring memory: a load of one line for each of them would
+        // take the address unit sixteen times as long.
+        auto get = [&](int u, Vec<TX, 4> (&r)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (TX)0.f;
+            const uint32_t from = here(base_lane);
+            if (base)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    r[e] = load<TX, 4>(at(kColumns ? base + (o0 + 4 * e + u) * c.ldbase + t0 : base + (t0 + 16 * u + e) * c.ldbase + o0, from));
+        };
+        for (int q = 0; q < jobs; ++q) {
+            const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
+            const int rank = a >= 0 ? rank_of(c.w, a) : 0;
+            const TW* w = static_cast<const TW*>(c.w.w) + (a >= 0 ? a * c.w.stride : 0) + (kAlong ? o0 : o0 * c.w.ld);
+            auto weights = [&](int r0, Pieces8 (&ws)[4][kW]) {  // past the rank: 0, whatever is there; lanes there read the first eight ranks again
+                const bool mine = r0 + 8 * g < rank;
+                const uint32_t from = here(w_lane) + (uint32_t)(mine ? kAlong ? (r0 + 8 * g) * c.w.ld : r0 + 8 * g : 0) * sizeof(TW);
+                Vec<TW, 8> u[4];
+                if constexpr (kAlong) {  // w[r * ld + o]
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const Vec<TW, 4> v = load<TW, 4>(at(w + e * c.w.ld, from));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) u[j][e] = v[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) u[j] = load<TW, 8>(at(w + j * c.w.ld, from));
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (4 * i + j >= left) continue;
-                    TX* p = y + (o0 + 4 * i + j) * c.ldy + t;
-                    if (all) {
-                        store_f32<TX, 4>(p, acc[s][j]);
-                    } else {
+                    if (rank % 8)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (mine[k]) p[k] = (TX)acc[s][j][k];
+                        for (int e = 0; e < 8; ++e) u[j][e] = r0 + 8 * g + e < rank ? u[j][e] : (TW)0.f;
+                    else if (!mine)
+                        u[j] = (TW)0.f;
+                    weight_operands<TW>(u[j], ws[j]);
+                }
+            };
+            auto operand = [&](int k, int t, int r0) { return *reinterpret_cast<const Pieces8*>(&planes[(k * kTile + t) * pitch + r0 + 8 * g]); };
+            Vec<TX, 4> raw[2][4];  // this quarter's and the next one's
+            get(0, raw[0]);
+            Pieces8 held[kHeld][4][kW];
+            if constexpr (kChunks)
+                if (rank > 0)
+#pragma unroll
+                    for (int r = 0; r < kChunks; ++r) weights(32 * r, held[r]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {  // rows: tokens 16 u .. + 15, four tiles of elements; columns: elements 4 (0 .. 15) + u, four tiles of tokens
+                if (u < 3) get(u + 1, raw[(u + 1) % 2]);
+                // the adapters of the lane's tokens (rows: 16 u + 4 g + e; columns: 4 i + e)
+                const Vec<int, 4> of = *reinterpret_cast<const Vec<int, 4>*>(&present.adapter[kColumns ? 4 * i : 16 * u + 4 * g]);
+                if (!__any(of[0] == a || of[1] == a || of[2] == a || of[3] == a)) continue;
+                F4 acc[4];  // [tile][row 4 g + e]
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[v][e] = (float)raw[u % 2][e][v];
+                auto chunk = [&](int r0, const Pieces8 (&ws)[4][kW]) {
+#pragma unroll
+                    for (int k = 0; k < kH; ++k) {
+                        Pieces8 h;
+                        if constexpr (!kColumns) h = operand(k, 16 * u + i, r0);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            if constexpr (kColumns) h = operand(k, 4 * i + v, r0);
+#pragma unroll
+                            for (int l = 0; l < kW; ++l)
+                                if (k + l < kH) acc[v] = kColumns ? product(ws[u][l], h, acc[v]) : product(h, ws[v][l], acc[v]);
+                        }
+                    }
+                };
+                if (rank > 0) {
+                    if constexpr (kChunks) {
+#pragma unroll
+                        for (int r = 0; r < kChunks; ++r) chunk(32 * r, held[r]);
+                    } else {
+#pragma unroll 1
+                        for (int r0 = 0; r0 < rank; r0 += 32) {
+                            weights(r0, held[0]);
+                            chunk(r0, held[0]);
+                        }
                     }
                 }
-            } else {
-                const int64_t t = t0 + 16 * s + i;
-                if (t >= c.tokens || present.adapter[16 * s + i] != a) continue;
-                constexpr int V = 16 / sizeof(TX);
+                const uint32_t to = here(y_lane);
 #pragma unroll
-                for (int q = 0; q < 16 / V; ++q) {
-                    Vec<float, V> u;
+                for (int e = 0; e < 4; ++e) {
+                    const Vec<float, 4> v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+                    TX* p = at(kColumns ? y + (o0 + 4 * e + u) * c.ldy + t0 : y + (t0 + 16 * u + e) * c.ldy + o0, to);
+                    if constexpr (kColumns) {
+                        if (of[0] == a && of[1] == a && of[2] == a && of[3] == a) {
+                            store_f32<TX, 4>(p, v);
+                        } else {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) u[k] = acc[s][(V * q + k) % 4][(V * q + k) / 4];
-                    store_some<TX, V>(y + t * c.ldy + o0 + 16 * g + V * q, u, left - 16 * g - V * q);
+                            for (int m = 0; m < 4; ++m)
+                                if (of[m] == a) p[m] = (TX)v[m];
+                        }
+                    } else if (of[e] == a) {
+                        store_f32<TX, 4>(p, v);
+                    }
                 }
             }
         }
@@ -390,7 +623,8 @@ __global__ __launch_bounds__(kBlock) void expand_kernel(ExpandArgs c) {
 
 // ---- outer ----------------------------------------------------------------------------------------------------------------------
 struct OuterArgs {
-    const float* g;  // [tokens][rank]
+    const float* g;          // [tokens][rank]
+    const uint16_t* planes;  // the same as planes_kernel lays it out, times s_a; activations in 16 bits
     Weights w;       // adapters, ranks, scales
     const int32_t* index;
     int64_t tokens, length;
@@ -401,46 +635,76 @@ struct OuterArgs {
     bool scale;
 };
 
+// The groups of kGroup tokens in from .. to in which the adapter occurs, in their order, for up to kOuterBlock groups from `first` on: their numbers
+// into `list`; returns how many.  All threads call it.
+template <int kGroup>
+__device__ __forceinline__ int list_groups(const int32_t* index, int64_t first, int64_t to, int a, int* list, int* count) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t mine = first + (int64_t)threadIdx.x * kGroup;
+    bool some = false;
+    if (mine + kGroup <= to) {
+        Vec<int32_t, 4> of[kGroup / 4];
+#pragma unroll
+        for (int k = 0; k < kGroup / 4; ++k) of[k] = load<int32_t, 4>(index + mine + 4 * k);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) some |= of[k / 4][k % 4] == a;
+    } else if (mine < to) {
+        for (int64_t k = mine; k < to; ++k) some |= index[k] == a;
+    }
+    const unsigned long long here = __ballot(some);
+    if (lane == 0) count[wave] = __popcll(here);
+    __syncthreads();
+    int at = __popcll(here & ((1ull << lane) - 1)), groups = 0;
+    for (int k = 0; k < kOuterBlock / 64; ++k) {
+        if (k < wave) at += count[k];
+        groups += count[k];
+    }
+    if (some) list[at] = threadIdx.x;
+    __syncthreads();
+    return groups;
+}
+
+// The waves' sums of kSums registers each, in the first wave's: the upper half's to the lower half's, until there is one.
+template <int kSums>
+__device__ __forceinline__ void add_waves(F4 (&acc)[kSums], F4 (*room)[kSums][64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int half = kOuterBlock / 128; half; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int r = 0; r < kSums; ++r) room[wave - half][r][lane] = acc[r];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int r = 0; r < kSums; ++r) acc[r] += room[wave][r][lane];
+        __syncthreads();
+    }
+}
+
 // Adapter blockIdx.y, 64 elements of the long axis, kRanks * 16 ranks; the waves share out the groups of 16 tokens in which the adapter occurs.
 template <class TX, bool kColumns, bool kRankLast, int kRanks>
-__global__ __launch_bounds__(kBlock) void outer_kernel(OuterArgs c) {
-    constexpr int kGroups = 256;  // looked at together
-    __shared__ int list[kGroups];
-    __shared__ int count[kWaves];
-    __shared__ F4 sums[kWaves / 2][kRanks * 4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4, a = blockIdx.y;
+__global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
+    __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
+    __shared__ F4 room[kOuterBlock / 128][kRanks * 4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
     const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks);
-    const int64_t o0 = (int64_t)(blockIdx.x / rank_blocks) * 64, left = c.length - o0;
+    const int64_t o0 = (int64_t)(blockIdx.x / rank_blocks) * 64;
+    const int left = (int)std::min<int64_t>(c.length - o0, 64);
     const int r0 = (int)(blockIdx.x % rank_blocks) * 16 * kRanks;
     const int rank = rank_of(c.w, a);
     const int64_t from = blockIdx.z * c.range, to = from + c.range < c.tokens ? from + c.range : c.tokens;
-    F4 acc[kRanks][4];
+    F4 acc[kRanks * 4];  // [rank tile][j]
 #pragma unroll
-    for (int r = 0; r < kRanks; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[r][j] = 0.f;
-    for (int64_t first = from; first < to; first += kGroups * 16) {
-        // the groups, in their order
-        const int64_t mine = first + threadIdx.x * 16;
-        bool some = false;
-        for (int k = 0; k < 16; ++k) some |= mine + k < to && c.index[mine + k] == a;
-        const unsigned long long here = __ballot(some);
-        if (lane == 0) count[wave] = __popcll(here);
-        __syncthreads();
-        int at = __popcll(here & ((1ull << lane) - 1)), groups = 0;
-        for (int k = 0; k < kWaves; ++k) {
-            if (k < wave) at += count[k];
-            groups += count[k];
-        }
-        if (some) list[at] = threadIdx.x;
-        __syncthreads();
+    for (int r = 0; r < kRanks * 4; ++r) acc[r] = 0.f;
+    for (int64_t first = from; first < to; first += kOuterBlock * 16) {
+        const int groups = list_groups<16>(c.index, first, to, a, list, count);
         if (rank > r0)
-            for (int q = wave; q < groups; q += kWaves) {
+            for (int q = wave; q < groups; q += kOuterBlock / 64) {
                 const int64_t t = first + list[q] * 16 + 4 * g;  // lane group g has tokens t .. t + 3
+                const int some = (int)std::max<int64_t>(0, std::min<int64_t>(to - t, 4));
                 bool own[4], every = true;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    own[k] = t + k < to && c.index[t + k] == a;
+                    own[k] = k < some && c.index[t + k] == a;
                     every &= own[k];
                 }
                 every = __all(every);
@@ -449,7 +713,7 @@ __global__ __launch_bounds__(kBlock) void outer_kernel(OuterArgs c) {
                     F4 v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        v[j] = 4 * i + j < left && t < to ? load_some<TX, 4>(static_cast<const TX*>(c.x) + (o0 + 4 * i + j) * c.ldx + t, to - t) : F4(0.f);
+                        v[j] = 4 * i + j < left ? load_some<TX, 4>(static_cast<const TX*>(c.x) + (o0 + 4 * i + j) * c.ldx + t, some) : F4(0.f);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -457,7 +721,7 @@ __global__ __launch_bounds__(kBlock) void outer_kernel(OuterArgs c) {
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        xs[k] = t + k < to ? load_some<TX, 4>(static_cast<const TX*>(c.x) + (t + k) * c.ldx + o0 + 4 * i, left - 4 * i) : F4(0.f);
+                        xs[k] = k < some ? load_some<TX, 4>(static_cast<const TX*>(c.x) + (t + k) * c.ldx + o0 + 4 * i, left - 4 * i) : F4(0.f);
                 }
                 float gs[kRanks][4];
 #pragma unroll
@@ -473,26 +737,11 @@ __global__ __launch_bounds__(kBlock) void outer_kernel(OuterArgs c) {
 #pragma unroll
                     for (int r = 0; r < kRanks; ++r)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[r][j] = product(gs[r][k], xs[k][j], acc[r][j]);
+                        for (int j = 0; j < 4; ++j) acc[4 * r + j] = product(gs[r][k], xs[k][j], acc[4 * r + j]);
             }
         __syncthreads();  // the list is made anew
     }
-    // the waves' sums: the upper half to the lower one, twice
-#pragma unroll
-    for (int half = kWaves / 2; half; half /= 2) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int r = 0; r < kRanks; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sums[wave - half][4 * r + j][lane] = acc[r][j];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int r = 0; r < kRanks; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[r][j] += sums[wave][4 * r + j][lane];
-        __syncthreads();
-    }
+    add_waves(acc, room);
     if (wave) return;
     const float scale = c.scale ? scale_of(c.w, a) : 1.f;
     float* out = c.out + ((int64_t)blockIdx.z * c.w.adapters + a) * c.w.rank * c.length;
@@ -502,16 +751,151 @@ __global__ __launch_bounds__(kBlock) void outer_kernel(OuterArgs c) {
         if constexpr (kRankLast) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (4 * i + j < left && at < c.w.rank) store_some<float, 4>(out + (o0 + 4 * i + j) * c.w.rank + at, acc[r][j] * scale, c.w.rank - at);
+                if (4 * i + j < left && at < c.w.rank) store_some<float, 4>(out + (o0 + 4 * i + j) * c.w.rank + at, acc[4 * r + j] * scale, c.w.rank - at);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (at + k >= c.w.rank) continue;
                 F4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[r][j][k] * scale;
+                for (int j = 0; j < 4; ++j) v[j] = acc[4 * r + j][k] * scale;
                 store_some<float, 4>(out + (at + k) * c.length + o0 + 4 * i, v, left - 4 * i);
             }
+        }
+    }
+}
+
+// Activations in 16 bits, rows: the 16-bit instruction over 32 tokens.  It wants eight tokens of one element in a lane where memory has eight
+// elements of one token: a lane loads eight by eight (kCols = 8; 16 bytes of 8 tokens, sixteen lanes 256 bytes side by side) and
+// turns them in its registers.  The other operand, d or hidden as three bf16 pieces, lies in `planes` as lanes take it (planes_kernel); fp16
+// activations are two bf16 pieces.  Nothing is lost against products in 32 bits.
+template <class TX, bool kRankLast, int kRanks, int kCols>
+__global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterArgs c) {
+    constexpr int kX = kWeightPieces<TX>, kSums = kRanks * kCols;
+    __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
+    __shared__ F4 room[kOuterBlock / 128][kSums][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
+    const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks), rank_tiles = (c.w.rank + 15) / 16;
+    const int64_t o0 = (int64_t)(blockIdx.x / rank_blocks) * (16 * kCols);
+    const int left = (int)std::min<int64_t>(c.length - o0, 16 * kCols) - kCols * i;
+    const int tile0 = (int)(blockIdx.x % rank_blocks) * kRanks;
+    const int rank = rank_of(c.w, a);
+    const int64_t from = blockIdx.z * c.range, to = from + c.range < c.tokens ? from + c.range : c.tokens;
+    const uint32_t x_lane = (uint32_t)(8 * g * c.ldx + kCols * i) * sizeof(TX);
+    F4 acc[kSums];  // [rank tile][column]
+#pragma unroll
+    for (int r = 0; r < kSums; ++r) acc[r] = 0.f;
+    for (int64_t first = from; first < to; first += kOuterBlock * 32) {
+        const int groups = list_groups<32>(c.index, first, to, a, list, count);
+        if (rank > 16 * tile0)
+            for (int q = wave; q < groups; q += kOuterBlock / 64) {
+                const int64_t t = first + __builtin_amdgcn_readfirstlane(list[q]) * 32;
+                const TX* x = static_cast<const TX*>(c.x) + t * c.ldx + o0;
+                Vec<TX, kCols> xs[8];
+                Vec<int32_t, 8> of;
+                const bool whole = t + 32 <= to;
+                if (whole && left >= kCols) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xs[e] = load<TX, kCols>(at(x + e * c.ldx, x_lane));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xs[e] = t + 8 * g + e < to ? load_own<TX, kCols>(at(x + e * c.ldx, x_lane), left) : Vec<TX, kCols>((TX)0.f);
+                }
+                Pieces8 gs[kRanks][3];
+                const Pieces8* planes = reinterpret_cast<const Pieces8*>(c.planes) + (t / 32 * 3 * rank_tiles + tile0) * 64 + lane;
+#pragma unroll
+                for (int r = 0; r < kRanks; ++r)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) gs[r][p] = planes[(p * rank_tiles + std::min(r, rank_tiles - 1 - tile0)) * 64];
+                if (whole) {
+                    of = load<int32_t, 8>(c.index + t + 8 * g);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) of[e] = t + 8 * g + e < to ? c.index[t + 8 * g + e] : -1;
+                }
+                bool every = true;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) every &= of[e] == a;
+                if (!__all(every)) {  // other adapters' tokens, whatever they hold
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (of[e] == a) continue;
+                        xs[e] = (TX)0.f;
+#pragma unroll
+                        for (int r = 0; r < kRanks; ++r)
+#pragma unroll
+                            for (int p = 0; p < 3; ++p) gs[r][p][e] = (__bf16)0.f;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) {
+                    const Vec<TX, 8> column = {xs[0][k], xs[1][k], xs[2][k], xs[3][k], xs[4][k], xs[5][k], xs[6][k], xs[7][k]};
+                    Pieces8 ps[kX];
+                    weight_operands<TX>(column, ps);
+#pragma unroll
+                    for (int r = 0; r < kRanks; ++r)
+#pragma unroll
+                        for (int p = 0; p < 3; ++p)
+#pragma unroll
+                            for (int l = 0; l < kX; ++l)
+                                if (p + l < 3) acc[r * kCols + k] = product(gs[r][p], ps[l], acc[r * kCols + k]);
+                }
+            }
+        __syncthreads();  // the list is made anew
+    }
+    add_waves(acc, room);
+    if (wave) return;
+    float* out = c.out + ((int64_t)blockIdx.z * c.w.adapters + a) * c.w.rank * c.length;
+#pragma unroll
+    for (int r = 0; r < kRanks; ++r) {
+        const int at = 16 * (tile0 + r) + 4 * g;
+        // a rank past the adapter's own: the planes have 0 there
+        if constexpr (kRankLast) {
+#pragma unroll
+            for (int k = 0; k < kCols; ++k)
+                if (k < left && at < c.w.rank) store_some<float, 4>(out + (o0 + kCols * i + k) * c.w.rank + at, acc[r * kCols + k], c.w.rank - at);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (at + e >= c.w.rank) continue;
+                Vec<float, kCols> v;
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) v[k] = acc[r * kCols + k][e];
+                store_some<float, kCols>(out + (at + e) * c.length + o0 + kCols * i, v, left);
+            }
+        }
+    }
+}
+
+// What outer16_kernel takes of d and hidden: pieces p = 0 .. 2 of [tokens][rank], for 32 tokens and 16 ranks lane by lane: element (token t, rank r)
+// at ((((t / 32) 3 + p) rank tiles + r / 16) 64 + r % 16 + 16 (t % 32 / 8)) 8 + t % 8; 0 for tokens without an adapter, past an adapter's rank and
+// past the last token.  A workgroup for 32 tokens: blockIdx.y = 0: d, from the parts that `shrink` has left, times s_a, which is also
+// written as numbers in 32 bits (c.out); 1: hidden times s_a.
+__global__ __launch_bounds__(kBlock) void planes_kernel(ShrinkArgs c, const float* part, uint32_t parts, const float* hidden, uint16_t* d_planes, uint16_t* hidden_planes) {
+    const bool is_d = blockIdx.y == 0;
+    uint16_t* planes = is_d ? d_planes : hidden_planes;
+    const float* from = is_d ? part : hidden;
+    const int rank_tiles = (c.w.rank + 15) / 16;
+    const int64_t all = c.tokens * c.w.rank, t = (int64_t)blockIdx.x * 32 + threadIdx.x / 8;
+    const int a = adapter_at(c.index, t, c.tokens, c.w.adapters);
+    const int rank = a >= 0 ? rank_of(c.w, a) : 0;
+    const float scale = a >= 0 ? scale_of(c.w, a) : 0.f;
+    for (int r = (threadIdx.x % 8) * 4; r < 16 * rank_tiles; r += 32) {
+        F4 sum = 0.f;
+        if (r < rank) {
+#pragma unroll 4
+            for (uint32_t k = 0; k < (is_d ? parts : 1); ++k) sum += load_some<float, 4>(from + k * all + t * c.w.rank + r, rank - r);
+        }
+        sum *= scale;
+        if (is_d && t < c.tokens) store_some<float, 4>(c.out + t * c.w.rank + r, sum, c.w.rank - r);
+        if (!planes) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint16_t p[3];
+            pieces_of<3>(sum[e], p);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                planes[((((int64_t)blockIdx.x * 3 + k) * rank_tiles + r / 16) * 64 + (r + e) % 16 + 16 * (t % 32 / 8)) * 8 + t % 8] = p[k];
         }
     }
 }
@@ -530,11 +914,11 @@ __global__ __launch_bounds__(kBlock) void outer_sum_kernel(const float* part, ui
 struct ShrinkShape {
     int tiles, ranks, parts;
     int64_t part;
-    ShrinkShape(int64_t tokens, int64_t rank, int64_t length) {
+    ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns) {
         ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
-        tiles = tokens <= 256 ? 1 : tokens <= 1024 || ranks == 8 ? 2 : 4;
+        tiles = tokens <= kFewTokens ? 1 : ranks < 8 ? 4 : columns ? 1 : 2;
         const int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((1024 + blocks - 1) / blocks, (length + 255) / 256));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (length + 255) / 256, 32}));
         part = ((length + want - 1) / want + 31) / 32 * 32;
         parts = (int)((length + part - 1) / part);
     }
@@ -543,16 +927,20 @@ struct ShrinkShape {
 template <class TX, class TW, bool kColumns, bool kAlong, int kTiles>
 int shrink_ranks(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
     const dim3 grid((unsigned)((c.tokens + 16 * kTiles - 1) / (16 * kTiles)), f.parts, (unsigned)((c.w.rank + 16 * f.ranks - 1) / (16 * f.ranks)));
-    if (f.ranks == 1) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 1><<<grid, kBlock, 0, s>>>(c);
-    else if (f.ranks == 2) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 2><<<grid, kBlock, 0, s>>>(c);
-    else if (f.ranks == 4) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 4><<<grid, kBlock, 0, s>>>(c);
-    else if constexpr (kTiles <= 2) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 8><<<grid, kBlock, 0, s>>>(c);
+    if constexpr (kTiles != 2) {
+        if (f.ranks == 1) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 1><<<grid, kShrinkBlock, 0, s>>>(c);
+        else if (f.ranks == 2) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 2><<<grid, kShrinkBlock, 0, s>>>(c);
+        else if (f.ranks == 4) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 4><<<grid, kShrinkBlock, 0, s>>>(c);
+    }
+    if constexpr (kTiles != 4)
+        if (f.ranks == 8) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 8><<<grid, kShrinkBlock, 0, s>>>(c);
     return (int)hipGetLastError();
 }
 template <class TX, class TW, bool kColumns, bool kAlong>
 int shrink_tiles(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
     if (f.tiles == 1) return shrink_ranks<TX, TW, kColumns, kAlong, 1>(c, f, s);
-    if (f.tiles == 2) return shrink_ranks<TX, TW, kColumns, kAlong, 2>(c, f, s);
+    if constexpr (!kColumns)
+        if (f.tiles == 2) return shrink_ranks<TX, TW, kColumns, kAlong, 2>(c, f, s);
     return shrink_ranks<TX, TW, kColumns, kAlong, 4>(c, f, s);
 }
 template <bool kAlong>
@@ -568,14 +956,29 @@ int shrink(ShrinkArgs c, const ShrinkShape& f, const cer_tokens_t& x, int32_t we
 
 template <class TX, class TW, bool kColumns, bool kAlong>
 int expand_tiles(ExpandArgs c, hipStream_t s) {
-    const int tiles = c.tokens <= 256 ? 1 : c.tokens <= 1024 || c.w.rank > 128 ? 2 : 4;
-    const int64_t across = (c.tokens + 16 * tiles - 1) / (16 * tiles), blocks = (c.length + 63) / 64;
-    c.blocks = across * blocks >= 2048 ? 4 : 1;
-    const dim3 grid((unsigned)across, (unsigned)((blocks + c.blocks - 1) / c.blocks));
-    const size_t lds = (size_t)16 * tiles * ((c.w.rank + 15) / 16 * 16 + 4) * 4;
-    if (tiles == 1) expand_kernel<TX, TW, kColumns, kAlong, 1><<<grid, kBlock, lds, s>>>(c);
-    else if (tiles == 2) expand_kernel<TX, TW, kColumns, kAlong, 2><<<grid, kBlock, lds, s>>>(c);
-    else expand_kernel<TX, TW, kColumns, kAlong, 4><<<grid, kBlock, lds, s>>>(c);
+    const int64_t blocks = (c.length + 63) / 64;
+    const size_t few = (size_t)16 * ((c.w.rank + 15) / 16 * 16 + 4) * 4;
+    // ranks in eights: a load takes eight of a row and must not leave it
+    if (c.tokens <= kFewTokens || c.length < 64 || c.w.rank % 8) {
+        const int64_t across = (c.tokens + 15) / 16;
+        c.blocks = across * blocks >= 2048 ? 4 : 1;
+        const dim3 grid((unsigned)across, (unsigned)((blocks + c.blocks - 1) / c.blocks));
+        expand_kernel<TX, TW, kColumns, kAlong><<<grid, kBlock, few, s>>>(c);
+    } else {
+        // the tokens' hidden is made ready once for a workgroup: as many blocks for each as leave about four workgroups for a compute unit
+        const int64_t across = c.tokens / 64, most = std::max<int64_t>(1, 1024 / across), whole = c.length / 64;
+        c.blocks = (uint32_t)std::max<int64_t>(kWaves, (whole + most - 1) / most);
+        c.groups = (uint32_t)((whole + c.blocks - 1) / c.blocks);
+        const int64_t ends = (c.tokens % 64 + 15) / 16 * ((blocks + 3) / 4) + (c.length % 64 ? across * 4 : 0);
+        const size_t lds = std::max(few, (size_t)(sizeof(TX) == 4 ? 3 : 2) * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
+        constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1;  // times 32 ranks, in registers
+        const auto kernel = c.w.rank <= 32           ? expand_wide_kernel<TX, TW, kColumns, kAlong, 1>
+                            : c.w.rank <= 32 * kMost ? expand_wide_kernel<TX, TW, kColumns, kAlong, kMost>
+                                                     : expand_wide_kernel<TX, TW, kColumns, kAlong, 0>;
+        if (lds > 60 * 1024)  // ranks over 160 in 32 bits
+            if (int e = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+        kernel<<<(unsigned)(across * c.groups + ends), kBlock, lds, s>>>(c);
+    }
     return (int)hipGetLastError();
 }
 template <bool kAlong>
@@ -593,26 +996,36 @@ template <class TX, bool kColumns, bool kRankLast>
 int outer_ranks(const OuterArgs& c, unsigned parts, hipStream_t s) {
     const int ranks = c.w.rank <= 16 ? 1 : c.w.rank <= 32 ? 2 : 4;
     const dim3 grid((unsigned)((c.length + 63) / 64 * ((c.w.rank + 16 * ranks - 1) / (16 * ranks))), (unsigned)c.w.adapters, parts);
-    if (ranks == 1) outer_kernel<TX, kColumns, kRankLast, 1><<<grid, kBlock, 0, s>>>(c);
-    else if (ranks == 2) outer_kernel<TX, kColumns, kRankLast, 2><<<grid, kBlock, 0, s>>>(c);
-    else outer_kernel<TX, kColumns, kRankLast, 4><<<grid, kBlock, 0, s>>>(c);
+    if (ranks == 1) outer_kernel<TX, kColumns, kRankLast, 1><<<grid, kOuterBlock, 0, s>>>(c);
+    else if (ranks == 2) outer_kernel<TX, kColumns, kRankLast, 2><<<grid, kOuterBlock, 0, s>>>(c);
+    else outer_kernel<TX, kColumns, kRankLast, 4><<<grid, kOuterBlock, 0, s>>>(c);
+    return (int)hipGetLastError();
+}
+template <class TX, bool kRankLast>
+int outer16_ranks(const OuterArgs& c, unsigned parts, hipStream_t s) {
+    const int ranks = c.w.rank <= 16 ? 1 : c.w.rank <= 32 ? 2 : 4, cols = ranks == 4 ? 4 : 8;
+    const dim3 grid((unsigned)((c.length + 16 * cols - 1) / (16 * cols) * ((c.w.rank + 16 * ranks - 1) / (16 * ranks))), (unsigned)c.w.adapters, parts);
+    if (ranks == 1) outer16_kernel<TX, kRankLast, 1, 8><<<grid, kOuterBlock, 0, s>>>(c);
+    else if (ranks == 2) outer16_kernel<TX, kRankLast, 2, 8><<<grid, kOuterBlock, 0, s>>>(c);
+    else outer16_kernel<TX, kRankLast, 4, 4><<<grid, kOuterBlock, 0, s>>>(c);
     return (int)hipGetLastError();
 }
 
-// The tokens are cut into ranges where an adapter's workgroups alone would be few or one of them long: parts of up to 2048 tokens.
+// The tokens are cut into ranges where an adapter's workgroups alone would be few: up to about 1024 workgroups, 512 tokens at least.
 template <bool kRankLast>
 int outer(OuterArgs c, const cer_tokens_t& x, hipStream_t s) {
     c.x = x.data, c.ldx = x.ld;
-    const unsigned parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>(8, c.tokens / 1024));
-    c.range = ((c.tokens + parts - 1) / parts + 15) / 16 * 16;
+    const int64_t without = c.w.adapters * ((c.length + 127) / 128);
+    const unsigned parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>({16, c.tokens / 512, 1024 / without}));
+    c.range = ((c.tokens + parts - 1) / parts + 31) / 32 * 32;
     const int64_t numbers = c.w.adapters * c.w.rank * c.length;
     float* out = c.out;
     Temporary t(parts > 1 ? (size_t)parts * numbers * 4 : 0, s);
     if (t.error) return t.error;
     if (parts > 1) c.out = t.floats();
     int e;
-    if (x.type == CER_TYPE_BF16) e = outer_ranks<__bf16, false, kRankLast>(c, parts, s);
-    else if (x.type == CER_TYPE_F16) e = outer_ranks<_Float16, false, kRankLast>(c, parts, s);
+    if (x.type == CER_TYPE_BF16) e = outer16_ranks<__bf16, kRankLast>(c, parts, s);
+    else if (x.type == CER_TYPE_F16) e = outer16_ranks<_Float16, kRankLast>(c, parts, s);
     else if (x.order == CER_ORDER_COLUMNS) e = outer_ranks<float, true, kRankLast>(c, parts, s);
     else e = outer_ranks<float, false, kRankLast>(c, parts, s);
     if (!e && parts > 1) {
@@ -632,11 +1045,11 @@ Weights side_b(const cer_adapters_t& w) { return {w.B, w.stride_b, w.ld_b, w.ran
 }  // namespace
 
 int64_t adapter_workspace(int64_t tokens, int64_t rank, int64_t in, int64_t) {
-    return ShrinkShape(tokens, rank, in).parts * tokens * rank * 4;
+    return std::max(ShrinkShape(tokens, rank, in, false).parts, ShrinkShape(tokens, rank, in, true).parts) * tokens * rank * 4;
 }
 
 int launch_adapters(const AdapterCall& c, hipStream_t s) {
-    const ShrinkShape f(c.tokens, c.w.rank, c.w.in);
+    const ShrinkShape f(c.tokens, c.w.rank, c.w.in, c.x.order == CER_ORDER_COLUMNS);
     const int64_t bytes = adapter_workspace(c.tokens, c.w.rank, c.w.in, c.w.out);
     Temporary t(c.workspace ? 0 : (size_t)bytes, s);
     if (t.error) return t.error;
@@ -656,37 +1069,51 @@ int launch_adapters_backward(const AdapterBackwardCall& c, hipStream_t s) {
             if (int e = clear(c.dA, c.w.adapters * c.w.rank * c.w.in, s)) return e;
         return c.dB ? clear(c.dB, c.w.adapters * c.w.rank * c.w.out, s) : 0;
     }
-    const ShrinkShape f(c.tokens, c.w.rank, c.w.out);
+    const ShrinkShape f(c.tokens, c.w.rank, c.w.out, c.dy.order == CER_ORDER_COLUMNS);
     const int64_t one = c.tokens * c.w.rank;
-    if (c.dx.data || c.dA) {
-        Temporary t((size_t)(f.parts > 1 ? f.parts + 1 : 1) * one * 4, s);
-        if (t.error) return t.error;
-        float* d = t.floats();
-        ShrinkArgs a{};
-        a.w = side_b(c.w), a.index = c.index, a.tokens = c.tokens, a.length = c.w.out;
-        a.out = f.parts > 1 ? d + one : d, a.scale = f.parts == 1;
+    const bool d_wanted = c.dx.data || c.dA, k16 = c.dy.type != CER_TYPE_F32;
+    // d, the parts of it, and the planes of d and hidden
+    const int64_t parts = d_wanted && (f.parts > 1 || k16) ? f.parts : 0;
+    const int64_t plane_floats = k16 ? (c.tokens + 31) / 32 * ((c.w.rank + 15) / 16) * (32 * 16 * 3 / 2) : 0;
+    const int64_t place = (one + 63) / 64 * 64;
+    Temporary t((size_t)((1 + parts) * place + 2 * plane_floats) * 4, s);
+    if (t.error) return t.error;
+    float *d = t.floats(), *part = d + place;
+    uint16_t* d_planes = c.dA && k16 ? reinterpret_cast<uint16_t*>(d + (1 + parts) * place) : nullptr;
+    uint16_t* hidden_planes = c.dB && k16 ? reinterpret_cast<uint16_t*>(d + (1 + parts) * place + plane_floats) : nullptr;
+    ShrinkArgs a{};
+    a.w = side_b(c.w), a.index = c.index, a.tokens = c.tokens, a.length = c.w.out;
+    if (d_wanted) {
+        a.out = parts ? part : d, a.scale = !parts;
         if (int e = shrink<false>(a, f, c.dy, c.w.type, s)) return e;
-        if (f.parts > 1) {
-            a.out = d, a.scale = true;
-            shrink_sum_kernel<<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, d + one, (uint32_t)f.parts);
+    }
+    a.out = d, a.scale = true;
+    if (k16) {
+        const unsigned first = d_wanted ? 0 : 1, last = c.dB ? 2 : 1;
+        if (first < last) {
+            // where hidden alone is wanted, its half of the grid runs behind an empty one
+            planes_kernel<<<dim3((unsigned)((c.tokens + 31) / 32), last), kBlock, 0, s>>>(a, part, d_wanted ? (uint32_t)f.parts : 0, c.hidden, d_planes, hidden_planes);
             if (int e = (int)hipGetLastError()) return e;
         }
-        if (c.dA) {  // before dx, which may lie where x does
-            OuterArgs o{};
-            o.g = d, o.w = side_a(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.in, o.out = c.dA;
-            if (int e = outer<false>(o, c.x, s)) return e;
-        }
-        if (c.dx.data) {
-            ExpandArgs b{};
-            b.w = side_a(c.w), b.index = c.index, b.tokens = c.tokens, b.length = c.w.in;
-            b.part = d, b.parts = 1;
-            if (int e = expand<true>(b, c.base, c.dx, c.w.type, s)) return e;
-        }
+    } else if (parts) {
+        shrink_sum_kernel<<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, part, (uint32_t)f.parts);
+        if (int e = (int)hipGetLastError()) return e;
+    }
+    if (c.dA) {  // before dx, which may lie where x does
+        OuterArgs o{};
+        o.g = d, o.planes = d_planes, o.w = side_a(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.in, o.out = c.dA;
+        if (int e = outer<false>(o, c.x, s)) return e;
     }
     if (c.dB) {
         OuterArgs o{};
-        o.g = c.hidden, o.w = side_b(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.out, o.out = c.dB, o.scale = true;
+        o.g = c.hidden, o.planes = hidden_planes, o.w = side_b(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.out, o.out = c.dB, o.scale = true;
         if (int e = outer<true>(o, c.dy, s)) return e;
+    }
+    if (c.dx.data) {
+        ExpandArgs b{};
+        b.w = side_a(c.w), b.index = c.index, b.tokens = c.tokens, b.length = c.w.in;
+        b.part = d, b.parts = 1;
+        return expand<true>(b, c.base, c.dx, c.w.type, s);
     }
     return 0;
 }

@@ -9,7 +9,7 @@
 namespace {
 using namespace cer;
 
-constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535;
+constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 24;
 
 int bytes_of(int type) { return type == CER_TYPE_F32 ? 4 : type == CER_TYPE_F8 ? 1 : 2; }
 bool number_type(int type) { return type == CER_TYPE_F32 || type == CER_TYPE_BF16 || type == CER_TYPE_F16; }
@@ -41,11 +41,12 @@ int check_adapters(const cer_adapters_t* w, int64_t tokens) {
     if (w->rank > kMostRank || w->adapters > kMostAdapters || w->in > kMostFeatures || w->out > kMostFeatures || tokens > kMostTokens) return CER_E_TOO_LARGE;
     if (tokens * w->rank >= (int64_t)1 << 31 || w->adapters * w->rank * std::max(w->in, w->out) > (int64_t)1 << 33) return CER_E_TOO_LARGE;
     if (reinterpret_cast<uintptr_t>(w->A) % bytes_of(w->type) || reinterpret_cast<uintptr_t>(w->B) % bytes_of(w->type)) return CER_E_INVALID;
-    constexpr int64_t most = (int64_t)1 << 40;  // of a stride, so that no product of one with an index overflows
     if (w->stride_a < 0 || w->stride_b < 0 || w->ld_a < 0 || w->ld_b < 0) return CER_E_INVALID;
-    if (w->stride_a > most || w->stride_b > most || w->ld_a > most || w->ld_b > most) return CER_E_TOO_LARGE;
+    // of strides: no product of one with an index overflows, and the kernels' offsets within a tile fit 32 bits
+    if (std::max(w->stride_a, w->stride_b) > (int64_t)1 << 40 || std::max(w->ld_a, w->ld_b) > kMostLd) return CER_E_TOO_LARGE;
     return CER_OK;
 }
+bool near(const cer_tokens_t* m) { return !there(m) || m->ld <= kMostLd; }
 // Activations beside adapters of this type.
 bool fits(const cer_tokens_t* m, const cer_adapters_t* w) { return m->type == CER_TYPE_F32 || m->type == w->type; }
 }  // namespace
@@ -96,6 +97,7 @@ int adapter_matmul(const cer_adapters_t* w, const int32_t* index, int64_t tokens
     if (tokens == 0) return CER_OK;
     if (!index || !good(X, tokens, w->in, false) || !good(Y, tokens, w->out, true) || !alike(X, Y) || !fits(X, w)) return CER_E_INVALID;
     if (there(base) && !(good(base, tokens, w->out, false) && alike(base, Y) && same_or_apart(base, Y))) return CER_E_INVALID;
+    if (!near(X) || !near(base) || !near(Y)) return CER_E_TOO_LARGE;
     if (workspace && (workspace_bytes < adapter_workspace(tokens, w->rank, w->in, w->out) || reinterpret_cast<uintptr_t>(workspace) % 4)) return CER_E_INVALID;
     AdapterCall c{*w, index, tokens, *X, or_none(base), *Y, hidden, workspace, workspace_bytes};
     return result(launch_adapters(c, static_cast<hipStream_t>(stream)));
@@ -110,6 +112,7 @@ int adapter_backward(const cer_adapters_t* w, const int32_t* index, int64_t toke
         if (dB && !hidden) return CER_E_INVALID;
         if (there(dX) && !(good(dX, tokens, w->in, true) && alike(dX, dY))) return CER_E_INVALID;
         if (there(dX) && there(base) && !(good(base, tokens, w->in, false) && alike(base, dX) && same_or_apart(base, dX))) return CER_E_INVALID;
+        if (!near(dY) || !near(X) || !near(base) || !near(dX)) return CER_E_TOO_LARGE;
     }
     AdapterBackwardCall c{*w, index, tokens, or_none(dY), or_none(X), or_none(base), or_none(dX), hidden, dA, dB};
     return result(launch_adapters_backward(c, static_cast<hipStream_t>(stream)));
