@@ -542,7 +542,7 @@ int rms_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_t
  * Low-rank adapters of many requests beside one projection.  Adapter a of `adapters` has A_a [rank][in], B_a [out][rank], both of `type`, each
  * row contiguous: element (r, k) of A_a at A[a * stride_a + r * ld_a + k], (o, r) of B_a at B[a * stride_b + o * ld_b + r]; a factor
  * scales[a] (NULL: 1) and a rank of its own ranks[a] (NULL: rank; what is past it is not read, outside 0 .. rank it counts as the nearer
- * one).  1 <= rank <= 256, adapters <= 65535, leading dimensions up to 2^24.
+ * one).  1 <= rank <= 256, adapters <= 65535, leading dimensions up to 2^22.
  * `index` [tokens] names each token's adapter; tokens with an index outside 0 .. adapters - 1 have none.  Tokens of one adapter need not be
  * neighbours, but the work is shared best where they are (requests one after the other).
  * Types: activations and adapters of the same type, or fp32 activations (either order) beside bf16 or fp16 adapters.

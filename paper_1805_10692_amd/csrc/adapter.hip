@@ -29,7 +29,7 @@ namespace {
 
 using F4 = Vec<float, 4>;
 constexpr int kBlock = 256, kWaves = kBlock / 64;
-constexpr int kShrinkBlock = 512, kOuterBlock = 256;
+constexpr int kShrinkBlock = 512, kOuterBlock = 256, kRowsBlock = 512;
 constexpr int kMostTile = 64;  // tokens of a workgroup
 constexpr int64_t kFewTokens = 256;
 
@@ -111,6 +111,13 @@ __device__ __forceinline__ uint32_t here(uint32_t bytes) {
     return bytes;
 }
 
+// Workgroup n of `all` as neighbours want it: the eight XCDs take workgroups in turn and have an L2 each, so that an eighth of the work items, one after the
+// other, goes to each: neighbouring tokens mostly have the same adapter, and its weights then come into one L2 or two and not into all of them.
+__device__ __forceinline__ unsigned by_xcd(unsigned n, unsigned all) {
+    const unsigned each = all / 8, more = all % 8, xcd = n % 8;
+    return xcd * each + (xcd < more ? xcd : more) + n / 8;
+}
+
 // ---- shrink ---------------------------------------------------------------------------------------------------------------------
 struct ShrinkArgs {
     Weights w;
@@ -118,9 +125,10 @@ struct ShrinkArgs {
     int64_t tokens, length;  // of the long axis
     const void* x;
     int64_t ldx;
-    int64_t part;  // elements of the long axis for a workgroup (blockIdx.y), a multiple of 32
-    float* out;    // [gridDim.y][tokens][rank]
-    bool scale;    // times s_a
+    int64_t part;    // elements of the long axis for a workgroup, a multiple of 64
+    uint32_t parts;  // of the long axis
+    float* out;      // [parts][tokens][rank]
+    bool scale;      // times s_a
 };
 
 // kTiles * 16 tokens, kRanks * 16 ranks from blockIdx.z on; the waves share out the adapters and pieces of the workgroup's part of the long
@@ -134,13 +142,14 @@ __global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void s
     using Operand = std::conditional_t<k16, Vec<TX, E>, Vec<float, E>>;
     __shared__ Present present;
     __shared__ float sums[kTile][kPitch];
-    const int64_t t0 = (int64_t)blockIdx.x * kTile;
+    const unsigned item = by_xcd(blockIdx.x, gridDim.x), part = item % c.parts;
+    const int64_t t0 = (int64_t)(item / c.parts) * kTile;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
     list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
     const int slots = __builtin_amdgcn_readfirstlane(present.slots);
     const int abreast = kTiles > 1 ? 1 : slots >= 8 ? 8 : slots >= 4 ? 4 : slots >= 2 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
     // the workgroup's part of the long axis; its waves take turns, so that together they read neighbouring lines
-    const int from = blockIdx.y * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
+    const int from = part * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
     constexpr int kAhead = k16 && kTiles * kRanks <= 4 ? 4 : kTiles * kRanks <= (kTiles == 1 && !k16 ? 4 : 8) ? 2 : 1;  // steps whose loads are on their way together
     constexpr int kRun = kAhead * kStep;
     int token[kTiles];  // in the tile
@@ -264,7 +273,7 @@ __global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void s
             __syncthreads();
         }
     }
-    float* out = c.out + (int64_t)blockIdx.y * c.tokens * c.w.rank;
+    float* out = c.out + part * c.tokens * c.w.rank;
     for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kShrinkBlock) {
         const int t = e / (16 * kRanks), r = e % (16 * kRanks);
         if (t0 + t >= c.tokens || r0 + r >= c.w.rank) continue;
@@ -273,6 +282,184 @@ __global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void s
         if (c.scale && a >= 0) all *= scale_of(c.w, a);
         out[(t0 + t) * c.w.rank + r0 + r] = all;
     }
+}
+
+// Rows, many tokens.  64 tokens, 16 for each of four waves, and 128 (16 bits) or 64 elements of the long axis at a time, half of them for each of two
+// such sets of waves.  A lane's operand of x is a line of
+// its own (a token's), which costs the address unit 64 clocks for a load of 1 KiB: that much of a compute unit's time pays for x, once,
+// and not for the weights too.  Those come by neighbouring lanes into LDS, for up to two adapters of the tile together -- a tile in which one
+// request ends and the next one begins costs hardly more than another one, and is not what the launch waits for.  x is requested
+// kAhead steps before its use, the weights one.
+template <class TX, class TW, bool kAlong, int kRanks>
+__global__ __launch_bounds__(kRowsBlock, kRanks == 8 ? 2 : 4) void shrink_rows_kernel(ShrinkArgs c) {
+    constexpr bool k16 = sizeof(TX) == 2;
+    constexpr int kChunk = k16 ? 128 : 64, kHalves = kChunk / 64, kTile = 64, kAhead = k16 && kRanks < 4 ? 3 : 2, R = 16 * kRanks;
+    constexpr int kRow = kChunk + 16 / (int)sizeof(TW);               // of a rank in LDS
+    constexpr int V = 16 / (int)sizeof(TW);                           // elements of a load
+    constexpr int kLoads = (R * kChunk / V + kRowsBlock - 1) / kRowsBlock;  // of a thread for an adapter's chunk
+    using Operand = std::conditional_t<k16, Vec<TX, 8>, Vec<float, 8>>;
+    __shared__ Present present;
+    __shared__ TW staged[2][2][R][kRow];  // [turn][slot]
+    const unsigned item = by_xcd(blockIdx.x, gridDim.x), part = item % c.parts;
+    const int64_t t0 = (int64_t)(item / c.parts) * kTile;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, set = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * R;
+    const int from = part * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
+    const int tokens_left = (int)std::min<int64_t>(c.tokens - t0, kTile);
+    const TX* x = static_cast<const TX*>(c.x) + t0 * c.ldx;
+    const uint32_t x_lane = (uint32_t)(std::min(16 * wave + i, tokens_left - 1) * c.ldx + 8 * g) * sizeof(TX);
+    auto x_of = [&](int k, Operand (&v)[kHalves]) {
+        k += set * (kChunk / 2);
+        if (k + kChunk / 2 <= to) {
+            const uint32_t place = here(x_lane);
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                if constexpr (k16) v[h] = load<TX, 8>(at(x + k + 32 * h, place));
+                else v[h] = load_f32<TX, 8>(at(x + k + 32 * h, place));
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int left = to - (k + 32 * h + 8 * g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[h][e] = (TX)0.f;
+                    if (e < left) v[h][e] = at(x + k + 32 * h, x_lane)[e];
+                }
+            }
+        }
+    };
+    Operand xs[kAhead][kHalves];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x_of(from + u * kChunk, xs[u]);
+    list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
+    const int slots = __builtin_amdgcn_readfirstlane(present.slots), own = present.adapter[16 * wave + i];
+    float* out = c.out + (part * c.tokens + t0) * c.w.rank;
+    for (int first = 0; first < slots; first += 2) {
+        int adapter[2], ranks[2];
+        bool mine[2];  // whether the wave has tokens of it
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            adapter[q] = first + q < slots ? __builtin_amdgcn_readfirstlane(present.slot[first + q]) : -1;
+            ranks[q] = adapter[q] >= 0 ? std::min(rank_of(c.w, adapter[q]) - r0, R) : 0;
+            mine[q] = ranks[q] > 0 && __any(own == adapter[q]);
+        }
+        if (ranks[0] <= 0 && ranks[1] <= 0) continue;
+        if (first)
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) x_of(from + u * kChunk, xs[u]);
+        Vec<TW, V> ws[2][kLoads];
+        auto w_of = [&](int k) {  // past the rank and past the end of the axis: 0
+            unsigned thread = threadIdx.x;
+            asm volatile("" : "+v"(thread));  // as in here()
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (ranks[q] <= 0) continue;
+                const TW* w = static_cast<const TW*>(c.w.w) + adapter[q] * c.w.stride + (kAlong ? r0 * c.w.ld + k : k * c.w.ld + r0);
+                const bool whole = k + kChunk <= to && ranks[q] == R && R * kChunk / V % kRowsBlock == 0;
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l) {
+                    const int n = l * kRowsBlock + thread;
+                    const int r = kAlong ? n / (kChunk / V) : n % (R / V) * V, e = kAlong ? n % (kChunk / V) * V : n / (R / V);
+                    const TW* p = at(w, (uint32_t)(kAlong ? r * c.w.ld + e : e * c.w.ld + r) * sizeof(TW));
+                    if (whole) {
+                        ws[q][l] = load<TW, V>(p);
+                    } else {
+                        int left = kAlong ? (r < ranks[q] ? to - k - e : 0) : (k + e < to && n < R * kChunk / V ? ranks[q] - r : 0);
+                        asm volatile("" : "+v"(left));
+                        ws[q][l] = load_own<TW, V>(p, left);
+                    }
+                }
+            }
+        };
+        auto w_put = [&](int turn) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (ranks[q] <= 0) continue;
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l) {
+                    const int n = l * kRowsBlock + threadIdx.x;
+                    if (n >= R * kChunk / V) continue;
+                    if constexpr (kAlong) {
+                        *reinterpret_cast<Vec<TW, V>*>(&staged[turn][q][n / (kChunk / V)][n % (kChunk / V) * V]) = ws[q][l];
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < V; ++m) staged[turn][q][n % (R / V) * V + m][n / (R / V)] = ws[q][l][m];
+                    }
+                }
+            }
+        };
+        F4 acc[2][kRanks];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int r = 0; r < kRanks; ++r) acc[q][r] = 0.f;
+        w_of(from);
+        w_put(0);
+        int turn = 0;
+        for (int k = from; k < to; k += kAhead * kChunk) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (k + u * kChunk >= to) break;
+                const bool more = k + (u + 1) * kChunk < to;
+                if (more) w_of(k + (u + 1) * kChunk);
+                __syncthreads();  // this turn's weights are there, and nobody reads the other's any more
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    if (!mine[q]) continue;
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                        for (int r = 0; r < kRanks; ++r) {
+                            const Vec<TW, 8> w = *reinterpret_cast<const Vec<TW, 8>*>(&staged[turn][q][16 * r + i][set * (kChunk / 2) + 32 * h + 8 * g]);
+                            if constexpr (k16) {
+                                acc[q][r] = product(w, xs[u][h], acc[q][r]);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) acc[q][r] = product((float)w[e], xs[u][h][e], acc[q][r]);
+                            }
+                        }
+                }
+                x_of(k + (u + kAhead) * kChunk, xs[u]);
+                if (more) w_put(turn ^ 1);
+                turn ^= 1;
+            }
+        }
+        // the second set's sums to the first one's, where the weights were
+        F4(*sums)[2 * kRanks][64] = reinterpret_cast<F4(*)[2 * kRanks][64]>(&staged[0][0][0][0]);
+        static_assert(sizeof(staged) >= 4 * sizeof(*sums), "");
+        __syncthreads();
+        if (set)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < kRanks; ++r) sums[wave][q * kRanks + r][lane] = acc[q][r];
+        __syncthreads();
+        if (!set)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < kRanks; ++r) acc[q][r] += sums[wave][q * kRanks + r][lane];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (set || !mine[q] || own != adapter[q]) continue;
+            const float scale = c.scale ? scale_of(c.w, adapter[q]) : 1.f;
+#pragma unroll
+            for (int r = 0; r < kRanks; ++r) {
+                F4 v = acc[q][r] * scale;
+                const int at_r = 16 * r + 4 * g;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at_r + e >= ranks[q]) v[e] = 0.f;
+                store_some<float, 4>(out + (16 * wave + i) * c.w.rank + r0 + at_r, v, c.w.rank - r0 - at_r);
+            }
+        }
+    }
+    // tokens without an adapter, or without ranks here
+    const bool nothing = own < 0 || rank_of(c.w, own) <= r0;
+    if (!set && 16 * wave + i < tokens_left && nothing)
+#pragma unroll
+        for (int r = 0; r < kRanks; ++r) store_some<float, 4>(out + (16 * wave + i) * c.w.rank + r0 + 16 * r + 4 * g, F4(0.f), c.w.rank - r0 - 16 * r - 4 * g);
 }
 
 // The parts of `shrink` added up in their order, times s_a (scale) -- where more than one kernel wants the sum.
@@ -476,23 +663,55 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
         return;
     }
     uint16_t* planes = reinterpret_cast<uint16_t*>(room);  // [piece][token][pitch]: hidden, 0 past the rank and for tokens without an adapter
-    const int64_t t0 = (int64_t)(blockIdx.x % tiles) * kTile;
-    const int group = blockIdx.x / tiles;
+    const unsigned item = by_xcd(blockIdx.x, inner);
+    const int64_t t0 = (int64_t)(item / c.groups) * kTile;
+    const int group = item % c.groups;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int rank32 = (c.w.rank + 31) / 32 * 32, pitch = rank32 + 8;
+    const TX* base = static_cast<const TX*>(c.base);
+    TX* y = static_cast<TX*>(c.y);
+    const int first = group * c.blocks, last = std::min(first + (int)c.blocks, blocks);
+    // a lane's place: the rest of an address is the wave's
+    const uint32_t base_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldbase + 4 * i) * sizeof(TX), y_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldy + 4 * i) * sizeof(TX);
+    const uint32_t w_lane = (uint32_t)(kAlong ? 4 * i : 4 * i * c.w.ld) * sizeof(TW);
+    // A quarter of base, 64 x 64.  rows: [e], elements 4 i .. + 3 of token 16 u + 4 g + e; columns: [e], tokens 4 i .. + 3 of element
+    // 16 g + 4 e + u.  Sixteen neighbouring lanes have neighbouring memory: a load of one line for each of them would
+    // take the address unit sixteen times as long.
+    auto get = [&](int block, int u, Vec<TX, 4> (&r)[4]) {
+        const int64_t o0 = (int64_t)block * 64;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (TX)0.f;
+        const uint32_t from = here(base_lane);
+        if (base)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = load<TX, 4>(at(kColumns ? base + (o0 + 4 * e + u) * c.ldbase + t0 : base + (t0 + 16 * u + e) * c.ldbase + o0, from));
+    };
+    // What does not depend on the tokens' adapters is requested before they are known: the first quarter of base, and hidden's parts, four threads
+    // for a token, four ranks at a time.
+    Vec<TX, 4> raw[2][4];  // this quarter's and the next one's
+    if (first + wave < last) get(first + wave, 0, raw[0]);
+    const int t = threadIdx.x >> 2, r_first = (threadIdx.x & 3) * 4;
+    auto sum_of = [&](int r) {
+        F4 sum = 0.f;
+        const float* p = c.part + (t0 + t) * c.w.rank + r;
+        if (r < c.w.rank)  // in eights
+#pragma unroll 4
+            for (uint32_t k = 0; k < c.parts; ++k) sum += load<float, 4>(p + k * c.tokens * c.w.rank);
+        return sum;
+    };
+    F4 early[2 * kHeld];
+    if constexpr (kChunks)
+#pragma unroll
+        for (int r = 0; r < 2 * kHeld; ++r) early[r] = sum_of(r_first + 16 * r);
     list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
     const int slots = __builtin_amdgcn_readfirstlane(present.slots), jobs = slots + (__builtin_amdgcn_readfirstlane(present.none) && c.base != c.y ? 1 : 0);
     if (jobs == 0 && !c.hidden) return;
-    {  // four threads for a token, four ranks at a time
-        const int t = threadIdx.x >> 2, a = present.adapter[t];
-        const int rank = a >= 0 ? rank_of(c.w, a) : 0;
-        const float scale = a >= 0 && c.scale ? scale_of(c.w, a) : 1.f;
-        for (int r = (threadIdx.x & 3) * 4; r < rank32; r += 16) {
-            F4 sum = 0.f;
-            const float* p = c.part + (t0 + t) * c.w.rank + r;
-#pragma unroll 4
-            for (uint32_t k = 0; k < c.parts; ++k) sum += load_some<float, 4>(p + k * c.tokens * c.w.rank, rank - r);
-            if (c.hidden && group == 0) store_some<float, 4>(c.hidden + (t0 + t) * c.w.rank + r, sum, c.w.rank - r);
+    {
+        const int a = present.adapter[t];
+        const float scale = a < 0 ? 0.f : c.scale ? scale_of(c.w, a) : 1.f;
+        auto put = [&](int r, F4 sum) {  // `shrink` has left 0 for tokens without an adapter and past an adapter's rank
+            if (c.hidden && group == 0 && r < c.w.rank) store<float, 4>(c.hidden + (t0 + t) * c.w.rank + r, sum);
             sum *= scale;
             uint16_t h[4][kH];
 #pragma unroll
@@ -502,29 +721,18 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
                 const Vec<uint16_t, 4> v = {h[0][k], h[1][k], h[2][k], h[3][k]};
                 *reinterpret_cast<Vec<uint16_t, 4>*>(&planes[(k * kTile + t) * pitch + r]) = v;
             }
+        };
+        if constexpr (kChunks) {
+#pragma unroll
+            for (int r = 0; r < 2 * kHeld; ++r)
+                if (r_first + 16 * r < rank32) put(r_first + 16 * r, early[r]);
+        } else {
+            for (int r = r_first; r < rank32; r += 16) put(r, sum_of(r));
         }
     }
     __syncthreads();
-    const TX* base = static_cast<const TX*>(c.base);
-    TX* y = static_cast<TX*>(c.y);
-    const int first = group * c.blocks, last = std::min(first + (int)c.blocks, blocks);
-    // a lane's place: the rest of an address is the wave's
-    const uint32_t base_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldbase + 4 * i) * sizeof(TX), y_lane = (uint32_t)((kColumns ? 16 : 4) * g * c.ldy + 4 * i) * sizeof(TX);
-    const uint32_t w_lane = (uint32_t)(kAlong ? 4 * i : 4 * i * c.w.ld) * sizeof(TW);
     for (int block = first + wave; block < last; block += kWaves) {
         const int64_t o0 = (int64_t)block * 64;
-        // A quarter of base, 64 x 64.  rows: [e], elements 4 i .. + 3 of token 16 u + 4 g + e; columns: [e], tokens 4 i .. + 3 of element
-        // 16 g + 4 e + u.  Sixteen neighbouring lanes have neighbouring memory: a load of one line for each of them would
-        // take the address unit sixteen times as long.
-        auto get = [&](int u, Vec<TX, 4> (&r)[4]) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = (TX)0.f;
-            const uint32_t from = here(base_lane);
-            if (base)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    r[e] = load<TX, 4>(at(kColumns ? base + (o0 + 4 * e + u) * c.ldbase + t0 : base + (t0 + 16 * u + e) * c.ldbase + o0, from));
-        };
         for (int q = 0; q < jobs; ++q) {
             const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
             const int rank = a >= 0 ? rank_of(c.w, a) : 0;
@@ -555,8 +763,6 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
                 }
             };
             auto operand = [&](int k, int t, int r0) { return *reinterpret_cast<const Pieces8*>(&planes[(k * kTile + t) * pitch + r0 + 8 * g]); };
-            Vec<TX, 4> raw[2][4];  // this quarter's and the next one's
-            get(0, raw[0]);
             Pieces8 held[kHeld][4][kW];
             if constexpr (kChunks)
                 if (rank > 0)
@@ -564,7 +770,9 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
                     for (int r = 0; r < kChunks; ++r) weights(32 * r, held[r]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {  // rows: tokens 16 u .. + 15, four tiles of elements; columns: elements 4 (0 .. 15) + u, four tiles of tokens
-                if (u < 3) get(u + 1, raw[(u + 1) % 2]);
+                if (u < 3) get(block, u + 1, raw[(u + 1) % 2]);
+                else if (q + 1 < jobs) get(block, 0, raw[0]);
+                else if (block + kWaves < last) get(block + kWaves, 0, raw[0]);
                 // the adapters of the lane's tokens (rows: 16 u + 4 g + e; columns: 4 i + e)
                 const Vec<int, 4> of = *reinterpret_cast<const Vec<int, 4>*>(&present.adapter[kColumns ? 4 * i : 16 * u + 4 * g]);
                 if (!__any(of[0] == a || of[1] == a || of[2] == a || of[3] == a)) continue;
@@ -916,42 +1124,38 @@ struct ShrinkShape {
     int64_t part;
     ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns) {
         ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
-        tiles = tokens <= kFewTokens ? 1 : ranks < 8 ? 4 : columns ? 1 : 2;
+        tiles = tokens <= kFewTokens || (columns && ranks == 8) ? 1 : 4;
         const int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (length + 255) / 256, 32}));
-        part = ((length + want - 1) / want + 31) / 32 * 32;
+        part = ((length + want - 1) / want + 63) / 64 * 64;
         parts = (int)((length + part - 1) / part);
     }
 };
 
-template <class TX, class TW, bool kColumns, bool kAlong, int kTiles>
-int shrink_ranks(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
-    const dim3 grid((unsigned)((c.tokens + 16 * kTiles - 1) / (16 * kTiles)), f.parts, (unsigned)((c.w.rank + 16 * f.ranks - 1) / (16 * f.ranks)));
-    if constexpr (kTiles != 2) {
-        if (f.ranks == 1) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 1><<<grid, kShrinkBlock, 0, s>>>(c);
-        else if (f.ranks == 2) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 2><<<grid, kShrinkBlock, 0, s>>>(c);
-        else if (f.ranks == 4) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 4><<<grid, kShrinkBlock, 0, s>>>(c);
-    }
-    if constexpr (kTiles != 4)
-        if (f.ranks == 8) shrink_kernel<TX, TW, kColumns, kAlong, kTiles, 8><<<grid, kShrinkBlock, 0, s>>>(c);
-    return (int)hipGetLastError();
+template <class TX, class TW, bool kColumns, bool kAlong, int kRanks>
+void shrink_tiles(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
+    const dim3 grid((unsigned)((c.tokens + 16 * f.tiles - 1) / (16 * f.tiles) * f.parts), 1, (unsigned)((c.w.rank + 16 * kRanks - 1) / (16 * kRanks)));
+    if (f.tiles == 1) shrink_kernel<TX, TW, kColumns, kAlong, 1, kRanks><<<grid, kShrinkBlock, 0, s>>>(c);
+    else if constexpr (!kColumns) shrink_rows_kernel<TX, TW, kAlong, kRanks><<<grid, kRowsBlock, 0, s>>>(c);
+    else if constexpr (kRanks < 8) shrink_kernel<TX, TW, kColumns, kAlong, 4, kRanks><<<grid, kShrinkBlock, 0, s>>>(c);
 }
 template <class TX, class TW, bool kColumns, bool kAlong>
-int shrink_tiles(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
-    if (f.tiles == 1) return shrink_ranks<TX, TW, kColumns, kAlong, 1>(c, f, s);
-    if constexpr (!kColumns)
-        if (f.tiles == 2) return shrink_ranks<TX, TW, kColumns, kAlong, 2>(c, f, s);
-    return shrink_ranks<TX, TW, kColumns, kAlong, 4>(c, f, s);
+int shrink_ranks(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
+    if (f.ranks == 1) shrink_tiles<TX, TW, kColumns, kAlong, 1>(c, f, s);
+    else if (f.ranks == 2) shrink_tiles<TX, TW, kColumns, kAlong, 2>(c, f, s);
+    else if (f.ranks == 4) shrink_tiles<TX, TW, kColumns, kAlong, 4>(c, f, s);
+    else shrink_tiles<TX, TW, kColumns, kAlong, 8>(c, f, s);
+    return (int)hipGetLastError();
 }
 template <bool kAlong>
 int shrink(ShrinkArgs c, const ShrinkShape& f, const cer_tokens_t& x, int32_t weights, hipStream_t s) {
-    c.x = x.data, c.ldx = x.ld, c.part = f.part;
-    if (x.type == CER_TYPE_BF16) return shrink_tiles<__bf16, __bf16, false, kAlong>(c, f, s);
-    if (x.type == CER_TYPE_F16) return shrink_tiles<_Float16, _Float16, false, kAlong>(c, f, s);
+    c.x = x.data, c.ldx = x.ld, c.part = f.part, c.parts = (uint32_t)f.parts;
+    if (x.type == CER_TYPE_BF16) return shrink_ranks<__bf16, __bf16, false, kAlong>(c, f, s);
+    if (x.type == CER_TYPE_F16) return shrink_ranks<_Float16, _Float16, false, kAlong>(c, f, s);
     const bool columns = x.order == CER_ORDER_COLUMNS;
-    if (weights == CER_TYPE_BF16) return columns ? shrink_tiles<float, __bf16, true, kAlong>(c, f, s) : shrink_tiles<float, __bf16, false, kAlong>(c, f, s);
-    if (weights == CER_TYPE_F16) return columns ? shrink_tiles<float, _Float16, true, kAlong>(c, f, s) : shrink_tiles<float, _Float16, false, kAlong>(c, f, s);
-    return columns ? shrink_tiles<float, float, true, kAlong>(c, f, s) : shrink_tiles<float, float, false, kAlong>(c, f, s);
+    if (weights == CER_TYPE_BF16) return columns ? shrink_ranks<float, __bf16, true, kAlong>(c, f, s) : shrink_ranks<float, __bf16, false, kAlong>(c, f, s);
+    if (weights == CER_TYPE_F16) return columns ? shrink_ranks<float, _Float16, true, kAlong>(c, f, s) : shrink_ranks<float, _Float16, false, kAlong>(c, f, s);
+    return columns ? shrink_ranks<float, float, true, kAlong>(c, f, s) : shrink_ranks<float, float, false, kAlong>(c, f, s);
 }
 
 template <class TX, class TW, bool kColumns, bool kAlong>

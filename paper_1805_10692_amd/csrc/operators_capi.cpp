@@ -9,7 +9,7 @@
 namespace {
 using namespace cer;
 
-constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 24;
+constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 22;
 
 int bytes_of(int type) { return type == CER_TYPE_F32 ? 4 : type == CER_TYPE_F8 ? 1 : 2; }
 bool number_type(int type) { return type == CER_TYPE_F32 || type == CER_TYPE_BF16 || type == CER_TYPE_F16; }
