@@ -29,7 +29,9 @@ namespace {
 
 using F4 = Vec<float, 4>;
 constexpr int kBlock = 256, kWaves = kBlock / 64;
-constexpr int kShrinkBlock = 512, kOuterBlock = 256, kRowsBlock = 512;
+template <int kTiles>
+constexpr int kShrinkThreads = kTiles == 1 ? 1024 : 512;
+constexpr int kFewBlock = 1024, kOuterBlock = 256, kRowsBlock = 512;
 constexpr int kMostTile = 64;  // tokens of a workgroup
 constexpr int64_t kFewTokens = 256;
 
@@ -88,16 +90,6 @@ __device__ __forceinline__ F4 product(float a, float b, F4 c) { return __builtin
 __device__ __forceinline__ F4 product(Vec<__bf16, 8> a, Vec<__bf16, 8> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ F4 product(Vec<_Float16, 8> a, Vec<_Float16, 8> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// Up to N elements in their own type, 0 past `left`.
-template <class T, int N>
-__device__ __forceinline__ Vec<T, N> load_own(const T* p, int64_t left) {
-    if (left >= N) return load<T, N>(p);
-    Vec<T, N> v;
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = j < left ? p[j] : (T)0.f;
-    return v;
-}
-
 // Elements at a wave's own address (a scalar) and a lane's offset in bytes from it.
 template <class T>
 __device__ __forceinline__ const T* at(const T* base, uint32_t bytes) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
@@ -125,7 +117,7 @@ struct ShrinkArgs {
     int64_t tokens, length;  // of the long axis
     const void* x;
     int64_t ldx;
-    int64_t part;    // elements of the long axis for a workgroup, a multiple of 64
+    int64_t part;    // elements of the long axis for a workgroup, a multiple of 32 (few tokens) or 64
     uint32_t parts;  // of the long axis
     float* out;      // [parts][tokens][rank]
     bool scale;      // times s_a
@@ -136,22 +128,24 @@ struct ShrinkArgs {
 // that belong to g: one 16-bit instruction, or eight 32-bit ones that take one of every g's.  The sides agree on which, and that is all that
 // their order has to do.  Rows of ranks: 16 r + i, or where a rank's elements lie apart (!kAlong) kRanks i + r, neighbours in one load.
 template <class TX, class TW, bool kColumns, bool kAlong, int kTiles, int kRanks>
-__global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void shrink_kernel(ShrinkArgs c) {
+__global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 : 4) void shrink_kernel(ShrinkArgs c) {
     constexpr bool k16 = sizeof(TX) == 2;
-    constexpr int E = 8, kStep = 4 * E, kTile = 16 * kTiles, kPitch = 16 * kRanks + 4, kWaves = kShrinkBlock / 64;
+    constexpr int E = 8, kStep = 4 * E, kTile = 16 * kTiles, kPitch = 16 * kRanks + 4, kThreads = kShrinkThreads<kTiles>, kWaves = kThreads / 64;
     using Operand = std::conditional_t<k16, Vec<TX, E>, Vec<float, E>>;
     __shared__ Present present;
-    __shared__ float sums[kTile][kPitch];
+    __shared__ std::conditional_t<kTiles == 1, F4[kRanks][64], float[kPitch]> sums[kTiles == 1 ? kWaves / 2 : kTile];
     const unsigned item = by_xcd(blockIdx.x, gridDim.x), part = item % c.parts;
     const int64_t t0 = (int64_t)(item / c.parts) * kTile;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
     list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
     const int slots = __builtin_amdgcn_readfirstlane(present.slots);
-    const int abreast = kTiles > 1 ? 1 : slots >= 8 ? 8 : slots >= 4 ? 4 : slots >= 2 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
-    // the workgroup's part of the long axis; its waves take turns, so that together they read neighbouring lines
+    const int abreast = kTiles > 1 ? 1 : slots > 8 ? 16 : slots > 4 ? 8 : slots > 2 ? 4 : slots > 1 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
+    // the workgroup's part of the long axis; its waves take turns, so that together they read neighbouring lines, or, few tokens, a stretch each
     const int from = part * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
-    constexpr int kAhead = k16 && kTiles * kRanks <= 4 ? 4 : kTiles * kRanks <= (kTiles == 1 && !k16 ? 4 : 8) ? 2 : 1;  // steps whose loads are on their way together
+    constexpr int kAhead = kTiles * kRanks <= 2 ? 4 : kTiles * kRanks <= (kTiles == 1 && !k16 ? 4 : 8) ? 2 : 1;  // steps whose loads are on their way together
     constexpr int kRun = kAhead * kStep;
+    const int stretch = kTiles == 1 ? ((to - from + pieces - 1) / pieces + kStep - 1) / kStep * kStep : kRun;
+    const int k_first = from + piece * stretch, k_last = kTiles == 1 ? std::min(k_first + stretch, to) : to, k_next = kTiles == 1 ? kRun : pieces * kRun;
     int token[kTiles];  // in the tile
 #pragma unroll
     for (int s = 0; s < kTiles; ++s) token[s] = kColumns ? kTiles * i + s : 16 * s + i;
@@ -245,41 +239,72 @@ __global__ __launch_bounds__(kShrinkBlock, kTiles * kRanks >= 16 ? 2 : 4) void s
                         }
                     }
             };
-            int k = from + piece * kRun;
-            for (; k + kRun <= to; k += pieces * kRun)
+            int k = k_first;
+            for (; k + kRun <= k_last; k += k_next)
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) step(k + u * kStep, std::true_type());
-            if (k < to) {  // the last run, by the wave whose turn it is
-                const int end = std::min(k + kRun, to);
+            if (k < k_last) {  // the last run, by the wave whose turn it is
+                const int end = std::min(k + kRun, k_last);
                 if constexpr (kAhead > 1)
 #pragma unroll 1
                     for (; k + kStep <= end; k += kStep) step(k, std::true_type());
                 if (k < end) step(k, std::false_type());
             }
         }
-        // the pieces of an adapter are added up in turn; each token is one adapter's
-        for (int p = 0; p < pieces; ++p) {
-            if (p == piece && rank > r0)
+        if constexpr (kTiles == 1) {
+            // the pieces of an adapter: the upper half's sums to the lower half's, until there is one
+            for (int half = pieces / 2; half; half /= 2) {
+                if (piece >= half && piece < 2 * half)
 #pragma unroll
-                for (int s = 0; s < kTiles; ++s)
-                    if (present.adapter[token[s]] == a)
+                    for (int r = 0; r < kRanks; ++r) sums[wave - half * abreast][r][lane] = acc[0][r];
+                __syncthreads();
+                if (piece < half)
 #pragma unroll
-                        for (int r = 0; r < kRanks; ++r)
+                    for (int r = 0; r < kRanks; ++r) acc[0][r] += sums[wave][r][lane];
+                __syncthreads();
+            }
+            if (piece == 0 && rank > r0 && present.adapter[i] == a) {
+                float* to_token = c.out + (part * c.tokens + t0 + i) * c.w.rank + r0;
+                const float scale = c.scale ? scale_of(c.w, a) : 1.f;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float* at = &sums[token[s]][kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r];
-                                *at = p ? *at + acc[s][r][e] : acc[s][r][e];
-                            }
-            __syncthreads();
+                for (int r = 0; r < kRanks; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at_r = kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r;
+                        if (r0 + at_r < c.w.rank) to_token[at_r] = r0 + at_r < rank ? acc[0][r][e] * scale : 0.f;
+                    }
+            }
+        } else {
+            // in turn, in LDS; each token is one adapter's
+            for (int p = 0; p < pieces; ++p) {
+                if (p == piece && rank > r0)
+#pragma unroll
+                    for (int s = 0; s < kTiles; ++s)
+                        if (present.adapter[token[s]] == a)
+#pragma unroll
+                            for (int r = 0; r < kRanks; ++r)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    float* at = &sums[token[s]][kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r];
+                                    *at = p ? *at + acc[s][r][e] : acc[s][r][e];
+                                }
+                __syncthreads();
+            }
         }
     }
+    // few tokens: those without an adapter, or without ranks here; else all of them
     float* out = c.out + part * c.tokens * c.w.rank;
-    for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kShrinkBlock) {
+    for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kThreads) {
         const int t = e / (16 * kRanks), r = e % (16 * kRanks);
         if (t0 + t >= c.tokens || r0 + r >= c.w.rank) continue;
-        const int a = present.adapter[t];
-        float all = a >= 0 && r0 + r < rank_of(c.w, a) ? sums[t][r] : 0.f;
-        if (c.scale && a >= 0) all *= scale_of(c.w, a);
+        const int a = present.adapter[t], rank = a >= 0 ? rank_of(c.w, a) : 0;
+        float all = 0.f;
+        if constexpr (kTiles == 1) {
+            if (rank > r0) continue;
+        } else {
+            if (r0 + r < rank) all = sums[t][r];
+            if (c.scale && a >= 0) all *= scale_of(c.w, a);
+        }
         out[(t0 + t) * c.w.rank + r0 + r] = all;
     }
 }
@@ -489,61 +514,69 @@ struct ExpandArgs {
     uint32_t groups;    // of such blocks
 };
 
-// The 16 tokens from t0 on, `blocks` times 64 elements of the long axis from block `first` on; a wave takes pairs of adapter and 64 elements.
-// Element o0 + 4 i + j is row (column) i of the tile j of four: the operands' loads have four neighbours in a lane where the weights lie
-// that way, and so do the results: lane (i, g) holds o0 + 16 g .. + 15 of token i (rows), or elements o0 + 4 i + j of tokens
-// 4 g .. + 3 (columns).  `room`: LDS of 16 * (the rank's next multiple of 16, + 4) floats.
-template <class TX, class TW, bool kColumns, bool kAlong>
-__device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int first, int blocks, bool tell, Present& present, float* room) {
+// The 16 tokens from t0 on, 64 elements of the long axis from o0 on; the waves share out the adapters.  Element o0 + 4 i + j is row (column) i of
+// the tile j of four, so that a lane's loads have four neighbours where the weights lie that way, and sixteen neighbouring lanes have neighbouring
+// memory in base and y.  `room`: LDS of 16 * (the rank's next multiple of 16, + 4) floats.
+template <class TX, class TW, bool kColumns, bool kAlong, int kThreads>
+__device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int64_t o0, Present& present, float* room) {
+    constexpr int kSplit = kThreads / 256;  // threads for a token and rank: neighbours
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int rank16 = (c.w.rank + 15) / 16 * 16, pitch = rank16 + 4;
-    list_adapters(present, c.index, t0, 16, c.tokens, c.w.adapters);
-    {  // hidden, 0 past the rank and for tokens without an adapter
-        const int t = threadIdx.x >> 4, a = present.adapter[t];
-        const int rank = a >= 0 ? rank_of(c.w, a) : 0;
-        const float scale = a >= 0 && c.scale ? scale_of(c.w, a) : 1.f;
-        for (int r = threadIdx.x & 15; r < rank16; r += 16) {
-            float sum = 0.f;
-            if (t0 + t < c.tokens && r < c.w.rank) {
-                const float* p = c.part + (t0 + t) * c.w.rank + r;
-                if (r < rank)
-#pragma unroll 8
-                    for (uint32_t k = 0; k < c.parts; ++k) sum += p[k * c.tokens * c.w.rank];
-                if (c.hidden && tell) c.hidden[(t0 + t) * c.w.rank + r] = sum;
+    const int left = (int)std::min<int64_t>(c.length - o0, 64), tokens_left = (int)std::min<int64_t>(c.tokens - t0, 16);
+    const TX* base = static_cast<const TX*>(c.base);
+    TX* y = static_cast<TX*>(c.y);
+    // What does not depend on the tokens' adapters is requested before they are known: base and hidden's parts.
+    // rows: acc[j][e], element o0 + 4 i + j of token 4 g + e; columns: element o0 + 16 g + 4 e + j of token i
+    F4 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = 0.f;
+    if (base) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (kColumns) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * g + 4 * e + j < left && i < tokens_left) acc[j][e] = (float)base[(o0 + 16 * g + 4 * e + j) * c.ldbase + t0 + i];
+            } else if (4 * g + e < tokens_left) {
+                const F4 v = load_some<TX, 4>(base + (t0 + 4 * g + e) * c.ldbase + o0 + 4 * i, left - 4 * i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j][e] = v[j];
             }
-            room[t * pitch + r] = sum * scale;
+        }
+    }
+    const int t_own = threadIdx.x / (16 * kSplit), split = threadIdx.x % kSplit;
+    auto sum_of = [&](int r) {
+        float sum = 0.f;
+        if (t_own < tokens_left && r < c.w.rank) {
+            const float* p = c.part + (t0 + t_own) * c.w.rank + r;
+#pragma unroll 8
+            for (uint32_t k = split; k < c.parts; k += kSplit) sum += p[k * c.tokens * c.w.rank];
+        }
+#pragma unroll
+        for (int k = 1; k < kSplit; k *= 2) sum += __shfl_xor(sum, k);
+        return sum;
+    };
+    const int r_own = threadIdx.x / kSplit % 16;
+    const float early = sum_of(r_own);
+    list_adapters(present, c.index, t0, 16, c.tokens, c.w.adapters);
+    {  // 0 past the rank and for tokens without an adapter
+        const int a = present.adapter[t_own];
+        const float scale = a < 0 ? 0.f : c.scale ? scale_of(c.w, a) : 1.f;
+        for (int r = r_own; r < rank16; r += 16) {
+            const float sum = r < 16 ? early : sum_of(r);
+            if (split) continue;
+            if (c.hidden && o0 == 0 && t_own < tokens_left && r < c.w.rank) c.hidden[(t0 + t_own) * c.w.rank + r] = sum;
+            room[t_own * pitch + r] = sum * scale;
         }
     }
     __syncthreads();
-    const TX* base = static_cast<const TX*>(c.base);
-    TX* y = static_cast<TX*>(c.y);
     // tokens without an adapter: a list entry of their own, unless y has what they get already
     const int slots = __builtin_amdgcn_readfirstlane(present.slots), jobs = slots + (__builtin_amdgcn_readfirstlane(present.none) && c.base != c.y ? 1 : 0);
-    for (int job = wave; job < jobs * blocks; job += kWaves) {
-        const int64_t o0 = (int64_t)(first + job / jobs) * 64;
-        if (o0 >= c.length) break;
-        const int a = job % jobs < slots ? __builtin_amdgcn_readfirstlane(present.slot[job % jobs]) : -1;
-        const int left = (int)std::min<int64_t>(c.length - o0, 64);
-        F4 acc[4];  // rows: [j], elements 16 g + 4 (0 .. 3) + j; columns: [j], tokens 4 g + (0 .. 3)
-        constexpr int V = 16 / sizeof(TX);
-        const int64_t t = t0 + (kColumns ? 4 * g : i);
-        const bool mine = t0 + i < c.tokens && present.adapter[i] == a;
-        if constexpr (kColumns) {
+    for (int job = wave; job < jobs; job += kThreads / 64) {
+        const int a = job < slots ? __builtin_amdgcn_readfirstlane(present.slot[job]) : -1;
+        F4 sum[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[j] = base && 4 * i + j < left && t < c.tokens ? load_some<TX, 4>(base + (o0 + 4 * i + j) * c.ldbase + t, c.tokens - t) : F4(0.f);
-        } else {
-            Vec<float, 16> v;
-#pragma unroll
-            for (int q = 0; q < 16 / V; ++q) {
-                Vec<float, V> u = 0.f;
-                if (base && mine) u = load_some<TX, V>(base + t * c.ldbase + o0 + 16 * g + V * q, left - 16 * g - V * q);
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[V * q + k] = u[k];
-            }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) acc[k % 4][k / 4] = v[k];
-        }
+        for (int j = 0; j < 4; ++j) sum[j] = acc[j];
         const int rank = a >= 0 ? rank_of(c.w, a) : 0;
         const TW* w = static_cast<const TW*>(c.w.w) + (a >= 0 ? a * c.w.stride : 0);
         for (int r0 = 0; r0 < rank; r0 += 16) {
@@ -563,46 +596,29 @@ __device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int
             }
             const F4 h = *reinterpret_cast<const F4*>(&room[i * pitch + from]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[j] = kColumns ? product(h[q], ws[j][q], acc[j]) : product(ws[j][q], h[q], acc[j]);
+                for (int j = 0; j < 4; ++j) sum[j] = kColumns ? product(ws[j][q], h[q], sum[j]) : product(h[q], ws[j][q], sum[j]);
         }
-        if constexpr (kColumns) {
-            bool own[4], all = true;
+        const bool mine = i < tokens_left && present.adapter[i] == a;  // columns
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                own[k] = t + k < c.tokens && present.adapter[4 * g + k] == a;
-                all &= own[k];
-            }
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (kColumns) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (4 * i + j >= left) continue;
-                TX* p = y + (o0 + 4 * i + j) * c.ldy + t;
-                if (all) {
-                    store_f32<TX, 4>(p, acc[j]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (own[k]) p[k] = (TX)acc[j][k];
-                }
-            }
-        } else if (mine) {
-#pragma unroll
-            for (int q = 0; q < 16 / V; ++q) {
-                Vec<float, V> u;
-#pragma unroll
-                for (int k = 0; k < V; ++k) u[k] = acc[(V * q + k) % 4][(V * q + k) / 4];
-                store_some<TX, V>(y + t * c.ldy + o0 + 16 * g + V * q, u, left - 16 * g - V * q);
+                for (int j = 0; j < 4; ++j)
+                    if (mine && 16 * g + 4 * e + j < left) y[(o0 + 16 * g + 4 * e + j) * c.ldy + t0 + i] = (TX)sum[j][e];
+            } else if (4 * g + e < tokens_left && present.adapter[4 * g + e] == a) {
+                store_some<TX, 4>(y + (t0 + 4 * g + e) * c.ldy + o0 + 4 * i, F4{sum[0][e], sum[1][e], sum[2][e], sum[3][e]}, left - 4 * i);
             }
         }
     }
 }
 
 template <class TX, class TW, bool kColumns, bool kAlong>
-__global__ __launch_bounds__(kBlock) void expand_kernel(ExpandArgs c) {
+__global__ __launch_bounds__(kFewBlock) void expand_kernel(ExpandArgs c) {
     extern __shared__ float room[];
     __shared__ Present present;
-    expand_some<TX, TW, kColumns, kAlong>(c, (int64_t)blockIdx.x * 16, blockIdx.y * c.blocks, c.blocks, blockIdx.y == 0, present, room);
+    expand_some<TX, TW, kColumns, kAlong, kFewBlock>(c, (int64_t)blockIdx.x * 16, (int64_t)blockIdx.y * 64, present, room);
 }
 
 // ---- expand, many tokens --------------------------------------------------------------------------------------------------------
@@ -657,9 +673,9 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
     const int tiles = (int)(c.tokens / 64), blocks = (int)(c.length / 64), all_blocks = (int)((c.length + 63) / 64);
     const unsigned inner = tiles * c.groups;
     if (blockIdx.x >= inner) {
-        const int n = blockIdx.x - inner, behind = (int)((c.tokens - 64 * (int64_t)tiles + 15) / 16), each = (all_blocks + 3) / 4;
-        if (n < behind * each) expand_some<TX, TW, kColumns, kAlong>(c, 64 * (int64_t)tiles + n / each * 16, n % each * 4, std::min(4, all_blocks - n % each * 4), n % each == 0, present, room);
-        else expand_some<TX, TW, kColumns, kAlong>(c, (int64_t)(n - behind * each) * 16, blocks, 1, false, present, room);
+        const int n = blockIdx.x - inner, behind = (int)((c.tokens - 64 * (int64_t)tiles + 15) / 16) * all_blocks;
+        if (n < behind) expand_some<TX, TW, kColumns, kAlong, kBlock>(c, 64 * (int64_t)tiles + n / all_blocks * 16, n % all_blocks * (int64_t)64, present, room);
+        else expand_some<TX, TW, kColumns, kAlong, kBlock>(c, (int64_t)(n - behind) * 16, (int64_t)blocks * 64, present, room);
         return;
     }
     uint16_t* planes = reinterpret_cast<uint16_t*>(room);  // [piece][token][pitch]: hidden, 0 past the rank and for tokens without an adapter
@@ -1122,12 +1138,17 @@ __global__ __launch_bounds__(kBlock) void outer_sum_kernel(const float* part, ui
 struct ShrinkShape {
     int tiles, ranks, parts;
     int64_t part;
-    ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns) {
+    ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns, int64_t adapters) {
         ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
         tiles = tokens <= kFewTokens || (columns && ranks == 8) ? 1 : 4;
         const int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (length + 255) / 256, 32}));
-        part = ((length + want - 1) / want + 63) / 64 * 64;
+        // few tokens: a workgroup for a compute unit, and no stretch of the long axis of less than 128 elements, or less than 32 for a wave where the
+        // sixteen waves have up to so many adapters abreast
+        const int64_t abreast = std::min<int64_t>({16, tokens, adapters});
+        const int64_t want = tokens <= kFewTokens ? std::min<int64_t>(256 / blocks, length / std::max<int64_t>(128, 512 / abreast))
+                                                  : std::min<int64_t>(512 / blocks, (length + 255) / 256);
+        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(want, 64)), step = tokens <= kFewTokens ? 32 : 64;
+        part = ((length + cut - 1) / cut + step - 1) / step * step;
         parts = (int)((length + part - 1) / part);
     }
 };
@@ -1135,9 +1156,9 @@ struct ShrinkShape {
 template <class TX, class TW, bool kColumns, bool kAlong, int kRanks>
 void shrink_tiles(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
     const dim3 grid((unsigned)((c.tokens + 16 * f.tiles - 1) / (16 * f.tiles) * f.parts), 1, (unsigned)((c.w.rank + 16 * kRanks - 1) / (16 * kRanks)));
-    if (f.tiles == 1) shrink_kernel<TX, TW, kColumns, kAlong, 1, kRanks><<<grid, kShrinkBlock, 0, s>>>(c);
+    if (f.tiles == 1) shrink_kernel<TX, TW, kColumns, kAlong, 1, kRanks><<<grid, kShrinkThreads<1>, 0, s>>>(c);
     else if constexpr (!kColumns) shrink_rows_kernel<TX, TW, kAlong, kRanks><<<grid, kRowsBlock, 0, s>>>(c);
-    else if constexpr (kRanks < 8) shrink_kernel<TX, TW, kColumns, kAlong, 4, kRanks><<<grid, kShrinkBlock, 0, s>>>(c);
+    else if constexpr (kRanks < 8) shrink_kernel<TX, TW, kColumns, kAlong, 4, kRanks><<<grid, kShrinkThreads<4>, 0, s>>>(c);
 }
 template <class TX, class TW, bool kColumns, bool kAlong>
 int shrink_ranks(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
@@ -1165,15 +1186,14 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
     // ranks in eights: a load takes eight of a row and must not leave it
     if (c.tokens <= kFewTokens || c.length < 64 || c.w.rank % 8) {
         const int64_t across = (c.tokens + 15) / 16;
-        c.blocks = across * blocks >= 2048 ? 4 : 1;
-        const dim3 grid((unsigned)across, (unsigned)((blocks + c.blocks - 1) / c.blocks));
-        expand_kernel<TX, TW, kColumns, kAlong><<<grid, kBlock, few, s>>>(c);
+        const dim3 grid((unsigned)across, (unsigned)blocks);
+        expand_kernel<TX, TW, kColumns, kAlong><<<grid, kFewBlock, few, s>>>(c);
     } else {
         // the tokens' hidden is made ready once for a workgroup: as many blocks for each as leave about four workgroups for a compute unit
         const int64_t across = c.tokens / 64, most = std::max<int64_t>(1, 1024 / across), whole = c.length / 64;
         c.blocks = (uint32_t)std::max<int64_t>(kWaves, (whole + most - 1) / most);
         c.groups = (uint32_t)((whole + c.blocks - 1) / c.blocks);
-        const int64_t ends = (c.tokens % 64 + 15) / 16 * ((blocks + 3) / 4) + (c.length % 64 ? across * 4 : 0);
+        const int64_t ends = (c.tokens % 64 + 15) / 16 * blocks + (c.length % 64 ? across * 4 : 0);
         const size_t lds = std::max(few, (size_t)(sizeof(TX) == 4 ? 3 : 2) * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
         constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1;  // times 32 ranks, in registers
         const auto kernel = c.w.rank <= 32           ? expand_wide_kernel<TX, TW, kColumns, kAlong, 1>
@@ -1249,11 +1269,11 @@ Weights side_b(const cer_adapters_t& w) { return {w.B, w.stride_b, w.ld_b, w.ran
 }  // namespace
 
 int64_t adapter_workspace(int64_t tokens, int64_t rank, int64_t in, int64_t) {
-    return std::max(ShrinkShape(tokens, rank, in, false).parts, ShrinkShape(tokens, rank, in, true).parts) * tokens * rank * 4;
+    return std::max(ShrinkShape(tokens, rank, in, false, 16).parts, ShrinkShape(tokens, rank, in, true, 16).parts) * tokens * rank * 4;  // the most, whatever the adapters' number
 }
 
 int launch_adapters(const AdapterCall& c, hipStream_t s) {
-    const ShrinkShape f(c.tokens, c.w.rank, c.w.in, c.x.order == CER_ORDER_COLUMNS);
+    const ShrinkShape f(c.tokens, c.w.rank, c.w.in, c.x.order == CER_ORDER_COLUMNS, c.w.adapters);
     const int64_t bytes = adapter_workspace(c.tokens, c.w.rank, c.w.in, c.w.out);
     Temporary t(c.workspace ? 0 : (size_t)bytes, s);
     if (t.error) return t.error;
@@ -1273,7 +1293,7 @@ int launch_adapters_backward(const AdapterBackwardCall& c, hipStream_t s) {
             if (int e = clear(c.dA, c.w.adapters * c.w.rank * c.w.in, s)) return e;
         return c.dB ? clear(c.dB, c.w.adapters * c.w.rank * c.w.out, s) : 0;
     }
-    const ShrinkShape f(c.tokens, c.w.rank, c.w.out, c.dy.order == CER_ORDER_COLUMNS);
+    const ShrinkShape f(c.tokens, c.w.rank, c.w.out, c.dy.order == CER_ORDER_COLUMNS, c.w.adapters);
     const int64_t one = c.tokens * c.w.rank;
     const bool d_wanted = c.dx.data || c.dA, k16 = c.dy.type != CER_TYPE_F32;
     // d, the parts of it, and the planes of d and hidden

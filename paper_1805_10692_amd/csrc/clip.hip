@@ -16,7 +16,7 @@
 namespace cer {
 namespace {
 
-constexpr int kEntries = 120, kThreads = 256, kPartsPerLaunch = 1024;
+constexpr int kEntries = 120, kThreads = 256, kPartsPerLaunch = 2048;
 constexpr int64_t kChunk = 8192;
 
 struct ClipTable {  // within the 4 KiB of arguments that a launch may have
@@ -44,9 +44,18 @@ template <class T>
 __device__ __forceinline__ double chunk_squares(const T* g, int64_t left) {
     constexpr int V = 16 / sizeof(T);
     double sum = 0;
-#pragma unroll 8
-    for (int64_t e = threadIdx.x * V; e < kChunk; e += kThreads * V) {
-        if (e >= left) break;
+    constexpr int kSteps = kChunk / (kThreads * V);
+    if (left >= kChunk) {
+        Vec<float, V> v[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) v[s] = load_f32<T, V>(g + (s * kThreads + threadIdx.x) * V);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum = fma((double)v[s][j], (double)v[s][j], sum);
+        return sum;
+    }
+    for (int64_t e = threadIdx.x * V; e < left; e += kThreads * V) {
         const Vec<float, V> v = load_some<T, V>(g + e, left - e);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
@@ -79,17 +88,27 @@ __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipTable t, dou
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-template <class T>
+template <bool kOnce, class T>
 __device__ __forceinline__ void chunk_scale(const T* g, T* out, int64_t left, float c) {
     constexpr int V = 16 / sizeof(T);
-#pragma unroll 8
-    for (int64_t e = threadIdx.x * V; e < kChunk; e += kThreads * V) {
-        if (e >= left) break;
-        store_some<T, V>(out + e, load_some<T, V>(g + e, left - e) * c, left - e);
+    constexpr int kSteps = kChunk / (kThreads * V);
+    if (left >= kChunk) {
+        Vec<float, V> v[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) v[s] = load_f32<T, V>(g + (s * kThreads + threadIdx.x) * V);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            T* to = out + (s * kThreads + threadIdx.x) * V;
+            if constexpr (kOnce) store_f32_once<T, V>(to, v[s] * c);
+            else store_f32<T, V>(to, v[s] * c);
+        }
+        return;
     }
+    for (int64_t e = threadIdx.x * V; e < left; e += kThreads * V) store_some<T, V>(out + e, load_some<T, V>(g + e, left - e) * c, left - e);
 }
 
 // The norm from the parts, then (`scale`) the table's gradients times the factor.
+template <bool kOnce>
 __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, const double* part, uint32_t parts, float max_norm, float* norm, bool scale) {
     __shared__ double room[kThreads / 64];
     double sum = 0;
@@ -99,15 +118,16 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, const
     if (!scale) return;
     float c = max_norm / (all + 1e-6f);
     if (c > 1.f) c = 1.f;  // a NaN stays one
-    for (uint32_t k = blockIdx.x; k < t.chunks; k += gridDim.x) {
+    for (uint32_t j = blockIdx.x; j < t.chunks; j += gridDim.x) {
+        const uint32_t k = t.chunks - 1 - j;  // what was read last is in the caches still
         const uint32_t i = tensor_of(t, k);
         if (c == 1.f && t.at[i].grad == t.at[i].out) continue;
         const int64_t at = (int64_t)(k - t.at[i].first) * kChunk, left = t.at[i].numbers - at;
         const void* g = t.at[i].grad;
         void* out = t.at[i].out;
-        if (t.at[i].type == CER_TYPE_BF16) chunk_scale(static_cast<const __bf16*>(g) + at, static_cast<__bf16*>(out) + at, left, c);
-        else if (t.at[i].type == CER_TYPE_F16) chunk_scale(static_cast<const _Float16*>(g) + at, static_cast<_Float16*>(out) + at, left, c);
-        else chunk_scale(static_cast<const float*>(g) + at, static_cast<float*>(out) + at, left, c);
+        if (t.at[i].type == CER_TYPE_BF16) chunk_scale<kOnce>(static_cast<const __bf16*>(g) + at, static_cast<__bf16*>(out) + at, left, c);
+        else if (t.at[i].type == CER_TYPE_F16) chunk_scale<kOnce>(static_cast<const _Float16*>(g) + at, static_cast<_Float16*>(out) + at, left, c);
+        else chunk_scale<kOnce>(static_cast<const float*>(g) + at, static_cast<float*>(out) + at, left, c);
     }
 }
 
@@ -158,14 +178,19 @@ int launch_clip(const ClipCall& c, hipStream_t s) {
     if (!c.scale || !parts) {
         ClipTable none;
         none.count = none.chunks = 0;
-        clip_scale_kernel<<<1, kThreads, 0, s>>>(none, part, parts, 0.f, c.norm, false);
+        clip_scale_kernel<false><<<1, kThreads, 0, s>>>(none, part, parts, 0.f, c.norm, false);
         return (int)hipGetLastError();
     }
+    // Where gradients and outputs together are more than the memory-side cache of 256 MiB holds, none of the outputs is there when somebody wants them,
+    // and stores that do not stay in the caches leave them to the gradients: 48 M numbers in 32 bits 98 us, with ordinary stores 116.
+    int64_t bytes = 0;
+    for (int64_t i = 0; i < c.count; ++i) bytes += c.grads[i].numbers * (c.grads[i].type == CER_TYPE_F32 ? 4 : 2) * (c.grads[i].out == c.grads[i].grad ? 1 : 2);
+    const bool once = bytes > (int64_t)256 << 20;
     float* norm = c.norm;
     for (int64_t i = 0, done = 0; i < c.count;) {
         const ClipTable t = next_table(c, &i, &done);
         if (!t.count) continue;
-        clip_scale_kernel<<<std::min<uint32_t>(t.chunks, 2 * kPartsPerLaunch), kThreads, 0, s>>>(t, part, parts, c.max_norm, norm, true);
+        (once ? clip_scale_kernel<true> : clip_scale_kernel<false>)<<<std::min<uint32_t>(t.chunks, kPartsPerLaunch), kThreads, 0, s>>>(t, part, parts, c.max_norm, norm, true);
         if (int e = (int)hipGetLastError()) return e;
         norm = nullptr;  // written once
     }

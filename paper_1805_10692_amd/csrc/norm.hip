@@ -54,6 +54,15 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
                 h[c] += load_some<TX, V>(r + e, a.n - e);
             }
         }
+        // few registers: the weights are on their way while the squares are added up
+        constexpr bool kEarly = kChunks * V <= 16;
+        Vec<float, V> w[kEarly ? kChunks : 1];
+        if (kEarly && a.w && a.y)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
+                w[kEarly ? c : 0] = load_some_of<V>(a.w, a.w_type, e, a.n - e);
+            }
         float squares = 0.f;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
@@ -78,7 +87,7 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
         for (int c = 0; c < kChunks; ++c) {
             const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
             h[c] *= rstd;
-            if (a.w) h[c] *= load_some_of<V>(a.w, a.w_type, e, a.n - e);
+            if (a.w) h[c] *= kEarly ? w[kEarly ? c : 0] : load_some_of<V>(a.w, a.w_type, e, a.n - e);
         }
         if constexpr (k8) {
             float most = 0.f;
@@ -145,8 +154,9 @@ int norm_rows(const NormArgs& a, hipStream_t s) {
     if (vectors <= 1024) return norm_rows_chunks<TX, TY, 1>(a, s);
     if (vectors <= 2048) return norm_rows_chunks<TX, TY, 2>(a, s);
     if (vectors <= 4096) return norm_rows_chunks<TX, TY, 4>(a, s);
-    if (vectors <= 8192) return norm_rows_chunks<TX, TY, 8>(a, s);
-    return norm_rows_chunks<TX, TY, 16>(a, s);  // 32 bits, up to 65536 features
+    if constexpr (V == 4)
+        if (vectors > 8192) return norm_rows_chunks<TX, TY, 16>(a, s);  // up to 65536 features
+    return norm_rows_chunks<TX, TY, 8>(a, s);
 }
 
 // ---- columns --------------------------------------------------------------------------------------------------------------------
@@ -233,35 +243,57 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(NormArgs a, int6
 }
 
 // x and y in different orders: a tile of 64 tokens by 64 features through LDS.  `sum` is written here and not with the sums of squares:
-// it may lie where x or r does, and h is wanted in 32 bits both times.
+// it may lie where x or r does, and h is wanted in 32 bits both times.  All loads of a thread are on their way before the first store.
 template <class TX, class TY, bool kFromColumns>
 __global__ __launch_bounds__(256) void norm_turn_kernel(NormArgs a) {
-    __shared__ float tile[64][65], room[256], rstds[64];
+    constexpr int V = 16 / sizeof(TX), kAbreast = 64 / V, kLoads = 64 / (256 / kAbreast);  // threads for a line of the tile; lines for a thread
+    __shared__ float tile[64][69], room[256], rstds[64];  // [token][feature]; a pitch that is odd in both directions' banks of four
     const int64_t t0 = (int64_t)blockIdx.x * 64, i0 = (int64_t)blockIdx.y * 64;
-    const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int along = threadIdx.x % kAbreast * V, line0 = threadIdx.x / kAbreast;
     const TX *x = static_cast<const TX*>(a.x), *r = static_cast<const TX*>(a.r);
-    // tile[token][feature]
+    // lines: tokens, or (from columns) features
+    const int64_t first = kFromColumns ? i0 : t0, lines = (kFromColumns ? a.n : a.tokens) - first, left = (kFromColumns ? a.tokens - t0 : a.n - i0) - along;
+    Vec<float, V> h[kLoads];
 #pragma unroll
-    for (unsigned k = 0; k < 16; ++k) {
-        const unsigned other = wave * 16 + k;
-        const int64_t t = t0 + (kFromColumns ? lane : other), i = i0 + (kFromColumns ? other : lane);
-        float h = 0.f;
-        if (t < a.tokens && i < a.n) {
-            h = (float)x[kFromColumns ? i * a.ldx + t : t * a.ldx + i];
-            if (r) h += (float)r[kFromColumns ? i * a.ldr + t : t * a.ldr + i];
-            if (a.sum) static_cast<TX*>(a.sum)[kFromColumns ? i * a.ldsum + t : t * a.ldsum + i] = (TX)h;
-        }
-        tile[kFromColumns ? lane : other][kFromColumns ? other : lane] = h;
+    for (int k = 0; k < kLoads; ++k) {
+        const int line = line0 + k * (256 / kAbreast);
+        h[k] = line < lines ? load_some<TX, V>(x + (first + line) * a.ldx + (kFromColumns ? t0 : i0) + along, left) : Vec<float, V>(0.f);
     }
-    norm_of_tokens(a, t0, 64, room, rstds, blockIdx.y == 0);
-    TY* y = static_cast<TY*>(a.y);
+    if (r)
 #pragma unroll
-    for (unsigned k = 0; k < 16; ++k) {
-        const unsigned other = wave * 16 + k, token = kFromColumns ? other : lane, feature = kFromColumns ? lane : other;
-        const int64_t t = t0 + token, i = i0 + feature;
-        if (t >= a.tokens || i >= a.n) continue;
-        const float w = a.w ? load_some_of<1>(a.w, a.w_type, i, 1)[0] : 1.f;
-        y[kFromColumns ? t * a.ldy + i : i * a.ldy + t] = (TY)(tile[token][feature] * rstds[token] * w);
+        for (int k = 0; k < kLoads; ++k) {
+            const int line = line0 + k * (256 / kAbreast);
+            if (line < lines) h[k] += load_some<TX, V>(r + (first + line) * a.ldr + (kFromColumns ? t0 : i0) + along, left);
+        }
+    norm_of_tokens(a, t0, 64, room, rstds, blockIdx.y == 0);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        const int line = line0 + k * (256 / kAbreast);
+        if (a.sum && line < lines) store_some<TX, V>(static_cast<TX*>(a.sum) + (first + line) * a.ldsum + (kFromColumns ? t0 : i0) + along, h[k], left);
+#pragma unroll
+        for (int j = 0; j < V; ++j) tile[kFromColumns ? along + j : line][kFromColumns ? line : along + j] = h[k][j];
+    }
+    __syncthreads();
+    TY* y = static_cast<TY*>(a.y);
+    // y's lines: the other way round, four numbers for a thread
+    const int out_along = threadIdx.x % 16 * 4;
+    const int64_t out_left = (kFromColumns ? a.n - i0 : a.tokens - t0) - out_along;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int line = threadIdx.x / 16 + 16 * k;
+        if (line >= (kFromColumns ? a.tokens - t0 : a.n - i0)) continue;
+        Vec<float, 4> v;
+        if constexpr (kFromColumns) {  // a token's features
+            const Vec<float, 4> w = a.w ? load_some_of<4>(a.w, a.w_type, i0 + out_along, out_left) : Vec<float, 4>(1.f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = tile[line][out_along + j] * rstds[line] * w[j];
+            store_some<TY, 4>(y + (t0 + line) * a.ldy + i0 + out_along, v, out_left);
+        } else {
+            const float w = a.w ? load_some_of<1>(a.w, a.w_type, i0 + line, 1)[0] : 1.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = tile[out_along + j][line] * rstds[out_along + j] * w;
+            store_some<TY, 4>(y + (i0 + line) * a.ldy + t0 + out_along, v, out_left);
+        }
     }
 }
 
@@ -419,11 +451,12 @@ int norm_back_rows(BackArgs a, hipStream_t s) {
     Temporary t(a.dw ? (size_t)a.parts * a.n * 4 : 0, s);
     if (t.error) return t.error;
     a.part = t.floats();
-    int e = vectors <= 1024   ? norm_back_rows_chunks<TD, TH, 1>(a, s)
-            : vectors <= 2048 ? norm_back_rows_chunks<TD, TH, 2>(a, s)
-            : vectors <= 4096 ? norm_back_rows_chunks<TD, TH, 4>(a, s)
-            : vectors <= 8192 ? norm_back_rows_chunks<TD, TH, 8>(a, s)
-                              : norm_back_rows_chunks<TD, TH, 16>(a, s);
+    int e;
+    if (vectors <= 1024) e = norm_back_rows_chunks<TD, TH, 1>(a, s);
+    else if (vectors <= 2048) e = norm_back_rows_chunks<TD, TH, 2>(a, s);
+    else if (vectors <= 4096) e = norm_back_rows_chunks<TD, TH, 4>(a, s);
+    else if (vectors <= 8192) e = norm_back_rows_chunks<TD, TH, 8>(a, s);
+    else e = norm_back_rows_chunks<TD, TH, V == 4 ? 16 : 8>(a, s);  // 32 bits, up to 65536 features
     if (!e && a.dw) {
         norm_back_weight_kernel<<<(unsigned)((a.n + 63) / 64), 1024, 0, s>>>(a.part, a.parts, a.n, a.dw);
         e = (int)hipGetLastError();

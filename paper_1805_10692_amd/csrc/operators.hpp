@@ -103,6 +103,11 @@ template <class T, int N>
 __device__ __forceinline__ void store_f32(T* p, Vec<float, N> v) {
     store<T, N>(p, __builtin_convertvector(v, Vec<T, N>));
 }
+// The same for what nobody reads soon: it does not take the place of other lines in the caches.
+template <class T, int N>
+__device__ __forceinline__ void store_f32_once(T* p, Vec<float, N> v) {
+    __builtin_nontemporal_store(__builtin_convertvector(v, Vec<T, N>), reinterpret_cast<typename Packed<T, N>::type*>(p));
+}
 // The first `left` of N elements (left may be over N or below 1); the others are 0 and not read.
 template <class T, int N>
 __device__ __forceinline__ Vec<float, N> load_some(const T* p, int64_t left) {
@@ -121,6 +126,18 @@ __device__ __forceinline__ void store_some(T* p, Vec<float, N> v, int64_t left) 
 #pragma unroll
     for (int j = 0; j < N; ++j)
         if (j < left) p[j] = (T)v[j];
+}
+// As they are in memory.
+template <class T, int N>
+__device__ __forceinline__ Vec<T, N> load_own(const T* p, int64_t left) {
+    if (left >= N) return load<T, N>(p);
+    Vec<T, N> v;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        v[j] = (T)0.f;
+        if (j < left) v[j] = p[j];
+    }
+    return v;
 }
 // The same of an array whose type is an argument (one branch for a whole wave).
 template <int N>
