@@ -117,7 +117,7 @@ struct ShrinkArgs {
     int64_t tokens, length;  // of the long axis
     const void* x;
     int64_t ldx;
-    int64_t part;    // elements of the long axis for a workgroup, a multiple of 32 (few tokens) or 64
+    int64_t part;    // elements of the long axis for a workgroup, a multiple of 32 (few tokens), of 128 (rows) or of 512 (columns: two steps for each of eight waves)
     uint32_t parts;  // of the long axis
     float* out;      // [parts][tokens][rank]
     bool scale;      // times s_a
@@ -130,10 +130,10 @@ struct ShrinkArgs {
 template <class TX, class TW, bool kColumns, bool kAlong, int kTiles, int kRanks>
 __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 : 4) void shrink_kernel(ShrinkArgs c) {
     constexpr bool k16 = sizeof(TX) == 2;
-    constexpr int E = 8, kStep = 4 * E, kTile = 16 * kTiles, kPitch = 16 * kRanks + 4, kThreads = kShrinkThreads<kTiles>, kWaves = kThreads / 64;
+    constexpr int E = 8, kStep = 4 * E, kTile = 16 * kTiles, kThreads = kShrinkThreads<kTiles>, kWaves = kThreads / 64;
     using Operand = std::conditional_t<k16, Vec<TX, E>, Vec<float, E>>;
     __shared__ Present present;
-    __shared__ std::conditional_t<kTiles == 1, F4[kRanks][64], float[kPitch]> sums[kTiles == 1 ? kWaves / 2 : kTile];
+    __shared__ F4 sums[kWaves / 2][kTiles * kRanks][64];
     const unsigned item = by_xcd(blockIdx.x, gridDim.x), part = item % c.parts;
     const int64_t t0 = (int64_t)(item / c.parts) * kTile;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
@@ -159,6 +159,7 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
 #pragma unroll
         for (int s = 0; s < kTiles; ++s) x_lane[s] = (uint32_t)(std::min(token[s], tokens_left - 1) * c.ldx + E * g) * sizeof(TX);
     }
+    float* out = c.out + part * c.tokens * c.w.rank;
     for (int first = 0; first < slots; first += abreast) {
         const int q = first + wave % abreast;
         const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
@@ -251,61 +252,43 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
                 if (k < end) step(k, std::false_type());
             }
         }
-        if constexpr (kTiles == 1) {
-            // the pieces of an adapter: the upper half's sums to the lower half's, until there is one
-            for (int half = pieces / 2; half; half /= 2) {
-                if (piece >= half && piece < 2 * half)
+        // the pieces of an adapter: the upper half's sums to the lower half's, until there is one
+        for (int half = pieces / 2; half; half /= 2) {
+            if (piece >= half && piece < 2 * half)
 #pragma unroll
-                    for (int r = 0; r < kRanks; ++r) sums[wave - half * abreast][r][lane] = acc[0][r];
-                __syncthreads();
-                if (piece < half)
+                for (int s = 0; s < kTiles; ++s)
 #pragma unroll
-                    for (int r = 0; r < kRanks; ++r) acc[0][r] += sums[wave][r][lane];
-                __syncthreads();
-            }
-            if (piece == 0 && rank > r0 && present.adapter[i] == a) {
-                float* to_token = c.out + (part * c.tokens + t0 + i) * c.w.rank + r0;
-                const float scale = c.scale ? scale_of(c.w, a) : 1.f;
+                    for (int r = 0; r < kRanks; ++r) sums[wave - half * abreast][s * kRanks + r][lane] = acc[s][r];
+            __syncthreads();
+            if (piece < half)
+#pragma unroll
+                for (int s = 0; s < kTiles; ++s)
+#pragma unroll
+                    for (int r = 0; r < kRanks; ++r) acc[s][r] += sums[wave][s * kRanks + r][lane];
+            __syncthreads();
+        }
+        if (piece == 0 && rank > r0) {
+            const float scale = c.scale ? scale_of(c.w, a) : 1.f;
+#pragma unroll
+            for (int s = 0; s < kTiles; ++s) {
+                if (present.adapter[token[s]] != a) continue;
+                float* to_token = out + (t0 + token[s]) * c.w.rank + r0;
 #pragma unroll
                 for (int r = 0; r < kRanks; ++r)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int at_r = kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r;
-                        if (r0 + at_r < c.w.rank) to_token[at_r] = r0 + at_r < rank ? acc[0][r][e] * scale : 0.f;
+                        if (r0 + at_r < c.w.rank) to_token[at_r] = r0 + at_r < rank ? acc[s][r][e] * scale : 0.f;
                     }
-            }
-        } else {
-            // in turn, in LDS; each token is one adapter's
-            for (int p = 0; p < pieces; ++p) {
-                if (p == piece && rank > r0)
-#pragma unroll
-                    for (int s = 0; s < kTiles; ++s)
-                        if (present.adapter[token[s]] == a)
-#pragma unroll
-                            for (int r = 0; r < kRanks; ++r)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    float* at = &sums[token[s]][kAlong ? 16 * r + 4 * g + e : kRanks * (4 * g + e) + r];
-                                    *at = p ? *at + acc[s][r][e] : acc[s][r][e];
-                                }
-                __syncthreads();
             }
         }
     }
-    // few tokens: those without an adapter, or without ranks here; else all of them
-    float* out = c.out + part * c.tokens * c.w.rank;
+    // tokens without an adapter, or without ranks here
     for (int e = threadIdx.x; e < kTile * 16 * kRanks; e += kThreads) {
         const int t = e / (16 * kRanks), r = e % (16 * kRanks);
         if (t0 + t >= c.tokens || r0 + r >= c.w.rank) continue;
-        const int a = present.adapter[t], rank = a >= 0 ? rank_of(c.w, a) : 0;
-        float all = 0.f;
-        if constexpr (kTiles == 1) {
-            if (rank > r0) continue;
-        } else {
-            if (r0 + r < rank) all = sums[t][r];
-            if (c.scale && a >= 0) all *= scale_of(c.w, a);
-        }
-        out[(t0 + t) * c.w.rank + r0 + r] = all;
+        const int a = present.adapter[t];
+        if (a < 0 || rank_of(c.w, a) <= r0) out[(t0 + t) * c.w.rank + r0 + r] = 0.f;
     }
 }
 
@@ -925,13 +908,7 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
             for (int q = wave; q < groups; q += kOuterBlock / 64) {
                 const int64_t t = first + list[q] * 16 + 4 * g;  // lane group g has tokens t .. t + 3
                 const int some = (int)std::max<int64_t>(0, std::min<int64_t>(to - t, 4));
-                bool own[4], every = true;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    own[k] = k < some && c.index[t + k] == a;
-                    every &= own[k];
-                }
-                every = __all(every);
+                // everything is requested before the tokens' adapters are known
                 F4 xs[4];  // [token k][element 4 i + j]
                 if constexpr (kColumns) {
                     F4 v[4];
@@ -951,11 +928,21 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
 #pragma unroll
                 for (int r = 0; r < kRanks; ++r)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) gs[r][k] = own[k] && r0 + 16 * r + i < rank ? c.g[(t + k) * c.w.rank + r0 + 16 * r + i] : 0.f;
-                if (!every)
+                    for (int k = 0; k < 4; ++k) gs[r][k] = k < some && r0 + 16 * r + i < rank ? c.g[(t + k) * c.w.rank + r0 + 16 * r + i] : 0.f;
+                Vec<int32_t, 4> of;
+                if (some == 4) {
+                    of = load<int32_t, 4>(c.index + t);
+                } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (!own[k]) xs[k] = 0.f;
+                    for (int k = 0; k < 4; ++k) of[k] = k < some ? c.index[t + k] : -1;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (of[k] != a) {  // another adapter's token, whatever it holds
+                        xs[k] = 0.f;
+#pragma unroll
+                        for (int r = 0; r < kRanks; ++r) gs[r][k] = 0.f;
+                    }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -1147,7 +1134,7 @@ struct ShrinkShape {
         const int64_t abreast = std::min<int64_t>({16, tokens, adapters});
         const int64_t want = tokens <= kFewTokens ? std::min<int64_t>(256 / blocks, length / std::max<int64_t>(128, 512 / abreast))
                                                   : std::min<int64_t>(512 / blocks, (length + 255) / 256);
-        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(want, 64)), step = tokens <= kFewTokens ? 32 : 64;
+        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(want, 64)), step = tokens <= kFewTokens ? 32 : columns && tiles == 4 ? 512 : 128;
         part = ((length + cut - 1) / cut + step - 1) / step * step;
         parts = (int)((length + part - 1) / part);
     }
