@@ -1,7 +1,7 @@
 """Python binding of the C ABI in include/cer.h -- argument marshalling only.
 
 Every function has the name of the C entry point it calls; the product calls (cer_matmul, cser_matmul, cer_matmul_noalloc,
-csr_matmul) and the operators beside a projection are native functions of _cerpy (csrc/pybind.cpp), because a small product takes less time than ctypes does.  Device buffers are passed as torch
+csr_matmul) are native functions of _cerpy (csrc/pybind.cpp) and the operators beside a projection of _cerops (csrc/pybind_operators.cpp), because a small product takes less time than ctypes does.  Device buffers are passed as torch
 tensors (their ``data_ptr()`` is handed to the library) or as raw integer addresses; streams as
 ``torch.cuda.Stream`` objects, raw ``hipStream_t`` integers, or None for the current torch stream.
 No step of the product runs in Python or in torch, and there is no CPU fallback: if the built
@@ -195,8 +195,6 @@ def lib() -> ctypes.CDLL:
         L.cer_last_hip_error.argtypes = []
         L.adapter_workspace_bytes.restype = i64
         L.adapter_workspace_bytes.argtypes = [i64] * 4
-        _cerpy.bind_operators(*(ctypes.cast(getattr(L, f), vp).value
-                                for f in ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip")))
         _cerpy.bind(*(ctypes.cast(getattr(L, f), vp).value
                       for f in ("cer_matmul", "cser_matmul", "cer_matmul_noalloc", "csr_matmul")))
         _lib = L
@@ -230,22 +228,35 @@ if _cerpy is not None:
     # f(h, X, Y, batch, stream=None) -> None
     cer_matmul, cser_matmul = _cerpy.cer_matmul, _cerpy.cser_matmul
     cer_matmul_noalloc, csr_matmul = _cerpy.cer_matmul_noalloc, _cerpy.csr_matmul
-    # Operators beside a projection (csrc/pybind_operators.cpp; include/cer.h says what each computes).  Activations are tensors of
-    # shape (tokens, features): contiguous rows, or, fp32, the transposed view of a contiguous (features, tokens) tensor, which is
-    # how cer_matmul has its X and Y.
-    rms_norm, rms_norm_backward = _cerpy.rms_norm, _cerpy.rms_norm_backward
-    adapter_matmul, adapter_backward = _cerpy.adapter_matmul, _cerpy.adapter_backward
-    grad_norm, grad_clip = _cerpy.grad_norm, _cerpy.grad_clip
 else:
     def cer_matmul(h, X, Y, batch: int, stream=None) -> None:
         lib()  # raises: not built
 
     cser_matmul = cer_matmul_noalloc = csr_matmul = cer_matmul
 
-    def rms_norm(*args, **kwargs) -> None:
-        lib()  # raises: not built
+# Operators beside a projection (csrc/pybind_operators.cpp; include/cer.h says what each computes).  Activations are tensors of shape
+# (tokens, features): contiguous rows, or, fp32, the transposed view of a contiguous (features, tokens) tensor, which is how cer_matmul has
+# its X and Y.  They are native functions of _cerops, which is loaded, after torch, when one of them is first asked for:
+#   rms_norm(X, Y, weight=None, residual=None, sum=None, eps=1e-6, scale=None, rstd=None, stream=None)
+#   rms_norm_backward(dY, H, rstd, dX, weight=None, dsum=None, dweight=None, stream=None)
+#   adapter_matmul(A, B, index, X, Y, scales=None, ranks=None, base=None, hidden=None, workspace=None, stream=None)
+#   adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)
+#   grad_norm(grads, norm, stream=None)
+#   grad_clip(grads, max_norm, norm, outs=None, stream=None)
+_OPERATORS = ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip")
 
-    rms_norm_backward = adapter_matmul = adapter_backward = grad_norm = grad_clip = rms_norm
+
+def __getattr__(name: str):
+    if name not in _OPERATORS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    L = lib()
+    import torch  # noqa: F401  (its libraries are _cerops' own)
+    from . import _cerops
+    _cerops.setup(_check)
+    _cerops.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _OPERATORS))
+    for f in _OPERATORS:
+        globals()[f] = getattr(_cerops, f)
+    return globals()[name]
 
 
 class Handle:

@@ -1,4 +1,4 @@
-"""Builds the HIP library in-tree, paper_1805_10692_amd/libcer_hip.so (gfx950 only), and the native part of its binding, _cerpy.so.
+"""Builds the HIP library in-tree, paper_1805_10692_amd/libcer_hip.so (gfx950 only), and the native parts of its binding, _cerpy.so and _cerops.so.
 
     python -m paper_1805_10692_amd.build
 """
@@ -13,6 +13,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcer_hip.so")
 NATIVE_BINDING = os.path.join(PKG, "_cerpy.so")
+NATIVE_OPERATORS = os.path.join(PKG, "_cerops.so")
 SOURCES = ["cer_host.cpp", "cer_capi.cpp", "cer_gemv.hip", "cer_gemm.hip", "cer_xtile.hip", "cer_strip.hip", "cer_narrow.hip", "cer_mfma.hip", "cer_fused.hip", "cer_tile.hip", "cer_matmul.hip", "dense_kernels.hip", "csr.hip", "cost_model.cpp", "frontend.hip",
            "operators_capi.cpp", "norm.hip", "adapter.hip", "clip.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -39,12 +40,28 @@ def build_binding(verbose: bool = True) -> str:
     """_cerpy.so: host code only, the interpreter's C API."""
     tmp = NATIVE_BINDING + f".tmp{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
-           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "pybind.cpp"), os.path.join(CSRC, "pybind_operators.cpp"), "-o", tmp]
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "pybind.cpp"), "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
     os.replace(tmp, NATIVE_BINDING)
     return NATIVE_BINDING
+
+
+def build_operators_binding(verbose: bool = True) -> str:
+    """_cerops.so: host code only, the interpreter's C API and torch's C++ interface (whose libraries are there when it is imported, after torch)."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    tmp = NATIVE_OPERATORS + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_paths()["include"], "-isystem", os.path.join(at, "include"),
+           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"), os.path.join(CSRC, "pybind_operators.cpp"), "-o", tmp,
+           "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(tmp, NATIVE_OPERATORS)
+    return NATIVE_OPERATORS
 
 
 def build_library(verbose: bool = True) -> str:
@@ -58,6 +75,7 @@ def build_library(verbose: bool = True) -> str:
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
     build_binding(verbose)
+    build_operators_binding(verbose)
     return LIB
 
 

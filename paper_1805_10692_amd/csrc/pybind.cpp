@@ -5,10 +5,10 @@
 // object), the library and the HIP launch 2.5 us.  The same checks and conversions through the C API take 0.5 us.  The
 // module links to neither torch nor the library: the entry points' addresses are handed over by binding.py when it has
 // loaded the library (`bind`), tensors are read through their Python attributes.
-#include "pybind.hpp"
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
 
 #include <cstdint>
-#include <vector>
 
 namespace {
 
@@ -90,9 +90,8 @@ bool device_pointer(PyObject* t, void** out) {
     return ok;
 }
 
-}  // namespace
-
-bool cerpy::stream_pointer(PyObject* s, void** out) {
+// None: the current torch stream of the current device; an int; or an object with .cuda_stream.
+bool stream_pointer(PyObject* s, void** out) {
     if (s && s != Py_None) return PyLong_Check(s) ? address_of(s, out) : attribute_address(s, s_cuda_stream, out);
     PyObject* v;
     if (g_raw_stream) {
@@ -122,31 +121,6 @@ bool cerpy::stream_pointer(PyObject* s, void** out) {
     return ok;
 }
 
-long cerpy::current_device() {
-    if (!g_get_device) return -1;
-    PyObject* v = PyObject_CallNoArgs(g_get_device);
-    if (!v) return -2;
-    const long d = PyLong_AsLong(v);
-    Py_DECREF(v);
-    return d == -1 && PyErr_Occurred() ? -2 : d;
-}
-
-bool cerpy::raise_unless_ok(int rc, const char* name) {
-    if (rc == 0) return true;
-    PyObject* r = PyObject_CallFunction(g_check, "is", rc, name);
-    Py_XDECREF(r);
-    return r != nullptr;
-}
-
-bool cerpy::load_library() {
-    PyObject* l = g_load ? PyObject_CallNoArgs(g_load) : PyErr_Format(PyExc_RuntimeError, "binding.py has not set up its native part");
-    Py_XDECREF(l);
-    return l != nullptr;
-}
-
-namespace {
-using cerpy::stream_pointer;
-
 const char* const kArgNames[5] = {"h", "X", "Y", "batch", "stream"};
 
 PyObject* product(int which, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
@@ -165,7 +139,9 @@ PyObject* product(int which, PyObject* const* args, Py_ssize_t nargs, PyObject* 
     for (int i = 0; i < 4; ++i)
         if (!a[i]) return PyErr_Format(PyExc_TypeError, "%s() missing required argument '%s'", kNames[which], kArgNames[i]);
     if (!g_fn[which]) {  // the library is not loaded yet
-        if (!cerpy::load_library()) return nullptr;
+        PyObject* l = g_load ? PyObject_CallNoArgs(g_load) : PyErr_Format(PyExc_RuntimeError, "binding.py has not set up its native part");
+        if (!l) return nullptr;
+        Py_DECREF(l);
         if (!g_fn[which]) return PyErr_Format(PyExc_RuntimeError, "%s is not bound", kNames[which]);
     }
     void *h, *X, *Y, *s;
@@ -178,7 +154,11 @@ PyObject* product(int which, PyObject* const* args, Py_ssize_t nargs, PyObject* 
     Py_BEGIN_ALLOW_THREADS
     rc = g_fn[which](h, static_cast<const float*>(X), static_cast<float*>(Y), batch, s);
     Py_END_ALLOW_THREADS
-    if (!cerpy::raise_unless_ok(rc, kNames[which])) return nullptr;
+    if (rc != 0) {
+        PyObject* r = PyObject_CallFunction(g_check, "is", rc, kNames[which]);
+        if (!r) return nullptr;
+        Py_DECREF(r);
+    }
     Py_RETURN_NONE;
 }
 
@@ -234,11 +214,5 @@ PyMODINIT_FUNC PyInit__cerpy(void) {
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!cerpy::setup_operators()) return nullptr;
-    static std::vector<PyMethodDef> methods;  // of both sources; the module keeps the address
-    for (PyMethodDef* m = g_methods; m->ml_name; ++m) methods.push_back(*m);
-    for (PyMethodDef* m = cerpy::operator_methods; m->ml_name; ++m) methods.push_back(*m);
-    methods.push_back({nullptr, nullptr, 0, nullptr});
-    g_module.m_methods = methods.data();
     return PyModule_Create(&g_module);
 }

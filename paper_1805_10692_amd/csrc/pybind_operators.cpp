@@ -1,9 +1,14 @@
-// The operators beside a projection as native functions of the binding: rms_norm, rms_norm_backward, adapter_matmul, adapter_backward, grad_norm,
-// grad_clip.  Tensors are read through their Python attributes (sizes, strides, type, address, device), as in pybind.cpp, and for
-// the same reason: a decode step's call lasts some microseconds on the GPU.
-#include "pybind.hpp"
+// The operators beside a projection as native functions of the binding (_cerops): rms_norm, rms_norm_backward, adapter_matmul, adapter_backward,
+// grad_norm, grad_clip.
+//
+// A call takes up to eight tensors and a decode step's call lasts some microseconds on the GPU.  Read through their Python attributes, a
+// tensor's shape, strides, type, device and address cost 0.6 us (torch makes a new object for each); torch's C++ interface gives them in some
+// nanoseconds.  The entry points' addresses are handed over by binding.py when it has loaded the library (`bind`).
+#include <Python.h>
+#include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <exception>
 #include <vector>
 
 #include "../../include/cer.h"
@@ -25,26 +30,11 @@ struct {
     ClipFn grad_clip;
 } g_fn = {};
 
-PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_numel, *s_is_contiguous;
+PyObject* g_check = nullptr;       // binding._check(rc, name): raises for an error code
+PyObject* g_get_device = nullptr;  // torch._C._cuda_getDevice, ._cuda_getCurrentRawStream
+PyObject* g_raw_stream = nullptr;
+PyObject* s_cuda_stream = nullptr;
 constexpr int kInt32 = 100;  // beside CER_TYPE_*
-PyObject* g_dtype[5] = {};   // torch's, in the order of kTypes
-constexpr int kTypes[5] = {CER_TYPE_F32, CER_TYPE_BF16, CER_TYPE_F16, CER_TYPE_F8, kInt32};
-
-bool know_types() {
-    if (g_dtype[0]) return true;
-    static const char* const names[5] = {"float32", "bfloat16", "float16", "float8_e4m3fn", "int32"};
-    PyObject* torch = PyImport_ImportModule("torch");
-    if (!torch) return false;
-    PyObject* found[5] = {};
-    bool ok = true;
-    for (int i = 0; i < 5 && ok; ++i) ok = (found[i] = PyObject_GetAttrString(torch, names[i])) != nullptr;
-    Py_DECREF(torch);
-    for (int i = 0; i < 5; ++i) {
-        if (ok) g_dtype[i] = found[i];
-        else Py_XDECREF(found[i]);
-    }
-    return ok;
-}
 
 bool fail(const char* what, const char* why) {
     PyErr_Format(PyExc_ValueError, "%s %s", what, why);
@@ -89,74 +79,71 @@ bool take(const Signature& f, PyObject* const* args, Py_ssize_t nargs, PyObject*
     return true;
 }
 
-// Steals v.
-bool to_int64(PyObject* v, int64_t* out) {
-    if (!v) return false;
-    *out = (int64_t)PyLong_AsLongLong(v);
-    Py_DECREF(v);
-    return !(*out == -1 && PyErr_Occurred());
+const at::Tensor* tensor_of(PyObject* o, const char* what) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s must be a torch tensor", what);
+        return nullptr;
+    }
+    const at::Tensor* t = &THPVariable_Unpack(o);
+    if (t->layout() == at::kStrided) return t;
+    fail(what, "must be a dense tensor");
+    return nullptr;
 }
-bool address_of(PyObject* t, void** out) {
-    PyObject* v = PyObject_CallMethodNoArgs(t, s_data_ptr);
-    if (!v) return false;
-    *out = PyLong_AsVoidPtr(v);
-    Py_DECREF(v);
-    return *out || !PyErr_Occurred();
+int type_of(const at::Tensor& t) {  // -1: another one
+    switch (t.scalar_type()) {
+        case at::kFloat: return CER_TYPE_F32;
+        case at::kBFloat16: return CER_TYPE_BF16;
+        case at::kHalf: return CER_TYPE_F16;
+        case at::kFloat8_e4m3fn: return CER_TYPE_F8;
+        case at::kInt: return kInt32;
+        default: return -1;
+    }
 }
-bool type_of(PyObject* t, int* out) {  // -1: another one
-    PyObject* d = PyObject_GetAttr(t, s_dtype);
-    if (!d) return false;
-    *out = -1;
-    for (int i = 0; i < 5; ++i)
-        if (d == g_dtype[i]) *out = kTypes[i];
-    Py_DECREF(d);
-    return true;
-}
-// All tensors of a call: in device memory, on the current device.
+
+// All tensors of a call: in device memory, on the current device.  The stream is asked for when there has been one (torch has initialised the
+// device then).
 struct Device {
     long current = -1;
-    bool known = false;
-    bool has(PyObject* t, const char* what) {
-        int64_t d;
-        if (!to_int64(PyObject_CallMethodNoArgs(t, s_get_device), &d)) return false;
-        if (d < 0) return fail(what, "must be in device memory");
-        if (!known) {
-            current = cerpy::current_device();
-            if (current == -2) return false;
-            known = true;
+    bool has(const at::Tensor& t, const char* what) {
+        if (!t.is_cuda()) return fail(what, "must be in device memory");
+        if (current < 0) {
+            PyObject* v = PyObject_CallNoArgs(g_get_device);
+            if (!v) return false;
+            current = PyLong_AsLong(v);
+            Py_DECREF(v);
+            if (current == -1 && PyErr_Occurred()) return false;
         }
-        if (current >= 0 && d != current) return fail(what, "is on another device than the current one");
+        if (t.get_device() != current) return fail(what, "is on another device than the current one");
         return true;
+    }
+    // None: the current torch stream of the current device; an int; or an object with .cuda_stream.
+    bool stream(PyObject* s, void** out) {
+        PyObject* v;
+        if (!s) {
+            PyObject* device = PyLong_FromLong(current);
+            v = device ? PyObject_CallOneArg(g_raw_stream, device) : nullptr;
+            Py_XDECREF(device);
+        } else if (PyLong_Check(s)) {
+            Py_INCREF(s);
+            v = s;
+        } else {
+            v = PyObject_GetAttr(s, s_cuda_stream);
+        }
+        if (!v) return false;
+        *out = PyLong_AsVoidPtr(v);
+        Py_DECREF(v);
+        return *out || !PyErr_Occurred();
     }
 };
 
-// Sizes and strides (in elements) of a tensor of `dims` dimensions.
-bool layout_of(PyObject* t, const char* what, int dims, int64_t* size, int64_t* stride) {
-    PyObject* shape = PyObject_GetAttr(t, s_shape);
-    if (!shape) return false;
-    PyObject* strides = PyObject_CallMethodNoArgs(t, s_stride);
-    if (!strides) {
-        Py_DECREF(shape);
-        return false;
-    }
-    bool ok = PyTuple_Check(shape) && PyTuple_Check(strides) && PyTuple_GET_SIZE(shape) == dims && PyTuple_GET_SIZE(strides) == dims;
-    if (!ok) PyErr_Format(PyExc_ValueError, "%s must have %d dimensions", what, dims);
-    for (int i = 0; i < dims && ok; ++i) {
-        size[i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
-        stride[i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(strides, i));
-        ok = !PyErr_Occurred();
-    }
-    Py_DECREF(shape);
-    Py_DECREF(strides);
-    return ok;
-}
-
 // (tokens, features), either dimension contiguous.  *tokens, *features: -1 takes the tensor's, else they have to be.
-bool tokens_of(PyObject* t, const char* what, Device& dev, cer_tokens_t* out, int64_t* tokens, int64_t* features) {
-    int64_t size[2], stride[2];
-    int type;
-    if (!dev.has(t, what) || !type_of(t, &type) || !layout_of(t, what, 2, size, stride)) return false;
+bool tokens_of(PyObject* o, const char* what, Device& dev, cer_tokens_t* out, int64_t* tokens, int64_t* features) {
+    const at::Tensor* t = tensor_of(o, what);
+    if (!t || !dev.has(*t, what)) return false;
+    if (t->dim() != 2) return fail(what, "must have 2 dimensions");
+    const int type = type_of(*t);
     if (type < 0 || type == kInt32) return fail(what, "must be float32, bfloat16, float16 or float8_e4m3fn");
+    const int64_t size[2] = {t->sizes()[0], t->sizes()[1]}, stride[2] = {t->strides()[0], t->strides()[1]};
     if (*tokens < 0) *tokens = size[0];
     if (*features < 0) *features = size[1];
     if (size[0] != *tokens || size[1] != *features) return fail(what, "has another shape than the other arguments ask for");
@@ -170,8 +157,10 @@ bool tokens_of(PyObject* t, const char* what, Device& dev, cer_tokens_t* out, in
     } else {
         return fail(what, "must have one contiguous dimension");
     }
+    if (size[0] <= 1 && out->order == CER_ORDER_ROWS) out->ld = size[1];  // not used: one token
     if (size[0] == 0 || size[1] == 0) out->ld = 0;
-    return address_of(t, &out->data);
+    out->data = t->data_ptr();
+    return true;
 }
 // A single token's or feature's order is both of them: the one that the call's other matrices have.
 void same_order(cer_tokens_t* m, const cer_tokens_t& as, int64_t tokens, int64_t features) {
@@ -192,30 +181,20 @@ void same_order(cer_tokens_t* m, const cer_tokens_t& as, int64_t tokens, int64_t
 }
 
 // A contiguous tensor of `numbers` elements (-1: any number) of a type (-1: any of the three floating ones, told in *type).
-bool flat_of(PyObject* t, const char* what, Device& dev, int type, int64_t numbers, void** out, int* type_out = nullptr, int64_t* numbers_out = nullptr) {
-    int have;
-    if (!dev.has(t, what) || !type_of(t, &have)) return false;
+bool flat_of(PyObject* o, const char* what, Device& dev, int type, int64_t numbers, void** out, int* type_out = nullptr, int64_t* numbers_out = nullptr) {
+    const at::Tensor* t = tensor_of(o, what);
+    if (!t || !dev.has(*t, what)) return false;
+    const int have = type_of(*t);
     if (type >= 0 ? have != type : (have != CER_TYPE_F32 && have != CER_TYPE_BF16 && have != CER_TYPE_F16))
         return fail(what, type == kInt32 ? "must be int32" : type == CER_TYPE_F32 ? "must be float32" : "must be float32, bfloat16 or float16");
-    PyObject* c = PyObject_CallMethodNoArgs(t, s_is_contiguous);
-    if (!c) return false;
-    const bool contiguous = c == Py_True;
-    Py_DECREF(c);
-    if (!contiguous) return fail(what, "must be contiguous");
-    int64_t n;
-    if (!to_int64(PyObject_CallMethodNoArgs(t, s_numel), &n)) return false;
-    if (numbers >= 0 && n != numbers) return fail(what, "has another number of elements than the other arguments ask for");
+    if (!t->is_contiguous()) return fail(what, "must be contiguous");
+    if (numbers >= 0 && t->numel() != numbers) return fail(what, "has another number of elements than the other arguments ask for");
     if (type_out) *type_out = have;
-    if (numbers_out) *numbers_out = n;
-    return address_of(t, out);
-}
-
-bool ready(const void* fn, const char* name) {
-    if (!know_types()) return false;
-    if (fn) return true;
-    if (!cerpy::load_library()) return false;
+    if (numbers_out) *numbers_out = t->numel();
+    *out = t->data_ptr();
     return true;
 }
+
 template <class Fn, class... Args>
 PyObject* call(Fn fn, const char* name, Args... args) {
     if (!fn) return PyErr_Format(PyExc_RuntimeError, "%s is not bound", name);
@@ -223,7 +202,11 @@ PyObject* call(Fn fn, const char* name, Args... args) {
     Py_BEGIN_ALLOW_THREADS
     rc = fn(args...);
     Py_END_ALLOW_THREADS
-    if (!cerpy::raise_unless_ok(rc, name)) return nullptr;
+    if (rc != 0) {
+        PyObject* r = PyObject_CallFunction(g_check, "is", rc, name);
+        if (!r) return nullptr;
+        Py_DECREF(r);
+    }
     Py_RETURN_NONE;
 }
 
@@ -232,9 +215,8 @@ PyObject* py_rms_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObje
     enum { X, Y, kWeight, kResidual, kSum, kEps, kScale, kRstd, kStream, kCount };
     static const Signature f = {"rms_norm", 2, kCount, names};
     PyObject* a[kCount];
-    if (!ready((const void*)g_fn.norm, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void* stream;
-    if (!cerpy::stream_pointer(a[kStream], &stream)) return nullptr;
     Device dev;
     int64_t tokens = -1, n = -1;
     cer_tokens_t x{}, y{}, r{}, sum{};
@@ -250,6 +232,7 @@ PyObject* py_rms_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObje
     if (a[kRstd] && !flat_of(a[kRstd], "rstd", dev, CER_TYPE_F32, tokens, &rstd)) return nullptr;
     const double eps = a[kEps] ? PyFloat_AsDouble(a[kEps]) : 1e-6;
     if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    if (!dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.norm, f.name, &x, &r, &sum, &y, tokens, n, weight, weight_type, (float)eps, static_cast<float*>(scale), static_cast<float*>(rstd), stream);
 }
 
@@ -258,9 +241,8 @@ PyObject* py_rms_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t narg
     enum { kDY, H, kRstd, kDX, kWeight, kDSum, kDWeight, kStream, kCount };
     static const Signature f = {"rms_norm_backward", 4, kCount, names};
     PyObject* a[kCount];
-    if (!ready((const void*)g_fn.norm_backward, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void* stream;
-    if (!cerpy::stream_pointer(a[kStream], &stream)) return nullptr;
     Device dev;
     int64_t tokens = -1, n = -1;
     cer_tokens_t dy{}, h{}, dsum{}, dx{};
@@ -275,24 +257,25 @@ PyObject* py_rms_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t narg
     if (!flat_of(a[kRstd], "rstd", dev, CER_TYPE_F32, tokens, &rstd)) return nullptr;
     if (a[kWeight] && !flat_of(a[kWeight], "weight", dev, -1, n, &weight, &weight_type)) return nullptr;
     if (a[kDWeight] && !flat_of(a[kDWeight], "dweight", dev, CER_TYPE_F32, n, &dweight)) return nullptr;
+    if (!dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.norm_backward, f.name, &dy, &h, &dsum, &dx, tokens, n, static_cast<float*>(rstd), weight, weight_type, static_cast<float*>(dweight), stream);
 }
 
 // A (adapters, rank, in), B (adapters, out, rank), scales, ranks, index
-bool adapters_of(PyObject* A, PyObject* B, PyObject* scales, PyObject* ranks, Device& dev, cer_adapters_t* w) {
-    int64_t sa[3], ta[3], sb[3], tb[3];
-    int type_a, type_b;
-    void *pa, *pb, *ps = nullptr, *pr = nullptr;
-    if (!dev.has(A, "A") || !dev.has(B, "B") || !type_of(A, &type_a) || !type_of(B, &type_b)) return false;
-    if (type_a != CER_TYPE_F32 && type_a != CER_TYPE_BF16 && type_a != CER_TYPE_F16) return fail("A", "must be float32, bfloat16 or float16");
-    if (type_b != type_a) return fail("B", "must have A's type");
-    if (!layout_of(A, "A", 3, sa, ta) || !layout_of(B, "B", 3, sb, tb)) return false;
+bool adapters_of(PyObject* a, PyObject* b, PyObject* scales, PyObject* ranks, Device& dev, cer_adapters_t* w) {
+    const at::Tensor *A = tensor_of(a, "A"), *B = A ? tensor_of(b, "B") : nullptr;
+    if (!B || !dev.has(*A, "A") || !dev.has(*B, "B")) return false;
+    const int type = type_of(*A);
+    if (type != CER_TYPE_F32 && type != CER_TYPE_BF16 && type != CER_TYPE_F16) return fail("A", "must be float32, bfloat16 or float16");
+    if (type_of(*B) != type) return fail("B", "must have A's type");
+    if (A->dim() != 3 || B->dim() != 3) return fail("A, B", "must have 3 dimensions");
+    const auto sa = A->sizes(), ta = A->strides(), sb = B->sizes(), tb = B->strides();
     if (sb[0] != sa[0] || sb[2] != sa[1]) return fail("B", "must have A's number of adapters and rank: A (adapters, rank, in), B (adapters, out, rank)");
     if ((ta[2] != 1 && sa[2] > 1) || (tb[2] != 1 && sb[2] > 1)) return fail("A, B", "must have contiguous rows");
+    void *ps = nullptr, *pr = nullptr;
     if (scales && !flat_of(scales, "scales", dev, CER_TYPE_F32, sa[0], &ps)) return false;
     if (ranks && !flat_of(ranks, "ranks", dev, kInt32, sa[0], &pr)) return false;
-    if (!address_of(A, &pa) || !address_of(B, &pb)) return false;
-    *w = {pa, pb, static_cast<float*>(ps), static_cast<int32_t*>(pr), sa[0], sa[1], sa[2], sb[1], ta[0], ta[1], tb[0], tb[1], type_a};
+    *w = {A->data_ptr(), B->data_ptr(), static_cast<float*>(ps), static_cast<int32_t*>(pr), sa[0], sa[1], sa[2], sb[1], ta[0], ta[1], tb[0], tb[1], type};
     return true;
 }
 
@@ -301,9 +284,8 @@ PyObject* py_adapter_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, 
     enum { A, B, kIndex, X, Y, kScales, kRanks, kBase, kHidden, kWorkspace, kStream, kCount };
     static const Signature f = {"adapter_matmul", 5, kCount, names};
     PyObject* a[kCount];
-    if (!ready((const void*)g_fn.adapter, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void* stream;
-    if (!cerpy::stream_pointer(a[kStream], &stream)) return nullptr;
     Device dev;
     cer_adapters_t w;
     if (!adapters_of(a[A], a[B], a[kScales], a[kRanks], dev, &w)) return nullptr;
@@ -319,6 +301,7 @@ PyObject* py_adapter_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, 
     if (!flat_of(a[kIndex], "index", dev, kInt32, tokens, &index)) return nullptr;
     if (a[kHidden] && !flat_of(a[kHidden], "hidden", dev, CER_TYPE_F32, tokens * w.rank, &hidden)) return nullptr;
     if (a[kWorkspace] && !flat_of(a[kWorkspace], "workspace", dev, CER_TYPE_F32, -1, &workspace, nullptr, &room)) return nullptr;
+    if (!dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.adapter, f.name, &w, static_cast<const int32_t*>(index), tokens, &x, &base, &y, static_cast<float*>(hidden), workspace, room * 4, stream);
 }
 
@@ -327,9 +310,8 @@ PyObject* py_adapter_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs
     enum { A, B, kIndex, kDY, X, kHidden, kScales, kRanks, kBase, kDX, kDA, kDB, kStream, kCount };
     static const Signature f = {"adapter_backward", 6, kCount, names};
     PyObject* a[kCount];
-    if (!ready((const void*)g_fn.adapter_backward, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void* stream;
-    if (!cerpy::stream_pointer(a[kStream], &stream)) return nullptr;
     Device dev;
     cer_adapters_t w;
     if (!adapters_of(a[A], a[B], a[kScales], a[kRanks], dev, &w)) return nullptr;
@@ -347,6 +329,7 @@ PyObject* py_adapter_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs
     if (!flat_of(a[kHidden], "hidden", dev, CER_TYPE_F32, tokens * w.rank, &hidden)) return nullptr;
     if (a[kDA] && !flat_of(a[kDA], "dA", dev, CER_TYPE_F32, w.adapters * w.rank * w.in, &dA)) return nullptr;
     if (a[kDB] && !flat_of(a[kDB], "dB", dev, CER_TYPE_F32, w.adapters * w.rank * w.out, &dB)) return nullptr;
+    if (!dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.adapter_backward, f.name, &w, static_cast<const int32_t*>(index), tokens, &dy, &x, static_cast<const float*>(hidden), &base, &dx,
                 static_cast<float*>(dA), static_cast<float*>(dB), stream);
 }
@@ -385,11 +368,11 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObj
     static const char* const names[] = {"grads", "norm", "stream"};
     static const Signature f = {"grad_norm", 2, 3, names};
     PyObject* a[3];
-    if (!ready((const void*)g_fn.grad_norm, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void *stream, *norm;
     Device dev;
     std::vector<cer_gradient_t> list;
-    if (!cerpy::stream_pointer(a[2], &stream) || !gradients_of(a[0], nullptr, dev, &list) || !flat_of(a[1], "norm", dev, CER_TYPE_F32, 1, &norm)) return nullptr;
+    if (!gradients_of(a[0], nullptr, dev, &list) || !flat_of(a[1], "norm", dev, CER_TYPE_F32, 1, &norm) || !dev.stream(a[2], &stream)) return nullptr;
     return call(g_fn.grad_norm, f.name, list.data(), (int64_t)list.size(), static_cast<float*>(norm), stream);
 }
 
@@ -397,18 +380,25 @@ PyObject* py_grad_clip(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObj
     static const char* const names[] = {"grads", "max_norm", "norm", "outs", "stream"};
     static const Signature f = {"grad_clip", 3, 5, names};
     PyObject* a[5];
-    if (!ready((const void*)g_fn.grad_clip, f.name) || !take(f, args, nargs, kwnames, a)) return nullptr;
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
     void *stream, *norm;
     Device dev;
     std::vector<cer_gradient_t> list;
-    if (!cerpy::stream_pointer(a[4], &stream) || !gradients_of(a[0], a[3], dev, &list) || !flat_of(a[2], "norm", dev, CER_TYPE_F32, 1, &norm)) return nullptr;
+    if (!gradients_of(a[0], a[3], dev, &list) || !flat_of(a[2], "norm", dev, CER_TYPE_F32, 1, &norm) || !dev.stream(a[4], &stream)) return nullptr;
     const double most = PyFloat_AsDouble(a[1]);
     if (most == -1.0 && PyErr_Occurred()) return nullptr;
     return call(g_fn.grad_clip, f.name, list.data(), (int64_t)list.size(), (float)most, static_cast<float*>(norm), stream);
 }
 
-// bind_operators(addresses): where the loaded library has them, in the order of g_fn
-PyObject* bind_operators(PyObject*, PyObject* args) {
+// setup(check): binding.py's function
+PyObject* setup(PyObject*, PyObject* check) {
+    Py_INCREF(check);
+    Py_XSETREF(g_check, check);
+    Py_RETURN_NONE;
+}
+
+// bind(addresses): where the loaded library has the operators, in the order of g_fn
+PyObject* bind(PyObject*, PyObject* args) {
     unsigned long long at[6];
     if (!PyArg_ParseTuple(args, "KKKKKK", &at[0], &at[1], &at[2], &at[3], &at[4], &at[5])) return nullptr;
     g_fn = {reinterpret_cast<NormFn>((uintptr_t)at[0]),    reinterpret_cast<NormBackwardFn>((uintptr_t)at[1]),
@@ -417,12 +407,23 @@ PyObject* bind_operators(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
-}  // namespace
+using Entry = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t, PyObject*);
+template <Entry kEntry>  // torch's interface may throw; nothing does through the interpreter
+PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    try {
+        return kEntry(self, args, nargs, kwnames);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+    }
+    return nullptr;
+}
 
 #define CER_OPERATOR(name, fn, text) \
-    {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(fn)), METH_FASTCALL | METH_KEYWORDS, text}
+    {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(guarded<fn>)), METH_FASTCALL | METH_KEYWORDS, text}
 
-PyMethodDef cerpy::operator_methods[] = {
+PyMethodDef g_methods[] = {
     CER_OPERATOR("rms_norm", py_rms_norm, "rms_norm(X, Y, weight=None, residual=None, sum=None, eps=1e-6, scale=None, rstd=None, stream=None)\n--\n\n"),
     CER_OPERATOR("rms_norm_backward", py_rms_norm_backward, "rms_norm_backward(dY, H, rstd, dX, weight=None, dsum=None, dweight=None, stream=None)\n--\n\n"),
     CER_OPERATOR("adapter_matmul", py_adapter_matmul,
@@ -431,17 +432,21 @@ PyMethodDef cerpy::operator_methods[] = {
                  "adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_norm", py_grad_norm, "grad_norm(grads, norm, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_clip", py_grad_clip, "grad_clip(grads, max_norm, norm, outs=None, stream=None)\n--\n\n"),
-    {"bind_operators", bind_operators, METH_VARARGS, nullptr},
+    {"setup", setup, METH_O, nullptr},
+    {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
-bool cerpy::setup_operators() {
-    s_dtype = PyUnicode_InternFromString("dtype");
-    s_shape = PyUnicode_InternFromString("shape");
-    s_stride = PyUnicode_InternFromString("stride");
-    s_data_ptr = PyUnicode_InternFromString("data_ptr");
-    s_get_device = PyUnicode_InternFromString("get_device");
-    s_numel = PyUnicode_InternFromString("numel");
-    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-    return s_dtype && s_shape && s_stride && s_data_ptr && s_get_device && s_numel && s_is_contiguous;
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_cerops", "Native operator calls of the binding.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__cerops(void) {
+    PyObject* c = PyImport_ImportModule("torch._C");
+    if (!c) return nullptr;
+    g_get_device = PyObject_GetAttrString(c, "_cuda_getDevice");
+    g_raw_stream = g_get_device ? PyObject_GetAttrString(c, "_cuda_getCurrentRawStream") : nullptr;
+    Py_DECREF(c);
+    s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    return g_raw_stream && s_cuda_stream ? PyModule_Create(&g_module) : nullptr;
 }
