@@ -241,6 +241,9 @@ ADAPTER_TYPES = [(F32, F32, False), (F32, F32, True), (F32, BF16, True), (F32, F
 ADAPTER_SHAPES = [(1, 64, 64, 1, 16, "last"), (1, 257, 131, 3, 5, "last"), (2, 1, 1, 2, 1, "any"), (7, 700, 190, 4, 8, "any"), (16, 96, 1000, 20, 17, "any"), (64, 320, 256, 70, 16, "any"),
                   (65, 33, 65, 2, 33, "runs"), (130, 512, 64, 3, 64, "none"), (257, 129, 96, 5, 24, "runs"), (300, 200, 320, 9, 100, "any"), (1030, 70, 90, 3, 16, "runs"),
                   (1100, 40, 72, 2, 130, "runs"), (2100, 64, 40, 3, 8, "any"), (40, 300, 80, 2, 256, "runs")]
+#: many tokens: whole and broken tiles of 64 by 64, ranks in eights and not, more adapters in a tile than are taken together
+WIDE_SHAPES = [(320, 256, 128, 4, 16, "runs"), (513, 200, 193, 3, 24, "any"), (449, 640, 330, 6, 40, "runs"), (385, 129, 257, 5, 64, "any"), (300, 65, 200, 2, 72, "runs"), (640, 320, 64, 1, 128, "last"),
+               (260, 140, 150, 2, 200, "runs"), (333, 90, 100, 3, 36, "any"), (700, 1100, 70, 90, 8, "any")]
 
 
 def make_adapters(shape, types, ragged):
@@ -270,7 +273,7 @@ def opt(x):
 
 
 @pytest.mark.parametrize("types", ADAPTER_TYPES, ids=lambda t: f"{t[0]}-{t[1]}-{int(t[2])}".replace("torch.", ""))
-@pytest.mark.parametrize("shape", ADAPTER_SHAPES, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("shape", ADAPTER_SHAPES + WIDE_SHAPES, ids=lambda s: "-".join(map(str, s)))
 def test_adapter_matmul(shape, types):
     tokens, n, m, N, R, kind = shape
     ta, tw, columns = types
@@ -296,7 +299,7 @@ def test_adapter_matmul(shape, types):
 
 
 @pytest.mark.parametrize("types", ADAPTER_TYPES, ids=lambda t: f"{t[0]}-{t[1]}-{int(t[2])}".replace("torch.", ""))
-@pytest.mark.parametrize("shape", ADAPTER_SHAPES, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("shape", ADAPTER_SHAPES + WIDE_SHAPES, ids=lambda s: "-".join(map(str, s)))
 def test_adapter_backward(shape, types):
     tokens, n, m, N, R, kind = shape
     ta, tw, columns = types
@@ -319,28 +322,31 @@ def test_adapter_backward(shape, types):
     near(GdB, dB, (tokens + 8) * U * sB, "dB")
 
 
-@pytest.mark.parametrize("columns", [False, True])
-def test_adapters_keep_requests_apart(columns):
-    """A request of NaN and infinities between two others, and an adapter of NaN that nobody has: nothing of them shows elsewhere."""
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("types", [(F32, False), (F32, True), (BF16, False), (F16, False)], ids=lambda t: f"{t[0]}-{int(t[1])}".replace("torch.", ""))
+def test_adapters_keep_requests_apart(types, wide):
+    """A request of NaN and infinities between two others, one whose adapter is NaN, and an adapter of NaN that nobody has: nothing of them shows elsewhere."""
+    ta, columns = types
     gen = torch.Generator().manual_seed(5)
-    tokens, n, m, N, R = 90, 100, 140, 4, 12
-    A, Bm = rand(gen, N, R, n).double(), rand(gen, N, m, R).double()
-    x, dy, base = rand(gen, tokens, n).double(), rand(gen, tokens, m).double(), rand(gen, tokens, m).double()
-    index = torch.tensor([0] * 20 + [1] * 13 + [-1] * 7 + [2] * 50, dtype=torch.int32)
+    n, m, N, R = 100, 140, 5, 16
+    tokens = 400 if wide else 97
+    A, Bm = rand(gen, N, R, n).to(ta).double(), rand(gen, N, m, R).to(ta).double()
+    x, dy, base = rand(gen, tokens, n).to(ta).double(), rand(gen, tokens, m).to(ta).double(), rand(gen, tokens, m).to(ta).double()
+    index = torch.tensor([0] * 20 + [1] * 13 + [-1] * 7 + [2] * (tokens - 47) + [4] * 7, dtype=torch.int32)
     clean, hidden, size = adapters_oracle(A, Bm, None, None, index, x, base)
     dx, sx, dA, sA, dB, sB = backward_oracle(A, Bm, None, None, index, dy, x, hidden, None)
-    A[3], Bm[3] = NAN, NAN
+    A[3:], Bm[3:] = NAN, NAN
     x[20:40], dy[20:40], base[20:33] = NAN, float("inf"), NAN
     hidden[20:40] = NAN
-    GA, GB, I = A.float().cuda(), Bm.float().cuda(), index.cuda()
-    Y = room_for(tokens, m, F32, columns)
-    B.adapter_matmul(GA, GB, I, put(x, F32, columns), Y, base=put(base, F32, columns))
-    fine = [t for t in range(tokens) if not 20 <= t < 33]
-    near(Y[fine], clean[fine], ((n + R + 8) * U * size)[fine], "y")
-    assert torch.isnan(host(Y)[20:33]).all()
-    DX, GdA, GdB = room_for(tokens, n, F32, columns), torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
-    B.adapter_backward(GA, GB, I, put(dy, F32, columns), put(x, F32, columns), hidden.float().cuda(), dX=DX, dA=GdA, dB=GdB)
-    near(DX[fine], dx[fine], ((m + R + 8) * U * sx)[fine], "dx")
+    GA, GB, I = A.to(ta).cuda(), Bm.to(ta).cuda(), index.cuda()
+    Y = room_for(tokens, m, ta, columns)
+    B.adapter_matmul(GA, GB, I, put(x, ta, columns), Y, base=put(base, ta, columns))
+    fine = [t for t in range(tokens - 7) if not 20 <= t < 33]
+    near(Y[fine], clean[fine], stored(clean, ta, (n + R + 8) * U * size)[fine], "y")
+    assert torch.isnan(host(Y)[20:33]).all() and torch.isnan(host(Y)[-7:]).all()
+    DX, GdA, GdB = room_for(tokens, n, ta, columns), torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
+    B.adapter_backward(GA, GB, I, put(dy, ta, columns), put(x, ta, columns), hidden.float().cuda(), dX=DX, dA=GdA, dB=GdB)
+    near(DX[fine], dx[fine], stored(dx, ta, (m + R + 8) * U * sx)[fine], "dx")
     for a in (0, 2, 3):
         near(GdA[a], dA[a], (m + tokens + 8) * U * sA[a], "dA")
         near(GdB[a], dB[a], (tokens + 8) * U * sB[a], "dB")
