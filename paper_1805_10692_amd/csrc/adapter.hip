@@ -123,8 +123,8 @@ struct ShrinkArgs {
     bool scale;      // times s_a
 };
 
-// kTiles * 16 tokens, kRanks * 16 ranks from blockIdx.z on; the waves share out the adapters and pieces of the workgroup's part of the long
-// axis.  Lane (i, g) = (lane % 16, lane / 16) holds of both sides' operands row i's (a rank's, a token's) eight elements of 32 of the long axis
+// Few tokens (kTiles = 1), and columns of many (4): kTiles * 16 tokens, kRanks * 16 ranks from blockIdx.z on; the waves share out the adapters and pieces
+// of the workgroup's part of the long axis.  Lane (i, g) = (lane % 16, lane / 16) holds of both sides' operands row i's (a rank's, a token's) eight elements of 32 of the long axis
 // that belong to g: one 16-bit instruction, or eight 32-bit ones that take one of every g's.  The sides agree on which, and that is all that
 // their order has to do.  Rows of ranks: 16 r + i, or where a rank's elements lie apart (!kAlong) kRanks i + r, neighbours in one load.
 template <class TX, class TW, bool kColumns, bool kAlong, int kTiles, int kRanks>
@@ -180,9 +180,6 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
             }
             const int ranks_left = rank - r0 - kRanks * i;
             const bool ranks_whole = rank - r0 >= 16 * kRanks;
-            bool here[kTiles];  // rows: tiles in which the adapter occurs (columns: a lane's vector has a token of each)
-#pragma unroll
-            for (int s = 0; s < kTiles; ++s) here[s] = kColumns || kTiles == 1 || __any(present.adapter[token[s]] == a);
             auto step = [&](int k, auto whole) {  // whole: nothing of the step is past the end
                 constexpr bool kWhole = decltype(whole)::value;
                 const int left = kWhole ? E : to - (k + E * g);
@@ -202,7 +199,6 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
                 } else {
 #pragma unroll
                     for (int s = 0; s < kTiles; ++s) {
-                        if (!here[s]) continue;
                         if constexpr (k16) xs[s] = load_own<TX, E>(at(x + k, x_lane[s]), left);
                         else xs[s] = load_some<TX, E>(at(x + k, x_lane[s]), left);
                     }
@@ -231,7 +227,6 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
                 for (int s = 0; s < kTiles; ++s)
 #pragma unroll
                     for (int r = 0; r < kRanks; ++r) {
-                        if (!here[s]) continue;
                         if constexpr (k16) {
                             acc[s][r] = product(ws[r], xs[s], acc[s][r]);
                         } else {
@@ -307,7 +302,7 @@ __global__ __launch_bounds__(kRowsBlock, kRanks == 8 ? 2 : 4) void shrink_rows_k
     constexpr int kLoads = (R * kChunk / V + kRowsBlock - 1) / kRowsBlock;  // of a thread for an adapter's chunk
     using Operand = std::conditional_t<k16, Vec<TX, 8>, Vec<float, 8>>;
     __shared__ Present present;
-    __shared__ TW staged[2][2][R][kRow];  // [turn][slot]
+    alignas(16) __shared__ TW staged[2][2][R][kRow];  // [turn][slot]
     const unsigned item = by_xcd(blockIdx.x, gridDim.x), part = item % c.parts;
     const int64_t t0 = (int64_t)(item / c.parts) * kTile;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, set = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * R;
@@ -418,7 +413,14 @@ __global__ __launch_bounds__(kRowsBlock, kRanks == 8 ? 2 : 4) void shrink_rows_k
                     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
                         for (int r = 0; r < kRanks; ++r) {
-                            const Vec<TW, 8> w = *reinterpret_cast<const Vec<TW, 8>*>(&staged[turn][q][16 * r + i][set * (kChunk / 2) + 32 * h + 8 * g]);
+                            const TW* line = &staged[turn][q][16 * r + i][set * (kChunk / 2) + 32 * h + 8 * g];  // at a multiple of 16 bytes
+                            Vec<TW, 8> w;
+                            if constexpr (sizeof(TW) == 4) {
+                                const F4 low = *reinterpret_cast<const F4*>(line), high = *reinterpret_cast<const F4*>(line + 4);
+                                w = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+                            } else {
+                                w = *reinterpret_cast<const Vec<TW, 8>*>(line);
+                            }
                             if constexpr (k16) {
                                 acc[q][r] = product(w, xs[u][h], acc[q][r]);
                             } else {
@@ -612,7 +614,7 @@ __device__ __forceinline__ void pieces_of(float x, uint16_t (&p)[kPieces]) {
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         if (k + 1 < kPieces) {
-            const uint32_t high = __float_as_uint(x) & 0xFFFF0000u;
+            const uint32_t high = x == x ? __float_as_uint(x) & 0xFFFF0000u : 0x7FC00000u;
             p[k] = (uint16_t)(high >> 16);
             x -= __uint_as_float(high);
             x = x == x ? x : 0.f;

@@ -9,7 +9,7 @@
 namespace {
 using namespace cer;
 
-constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 22;
+constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostAdapterTokens = (int64_t)1 << 24, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 22;
 
 int bytes_of(int type) { return type == CER_TYPE_F32 ? 4 : type == CER_TYPE_F8 ? 1 : 2; }
 bool number_type(int type) { return type == CER_TYPE_F32 || type == CER_TYPE_BF16 || type == CER_TYPE_F16; }
@@ -38,7 +38,7 @@ int result(int hip) { return hip ? record_hip_error(hip) : CER_OK; }
 int check_adapters(const cer_adapters_t* w, int64_t tokens) {
     if (!w || !w->A || !w->B || !number_type(w->type)) return CER_E_INVALID;
     if (w->adapters < 1 || w->rank < 1 || w->in < 1 || w->out < 1 || tokens < 0) return CER_E_INVALID;
-    if (w->rank > kMostRank || w->adapters > kMostAdapters || w->in > kMostFeatures || w->out > kMostFeatures || tokens > kMostTokens) return CER_E_TOO_LARGE;
+    if (w->rank > kMostRank || w->adapters > kMostAdapters || w->in > kMostFeatures || w->out > kMostFeatures || tokens > kMostAdapterTokens) return CER_E_TOO_LARGE;
     if (tokens * w->rank >= (int64_t)1 << 31 || w->adapters * w->rank * std::max(w->in, w->out) > (int64_t)1 << 33) return CER_E_TOO_LARGE;
     if (reinterpret_cast<uintptr_t>(w->A) % bytes_of(w->type) || reinterpret_cast<uintptr_t>(w->B) % bytes_of(w->type)) return CER_E_INVALID;
     if (w->stride_a < 0 || w->stride_b < 0 || w->ld_a < 0 || w->ld_b < 0) return CER_E_INVALID;
@@ -87,7 +87,7 @@ int rms_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_t
 
 int64_t adapter_workspace_bytes(int64_t tokens, int64_t rank, int64_t in, int64_t out) {
     if (tokens < 0 || rank < 1 || in < 1 || out < 1) return CER_E_INVALID;
-    if (tokens > kMostTokens || rank > kMostRank || in > kMostFeatures || out > kMostFeatures) return CER_E_TOO_LARGE;
+    if (tokens > kMostAdapterTokens || rank > kMostRank || in > kMostFeatures || out > kMostFeatures) return CER_E_TOO_LARGE;
     return tokens ? adapter_workspace(tokens, rank, in, out) : 0;
 }
 
