@@ -31,7 +31,7 @@ using F4 = Vec<float, 4>;
 constexpr int kBlock = 256, kWaves = kBlock / 64;
 template <int kTiles>
 constexpr int kShrinkThreads = kTiles == 1 ? 1024 : 512;
-constexpr int kFewBlock = 1024, kOuterBlock = 256, kRowsBlock = 512;
+constexpr int kOuterBlock = 256, kRowsBlock = 512;
 constexpr int kMostTile = 64;  // tokens of a workgroup
 constexpr int64_t kFewTokens = 256;
 
@@ -599,11 +599,11 @@ __device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int
     }
 }
 
-template <class TX, class TW, bool kColumns, bool kAlong>
-__global__ __launch_bounds__(kFewBlock) void expand_kernel(ExpandArgs c) {
+template <class TX, class TW, bool kColumns, bool kAlong, int kThreads>
+__global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs c) {
     extern __shared__ float room[];
     __shared__ Present present;
-    expand_some<TX, TW, kColumns, kAlong, kFewBlock>(c, (int64_t)blockIdx.x * 16, (int64_t)blockIdx.y * 64, present, room);
+    expand_some<TX, TW, kColumns, kAlong, kThreads>(c, (int64_t)blockIdx.x * 16, (int64_t)blockIdx.y * 64, present, room);
 }
 
 // ---- expand, many tokens --------------------------------------------------------------------------------------------------------
@@ -840,9 +840,22 @@ struct OuterArgs {
     const void* x;
     int64_t ldx;
     int64_t range;  // tokens for a workgroup (blockIdx.z), a multiple of 16
-    float* out;     // [gridDim.z][adapters][rank][length], or kRankLast: [gridDim.z][adapters][length][rank]
-    bool scale;
+    uint32_t parts;   // such ranges
+    uint32_t blocks;  // workgroups for an adapter and range
+    float* out;       // [parts][adapters][rank][length], or rank_last: [parts][adapters][length][rank]
+    bool scale, rank_last;
 };
+// dA and dB in one launch: they do not depend on one another, and alone neither fills the chip at a small step's sizes.
+struct OuterPair {
+    OuterArgs a, b;  // b.blocks == 0: only a
+};
+// Which of the two a workgroup belongs to, and its number there; false: nothing to do.
+__device__ __forceinline__ bool outer_of(const OuterPair& pair, OuterArgs& c, unsigned& block) {
+    const bool second = blockIdx.x >= pair.a.blocks;
+    c = second ? pair.b : pair.a;
+    block = blockIdx.x - (second ? pair.a.blocks : 0);
+    return blockIdx.z < c.parts;
+}
 
 // The groups of kGroup tokens in from .. to in which the adapter occurs, in their order, for up to kOuterBlock groups from `first` on: their numbers
 // into `list`; returns how many.  All threads call it.
@@ -890,15 +903,18 @@ __device__ __forceinline__ void add_waves(F4 (&acc)[kSums], F4 (*room)[kSums][64
 }
 
 // Adapter blockIdx.y, 64 elements of the long axis, kRanks * 16 ranks; the waves share out the groups of 16 tokens in which the adapter occurs.
-template <class TX, bool kColumns, bool kRankLast, int kRanks>
-__global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
+template <class TX, bool kColumns, int kRanks>
+__global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
+    OuterArgs c;
+    unsigned block;
+    if (!outer_of(pair, c, block)) return;
     __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
     __shared__ F4 room[kOuterBlock / 128][kRanks * 4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
     const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks);
-    const int64_t o0 = (int64_t)(blockIdx.x / rank_blocks) * 64;
+    const int64_t o0 = (int64_t)(block / rank_blocks) * 64;
     const int left = (int)std::min<int64_t>(c.length - o0, 64);
-    const int r0 = (int)(blockIdx.x % rank_blocks) * 16 * kRanks;
+    const int r0 = (int)(block % rank_blocks) * 16 * kRanks;
     const int rank = rank_of(c.w, a);
     const int64_t from = blockIdx.z * c.range, to = from + c.range < c.tokens ? from + c.range : c.tokens;
     F4 acc[kRanks * 4];  // [rank tile][j]
@@ -961,7 +977,7 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
 #pragma unroll
     for (int r = 0; r < kRanks; ++r) {
         const int at = r0 + 16 * r + 4 * g;
-        if constexpr (kRankLast) {
+        if (c.rank_last) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (4 * i + j < left && at < c.w.rank) store_some<float, 4>(out + (o0 + 4 * i + j) * c.w.rank + at, acc[4 * r + j] * scale, c.w.rank - at);
@@ -982,16 +998,19 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterArgs c) {
 // elements of one token: a lane loads eight by eight (kCols = 8; 16 bytes of 8 tokens, sixteen lanes 256 bytes side by side) and
 // turns them in its registers.  The other operand, d or hidden as three bf16 pieces, lies in `planes` as lanes take it (planes_kernel); fp16
 // activations are two bf16 pieces.  Nothing is lost against products in 32 bits.
-template <class TX, bool kRankLast, int kRanks, int kCols>
-__global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterArgs c) {
+template <class TX, int kRanks, int kCols>
+__global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterPair pair) {
+    OuterArgs c;
+    unsigned block;
+    if (!outer_of(pair, c, block)) return;
     constexpr int kX = kWeightPieces<TX>, kSums = kRanks * kCols;
     __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
     __shared__ F4 room[kOuterBlock / 128][kSums][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
     const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks), rank_tiles = (c.w.rank + 15) / 16;
-    const int64_t o0 = (int64_t)(blockIdx.x / rank_blocks) * (16 * kCols);
+    const int64_t o0 = (int64_t)(block / rank_blocks) * (16 * kCols);
     const int left = (int)std::min<int64_t>(c.length - o0, 16 * kCols) - kCols * i;
-    const int tile0 = (int)(blockIdx.x % rank_blocks) * kRanks;
+    const int tile0 = (int)(block % rank_blocks) * kRanks;
     const int rank = rank_of(c.w, a);
     const int64_t from = blockIdx.z * c.range, to = from + c.range < c.tokens ? from + c.range : c.tokens;
     const uint32_t x_lane = (uint32_t)(8 * g * c.ldx + kCols * i) * sizeof(TX);
@@ -1063,7 +1082,7 @@ __global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterArgs c) {
     for (int r = 0; r < kRanks; ++r) {
         const int at = 16 * (tile0 + r) + 4 * g;
         // a rank past the adapter's own: the planes have 0 there
-        if constexpr (kRankLast) {
+        if (c.rank_last) {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
                 if (k < left && at < c.w.rank) store_some<float, 4>(out + (o0 + kCols * i + k) * c.w.rank + at, acc[r * kCols + k], c.w.rank - at);
@@ -1176,7 +1195,9 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
     if (c.tokens <= kFewTokens || c.length < 64 || c.w.rank % 8) {
         const int64_t across = (c.tokens + 15) / 16;
         const dim3 grid((unsigned)across, (unsigned)blocks);
-        expand_kernel<TX, TW, kColumns, kAlong><<<grid, kFewBlock, few, s>>>(c);
+        // sixteen waves for up to sixteen adapters, where that many workgroups run together; else eight
+        if (across * blocks <= 512) expand_kernel<TX, TW, kColumns, kAlong, 1024><<<grid, 1024, few, s>>>(c);
+        else expand_kernel<TX, TW, kColumns, kAlong, 512><<<grid, 512, few, s>>>(c);
     } else {
         // the tokens' hidden is made ready once for a workgroup: as many blocks for each as leave about four workgroups for a compute unit
         const int64_t across = c.tokens / 64, most = std::max<int64_t>(1, 1024 / across), whole = c.length / 64;
@@ -1205,47 +1226,57 @@ int expand(ExpandArgs c, const cer_tokens_t& base, const cer_tokens_t& y, int32_
     return columns ? expand_tiles<float, float, true, kAlong>(c, s) : expand_tiles<float, float, false, kAlong>(c, s);
 }
 
-template <class TX, bool kColumns, bool kRankLast>
-int outer_ranks(const OuterArgs& c, unsigned parts, hipStream_t s) {
-    const int ranks = c.w.rank <= 16 ? 1 : c.w.rank <= 32 ? 2 : 4;
-    const dim3 grid((unsigned)((c.length + 63) / 64 * ((c.w.rank + 16 * ranks - 1) / (16 * ranks))), (unsigned)c.w.adapters, parts);
-    if (ranks == 1) outer_kernel<TX, kColumns, kRankLast, 1><<<grid, kOuterBlock, 0, s>>>(c);
-    else if (ranks == 2) outer_kernel<TX, kColumns, kRankLast, 2><<<grid, kOuterBlock, 0, s>>>(c);
-    else outer_kernel<TX, kColumns, kRankLast, 4><<<grid, kOuterBlock, 0, s>>>(c);
-    return (int)hipGetLastError();
-}
-template <class TX, bool kRankLast>
-int outer16_ranks(const OuterArgs& c, unsigned parts, hipStream_t s) {
-    const int ranks = c.w.rank <= 16 ? 1 : c.w.rank <= 32 ? 2 : 4, cols = ranks == 4 ? 4 : 8;
-    const dim3 grid((unsigned)((c.length + 16 * cols - 1) / (16 * cols) * ((c.w.rank + 16 * ranks - 1) / (16 * ranks))), (unsigned)c.w.adapters, parts);
-    if (ranks == 1) outer16_kernel<TX, kRankLast, 1, 8><<<grid, kOuterBlock, 0, s>>>(c);
-    else if (ranks == 2) outer16_kernel<TX, kRankLast, 2, 8><<<grid, kOuterBlock, 0, s>>>(c);
-    else outer16_kernel<TX, kRankLast, 4, 4><<<grid, kOuterBlock, 0, s>>>(c);
-    return (int)hipGetLastError();
-}
-
-// The tokens are cut into ranges where an adapter's workgroups alone would be few: up to about 1024 workgroups, 512 tokens at least.
-template <bool kRankLast>
-int outer(OuterArgs c, const cer_tokens_t& x, hipStream_t s) {
+// How one side's outer products are cut: the tokens into ranges where an adapter's workgroups alone would be few (up to about 1024 workgroups, 512 tokens
+// at least), the long axis into 64 elements, or 128 for activations in 16 bits and ranks up to 32.
+void outer_shape(OuterArgs& c, const cer_tokens_t& x) {
     c.x = x.data, c.ldx = x.ld;
     const int64_t without = c.w.adapters * ((c.length + 127) / 128);
-    const unsigned parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>({16, c.tokens / 512, 1024 / without}));
-    c.range = ((c.tokens + parts - 1) / parts + 31) / 32 * 32;
-    const int64_t numbers = c.w.adapters * c.w.rank * c.length;
-    float* out = c.out;
-    Temporary t(parts > 1 ? (size_t)parts * numbers * 4 : 0, s);
-    if (t.error) return t.error;
-    if (parts > 1) c.out = t.floats();
-    int e;
-    if (x.type == CER_TYPE_BF16) e = outer16_ranks<__bf16, kRankLast>(c, parts, s);
-    else if (x.type == CER_TYPE_F16) e = outer16_ranks<_Float16, kRankLast>(c, parts, s);
-    else if (x.order == CER_ORDER_COLUMNS) e = outer_ranks<float, true, kRankLast>(c, parts, s);
-    else e = outer_ranks<float, false, kRankLast>(c, parts, s);
-    if (!e && parts > 1) {
-        outer_sum_kernel<<<(unsigned)((numbers + 4 * kBlock - 1) / (4 * kBlock)), kBlock, 0, s>>>(c.out, parts, numbers, out);
-        e = (int)hipGetLastError();
+    c.parts = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({16, c.tokens / 512, 1024 / without}));
+    c.range = ((c.tokens + c.parts - 1) / c.parts + 31) / 32 * 32;
+    const int ranks = c.w.rank <= 16 ? 1 : c.w.rank <= 32 ? 2 : 4;
+    const int elements = x.type != CER_TYPE_F32 && ranks < 4 ? 128 : 64;
+    c.blocks = (uint32_t)((c.length + elements - 1) / elements * ((c.w.rank + 16 * ranks - 1) / (16 * ranks)));
+}
+
+// dA and dB, or one of them (`both` false: a).
+int outer(OuterPair p, bool both, const cer_tokens_t& x_of_a, const cer_tokens_t& x_of_b, hipStream_t s) {
+    outer_shape(p.a, x_of_a);
+    if (both) outer_shape(p.b, x_of_b);
+    OuterArgs* const sides[2] = {&p.a, &p.b};
+    float* out[2];
+    int64_t numbers[2], room = 0;
+    for (int k = 0; k < (both ? 2 : 1); ++k) {
+        out[k] = sides[k]->out;
+        numbers[k] = sides[k]->w.adapters * sides[k]->w.rank * sides[k]->length;
+        if (sides[k]->parts > 1) room += sides[k]->parts * numbers[k];
     }
-    return e;
+    Temporary t((size_t)room * 4, s);
+    if (t.error) return t.error;
+    float* next = t.floats();
+    for (int k = 0; k < (both ? 2 : 1); ++k)
+        if (sides[k]->parts > 1) {
+            sides[k]->out = next;
+            next += sides[k]->parts * numbers[k];
+        }
+    const dim3 grid(p.a.blocks + (both ? p.b.blocks : 0), (unsigned)p.a.w.adapters, both ? std::max(p.a.parts, p.b.parts) : p.a.parts);
+    const int rank = p.a.w.rank;
+    auto go = [&](auto kernel) { kernel<<<grid, kOuterBlock, 0, s>>>(p); };
+    auto of_ranks = [&](auto one, auto two, auto four) {
+        if (rank <= 16) go(one);
+        else if (rank <= 32) go(two);
+        else go(four);
+    };
+    if (x_of_a.type == CER_TYPE_BF16) of_ranks(outer16_kernel<__bf16, 1, 8>, outer16_kernel<__bf16, 2, 8>, outer16_kernel<__bf16, 4, 4>);
+    else if (x_of_a.type == CER_TYPE_F16) of_ranks(outer16_kernel<_Float16, 1, 8>, outer16_kernel<_Float16, 2, 8>, outer16_kernel<_Float16, 4, 4>);
+    else if (x_of_a.order == CER_ORDER_COLUMNS) of_ranks(outer_kernel<float, true, 1>, outer_kernel<float, true, 2>, outer_kernel<float, true, 4>);
+    else of_ranks(outer_kernel<float, false, 1>, outer_kernel<float, false, 2>, outer_kernel<float, false, 4>);
+    if (int e = (int)hipGetLastError()) return e;
+    for (int k = 0; k < (both ? 2 : 1); ++k) {
+        if (sides[k]->parts == 1) continue;
+        outer_sum_kernel<<<(unsigned)((numbers[k] + 4 * kBlock - 1) / (4 * kBlock)), kBlock, 0, s>>>(sides[k]->out, sides[k]->parts, numbers[k], out[k]);
+        if (int e = (int)hipGetLastError()) return e;
+    }
+    return 0;
 }
 
 int clear(float* out, int64_t numbers, hipStream_t s) {  // the sum of no parts
@@ -1312,15 +1343,13 @@ int launch_adapters_backward(const AdapterBackwardCall& c, hipStream_t s) {
         shrink_sum_kernel<<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, part, (uint32_t)f.parts);
         if (int e = (int)hipGetLastError()) return e;
     }
-    if (c.dA) {  // before dx, which may lie where x does
-        OuterArgs o{};
-        o.g = d, o.planes = d_planes, o.w = side_a(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.in, o.out = c.dA;
-        if (int e = outer<false>(o, c.x, s)) return e;
-    }
-    if (c.dB) {
-        OuterArgs o{};
-        o.g = c.hidden, o.planes = hidden_planes, o.w = side_b(c.w), o.index = c.index, o.tokens = c.tokens, o.length = c.w.out, o.out = c.dB, o.scale = true;
-        if (int e = outer<true>(o, c.dy, s)) return e;
+    if (c.dA || c.dB) {  // before dx, which may lie where x or dy does
+        OuterArgs of_a{}, of_b{};
+        of_a.g = d, of_a.planes = d_planes, of_a.w = side_a(c.w), of_a.index = c.index, of_a.tokens = c.tokens, of_a.length = c.w.in, of_a.out = c.dA;
+        of_b.g = c.hidden, of_b.planes = hidden_planes, of_b.w = side_b(c.w), of_b.index = c.index, of_b.tokens = c.tokens, of_b.length = c.w.out, of_b.out = c.dB;
+        of_b.scale = of_b.rank_last = true;
+        const bool both = c.dA && c.dB;
+        if (int e = outer(c.dA ? OuterPair{of_a, of_b} : OuterPair{of_b, {}}, both, c.dA ? c.x : c.dy, c.dy, s)) return e;
     }
     if (c.dx.data) {
         ExpandArgs b{};
