@@ -117,7 +117,7 @@ struct ShrinkArgs {
     int64_t tokens, length;  // of the long axis
     const void* x;
     int64_t ldx;
-    int64_t part;    // elements of the long axis for a workgroup, a multiple of 32 (few tokens), of 128 (rows) or of 512 (columns: two steps for each of eight waves)
+    int64_t part;    // elements of the long axis for a workgroup, a multiple of 32 (few tokens), of 128 (rows) or (columns) of 512, two steps for each of eight waves, or 256
     uint32_t parts;  // of the long axis
     float* out;      // [parts][tokens][rank]
     bool scale;      // times s_a
@@ -139,11 +139,13 @@ __global__ __launch_bounds__(kShrinkThreads<kTiles>, kTiles * kRanks >= 16 ? 2 :
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, r0 = blockIdx.z * 16 * kRanks;
     list_adapters(present, c.index, t0, kTile, c.tokens, c.w.adapters);
     const int slots = __builtin_amdgcn_readfirstlane(present.slots);
-    const int abreast = kTiles > 1 ? 1 : slots > 8 ? 16 : slots > 4 ? 8 : slots > 2 ? 4 : slots > 1 ? 2 : 1, pieces = kWaves / abreast, piece = wave / abreast;
     // the workgroup's part of the long axis; its waves take turns, so that together they read neighbouring lines, or, few tokens, a stretch each
     const int from = part * (int)c.part, to = std::min<int64_t>(from + c.part, c.length);
     constexpr int kAhead = kTiles * kRanks <= 2 ? 4 : kTiles * kRanks <= (kTiles == 1 && !k16 ? 4 : 8) ? 2 : 1;  // steps whose loads are on their way together
     constexpr int kRun = kAhead * kStep;
+    const int want = slots > 8 ? 16 : slots > 4 ? 8 : slots > 2 ? 4 : slots > 1 ? 2 : 1;
+    const int runs = kTiles > 1 ? (to - from + kRun - 1) / kRun : 1;  // many tokens: as many abreast as leave every wave a run
+    const int abreast = std::min(want, runs > 4 ? 1 : runs > 2 ? 2 : runs > 1 ? 4 : kWaves), pieces = kWaves / abreast, piece = wave / abreast;
     const int stretch = kTiles == 1 ? ((to - from + pieces - 1) / pieces + kStep - 1) / kStep * kStep : kRun;
     const int k_first = from + piece * stretch, k_last = kTiles == 1 ? std::min(k_first + stretch, to) : to, k_next = kTiles == 1 ? kRun : pieces * kRun;
     int token[kTiles];  // in the tile
@@ -1155,7 +1157,7 @@ struct ShrinkShape {
         const int64_t abreast = std::min<int64_t>({16, tokens, adapters});
         const int64_t want = tokens <= kFewTokens ? std::min<int64_t>(256 / blocks, length / std::max<int64_t>(128, 512 / abreast))
                                                   : std::min<int64_t>(512 / blocks, (length + 255) / 256);
-        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(want, 64)), step = tokens <= kFewTokens ? 32 : columns && tiles == 4 ? 512 : 128;
+        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(want, 64)), step = tokens <= kFewTokens ? 32 : columns && tiles == 4 ? (blocks < 32 ? 256 : 512) : 128;
         part = ((length + cut - 1) / cut + step - 1) / step * step;
         parts = (int)((length + part - 1) / part);
     }
