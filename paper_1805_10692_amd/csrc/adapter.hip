@@ -647,12 +647,12 @@ __device__ __forceinline__ void weight_operands(const Vec<TW, 8> v, Pieces8 (&ou
 }
 
 // 64 tokens.  A wave takes 64 elements of the long axis at a time, with what base has there in registers, and goes through the adapters, each
-// one's weights (ranks up to kChunks * 32; 0: any, loaded again for every tile) in registers.  Element o0 + 4 i + j is row (column) i of
+// one's weights (ranks up to kChunks * 32; 0: any, loaded again for every tile of 16 tokens) in registers.  Element o0 + 4 i + j is row (column) i of
 // tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as bf16 pieces by the weights' pieces in the 16-bit instruction, at an
 // eighth to a fifth of the 32-bit one's time: three pieces where y has 32 bits, two where it has 16 (2^-16 of hidden, an eighth of half a
 // step of y in fp16); products of pieces that are together below that are left out.
 template <class TX, class TW, bool kColumns, bool kAlong, int kChunks>
-__global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
+__global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kernel(ExpandArgs c) {
     constexpr int kTile = 64, kH = sizeof(TX) == 4 ? 3 : 2, kW = kWeightPieces<TW>, kHeld = kChunks ? kChunks : 1;
     extern __shared__ float room[];
     __shared__ Present present;
@@ -698,7 +698,7 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
     auto sum_of = [&](int r) {
         F4 sum = 0.f;
         const float* p = c.part + (t0 + t) * c.w.rank + r;
-        if (r < c.w.rank)  // in eights
+        if (r < c.w.rank)  // in fours
 #pragma unroll 4
             for (uint32_t k = 0; k < c.parts; ++k) sum += load<float, 4>(p + k * c.tokens * c.w.rank);
         return sum;
@@ -740,27 +740,35 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
             const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
             const int rank = a >= 0 ? rank_of(c.w, a) : 0;
             const TW* w = static_cast<const TW*>(c.w.w) + (a >= 0 ? a * c.w.stride : 0) + (kAlong ? o0 : o0 * c.w.ld);
-            auto weights = [&](int r0, Pieces8 (&ws)[4][kW]) {  // past the rank: 0, whatever is there; lanes there read the first eight ranks again
-                const bool mine = r0 + 8 * g < rank;
-                const uint32_t from = here(w_lane) + (uint32_t)(mine ? kAlong ? (r0 + 8 * g) * c.w.ld : r0 + 8 * g : 0) * sizeof(TW);
+            // Past the rank: 0, whatever is there.  Lanes whose ranks are past the rows' end read the first ones again.
+            auto weights = [&](int r0, Pieces8 (&ws)[4][kW]) {
+                const int low = r0 + 8 * g;
+                auto place = [&](int r) { return here(w_lane) + (uint32_t)(r < c.w.rank ? kAlong ? r * c.w.ld : r : 0) * sizeof(TW); };
                 Vec<TW, 8> u[4];
-                if constexpr (kAlong) {  // w[r * ld + o]
+                if constexpr (kAlong) {  // w[r * ld + o]; the rows' number is a multiple of four
+                    const uint32_t first = place(low), second = place(low + 4);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const Vec<TW, 4> v = load<TW, 4>(at(w + e * c.w.ld, from));
+                        const Vec<TW, 4> v = load<TW, 4>(at(w + e % 4 * c.w.ld, e < 4 ? first : second));
 #pragma unroll
                         for (int j = 0; j < 4; ++j) u[j][e] = v[j];
                     }
-                } else {
+                } else if (c.w.rank % 8 == 0) {
+                    const uint32_t first = place(low);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) u[j] = load<TW, 8>(at(w + j * c.w.ld, from));
+                    for (int j = 0; j < 4; ++j) u[j] = load<TW, 8>(at(w + j * c.w.ld, first));
+                } else {
+                    const uint32_t first = place(low), second = place(low + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        u[j] = __builtin_shufflevector(load<TW, 4>(at(w + j * c.w.ld, first)), load<TW, 4>(at(w + j * c.w.ld, second)), 0, 1, 2, 3, 4, 5, 6, 7);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (rank % 8)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) u[j][e] = r0 + 8 * g + e < rank ? u[j][e] : (TW)0.f;
-                    else if (!mine)
+                        for (int e = 0; e < 8; ++e) u[j][e] = low + e < rank ? u[j][e] : (TW)0.f;
+                    else if (low >= rank)
                         u[j] = (TW)0.f;
                     weight_operands<TW>(u[j], ws[j]);
                 }
@@ -770,7 +778,8 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
             if constexpr (kChunks)
                 if (rank > 0)
 #pragma unroll
-                    for (int r = 0; r < kChunks; ++r) weights(32 * r, held[r]);
+                    for (int r = 0; r < kChunks; ++r)
+                        if (kChunks < 4 || 32 * r < rank32) weights(32 * r, held[r]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {  // rows: tokens 16 u .. + 15, four tiles of elements; columns: elements 4 (0 .. 15) + u, four tiles of tokens
                 if (u < 3) get(block, u + 1, raw[(u + 1) % 2]);
@@ -801,7 +810,8 @@ __global__ __launch_bounds__(kBlock, 4) void expand_wide_kernel(ExpandArgs c) {
                 if (rank > 0) {
                     if constexpr (kChunks) {
 #pragma unroll
-                        for (int r = 0; r < kChunks; ++r) chunk(32 * r, held[r]);
+                        for (int r = 0; r < kChunks; ++r)
+                            if (kChunks < 4 || 32 * r < rank32) chunk(32 * r, held[r]);
                     } else {
 #pragma unroll 1
                         for (int r0 = 0; r0 < rank; r0 += 32) {
@@ -1193,8 +1203,8 @@ template <class TX, class TW, bool kColumns, bool kAlong>
 int expand_tiles(ExpandArgs c, hipStream_t s) {
     const int64_t blocks = (c.length + 63) / 64;
     const size_t few = (size_t)16 * ((c.w.rank + 15) / 16 * 16 + 4) * 4;
-    // ranks in eights: a load takes eight of a row and must not leave it
-    if (c.tokens <= kFewTokens || c.length < 64 || c.w.rank % 8) {
+    // ranks in fours: a load takes four of a row, or four rows, and must not leave them
+    if (c.tokens <= kFewTokens || c.length < 64 || c.w.rank % 4) {
         const int64_t across = (c.tokens + 15) / 16;
         const dim3 grid((unsigned)across, (unsigned)blocks);
         // sixteen waves for up to sixteen adapters, where that many workgroups run together; else eight
@@ -1207,9 +1217,12 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
         c.groups = (uint32_t)((whole + c.blocks - 1) / c.blocks);
         const int64_t ends = (c.tokens % 64 + 15) / 16 * blocks + (c.length % 64 ? across * 4 : 0);
         const size_t lds = std::max(few, (size_t)(sizeof(TX) == 4 ? 3 : 2) * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
-        constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1;  // times 32 ranks, in registers
+        // An adapter's weights stay in registers for a block's 64 tokens where they are few; ranks over 64 in half as many waves then, which
+        // pays in rows (4096 tokens of 64 features -> 4096, rank 128, 8 requests: 52 -> 40 us) and not in columns (rank 128, one: 65 -> 70).
+        constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1, kRows = !kColumns && kWeightPieces<TW> == 1 ? 4 : kMost;  // times 32 ranks
         const auto kernel = c.w.rank <= 32           ? expand_wide_kernel<TX, TW, kColumns, kAlong, 1>
                             : c.w.rank <= 32 * kMost ? expand_wide_kernel<TX, TW, kColumns, kAlong, kMost>
+                            : c.w.rank <= 32 * kRows ? expand_wide_kernel<TX, TW, kColumns, kAlong, kRows>
                                                      : expand_wide_kernel<TX, TW, kColumns, kAlong, 0>;
         if (lds > 60 * 1024)  // ranks over 160 in 32 bits
             if (int e = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;

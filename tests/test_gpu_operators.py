@@ -243,7 +243,8 @@ ADAPTER_SHAPES = [(1, 64, 64, 1, 16, "last"), (1, 257, 131, 3, 5, "last"), (2, 1
                   (1100, 40, 72, 2, 130, "runs"), (2100, 64, 40, 3, 8, "any"), (40, 300, 80, 2, 256, "runs")]
 #: many tokens: whole and broken tiles of 64 by 64, ranks in eights and not, more adapters in a tile than are taken together
 WIDE_SHAPES = [(320, 256, 128, 4, 16, "runs"), (513, 200, 193, 3, 24, "any"), (449, 640, 330, 6, 40, "runs"), (385, 129, 257, 5, 64, "any"), (300, 65, 200, 2, 72, "runs"), (640, 320, 64, 1, 128, "last"),
-               (260, 140, 150, 2, 200, "runs"), (333, 90, 100, 3, 36, "any"), (700, 1100, 70, 90, 8, "any")]
+               (260, 140, 150, 2, 200, "runs"), (333, 90, 100, 3, 36, "any"), (700, 1100, 70, 90, 8, "any"),
+               (400, 130, 192, 3, 4, "runs"), (330, 192, 130, 2, 12, "runs"), (350, 100, 128, 2, 100, "runs")]
 
 
 def make_adapters(shape, types, ragged):
