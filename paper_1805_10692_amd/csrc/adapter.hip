@@ -506,7 +506,6 @@ struct ExpandArgs {
 // memory in base and y.  `room`: LDS of 16 * (the rank's next multiple of 16, + 4) floats.
 template <class TX, class TW, bool kColumns, bool kAlong, int kThreads>
 __device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int64_t o0, Present& present, float* room) {
-    constexpr int kSplit = kThreads / 256;  // threads for a token and rank: neighbours
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int rank16 = (c.w.rank + 15) / 16 * 16, pitch = rank16 + 4;
     const int left = (int)std::min<int64_t>(c.length - o0, 64), tokens_left = (int)std::min<int64_t>(c.tokens - t0, 16);
@@ -531,29 +530,38 @@ __device__ __forceinline__ void expand_some(const ExpandArgs& c, int64_t t0, int
             }
         }
     }
-    const int t_own = threadIdx.x / (16 * kSplit), split = threadIdx.x % kSplit;
+    // a token has kThreads / 16 threads: up to sixteen for its ranks, in fours, each as neighbours that share the parts
+    constexpr int kToken = kThreads / 16;
+    const int fours = rank16 <= 16 ? 4 : rank16 <= 32 ? 8 : 16, splits = kToken / fours;
+    const int t_own = threadIdx.x / kToken, split = threadIdx.x % splits, r_own = threadIdx.x % kToken / splits * 4;
     auto sum_of = [&](int r) {
-        float sum = 0.f;
+        F4 sum = 0.f;
         if (t_own < tokens_left && r < c.w.rank) {
             const float* p = c.part + (t0 + t_own) * c.w.rank + r;
-#pragma unroll 8
-            for (uint32_t k = split; k < c.parts; k += kSplit) sum += p[k * c.tokens * c.w.rank];
+            if (r + 4 <= c.w.rank)
+#pragma unroll 4
+                for (uint32_t k = split; k < c.parts; k += splits) sum += load<float, 4>(p + k * c.tokens * c.w.rank);
+            else
+                for (uint32_t k = split; k < c.parts; k += splits) sum += load_some<float, 4>(p + k * c.tokens * c.w.rank, c.w.rank - r);
         }
+        for (int k = 1; k < splits; k *= 2)
 #pragma unroll
-        for (int k = 1; k < kSplit; k *= 2) sum += __shfl_xor(sum, k);
+            for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], k);
         return sum;
     };
-    const int r_own = threadIdx.x / kSplit % 16;
-    const float early = sum_of(r_own);
+    const F4 early = sum_of(r_own);
     list_adapters(present, c.index, t0, 16, c.tokens, c.w.adapters);
     {  // 0 past the rank and for tokens without an adapter
         const int a = present.adapter[t_own];
         const float scale = a < 0 ? 0.f : c.scale ? scale_of(c.w, a) : 1.f;
-        for (int r = r_own; r < rank16; r += 16) {
-            const float sum = r < 16 ? early : sum_of(r);
+        for (int r = r_own; r < rank16; r += 4 * fours) {
+            const F4 sum = r < 4 * fours ? early : sum_of(r);
             if (split) continue;
-            if (c.hidden && o0 == 0 && t_own < tokens_left && r < c.w.rank) c.hidden[(t0 + t_own) * c.w.rank + r] = sum;
-            room[t_own * pitch + r] = sum * scale;
+            if (c.hidden && o0 == 0 && t_own < tokens_left)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (r + e < c.w.rank) c.hidden[(t0 + t_own) * c.w.rank + r + e] = sum[e];
+            *reinterpret_cast<F4*>(&room[t_own * pitch + r]) = sum * scale;
         }
     }
     __syncthreads();
@@ -1161,7 +1169,9 @@ struct ShrinkShape {
     ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns, int64_t adapters) {
         ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
         tiles = tokens <= kFewTokens || (columns && ranks == 8) ? 1 : 4;
-        const int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
+        int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
+        // Few tokens: workgroups for sixteen ranks each, while that leaves the long axis at least eight parts; the sum of fewer parts is less to read.
+        for (; tokens <= kFewTokens && ranks > 1 && blocks <= 16; ranks /= 2) blocks *= 2;
         // few tokens: a workgroup for a compute unit, and no stretch of the long axis of less than 128 elements, or less than 32 for a wave where the
         // sixteen waves have up to so many adapters abreast
         const int64_t abreast = std::min<int64_t>({16, tokens, adapters});
