@@ -575,7 +575,7 @@ int adapter_backward(const cer_adapters_t* w, const int32_t* index, int64_t toke
  * min(1, max_norm / (norm + 1e-6)) . grad for every one of them.  Each tensor is contiguous, fp32, bf16 or fp16, of any length from 0; out
  * has its type and may be grad itself (then nothing is written where the factor is 1).  A NaN or an infinity in any of them makes
  * the norm NaN or infinite, and the factor NaN or 0.  `grads` is a host array, read during the call; max_norm >= 0.
- * A temporary of 8 KiB per 120 tensors.
+ * A temporary of 16 KiB per 120 tensors.
  */
 typedef struct {
     const void* grad;

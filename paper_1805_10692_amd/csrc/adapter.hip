@@ -33,6 +33,8 @@ template <int kTiles>
 constexpr int kShrinkThreads = kTiles == 1 ? 1024 : 512;
 constexpr int kOuterBlock = 256, kRowsBlock = 512;
 constexpr int kMostTile = 64;  // tokens of a workgroup
+// Up to so many tokens the kernels for 16 of them run, tiles of 64 would be too few for the chip.  4096 -> 4096 features, these kernels against those:
+// 320 tokens of 8 requests, columns, rank 16: 21.5 and 31.7 us, of one request, bf16, rank 64: 27.4 and 19.8; 512 tokens: 26.4 and 18.0, 36.1 and 19.0.
 constexpr int64_t kFewTokens = 256;
 
 // One side's weights: element (long axis k, rank r) of adapter a at w[a * stride + (kAlong ? r * ld + k : k * ld + r)].
@@ -1168,9 +1170,12 @@ struct ShrinkShape {
     int64_t part;
     ShrinkShape(int64_t tokens, int64_t rank, int64_t length, bool columns, int64_t adapters) {
         ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
+        // columns, ranks over 64: 128 of them take all of a wave's registers with 16 tokens; 64 tokens and x twice took longer (4096 tokens of 4096
+        // features, rank 128: 95 -> 131 us, both launches)
         tiles = tokens <= kFewTokens || (columns && ranks == 8) ? 1 : 4;
         int64_t blocks = (tokens + 16 * tiles - 1) / (16 * tiles);
-        // Few tokens: workgroups for sixteen ranks each, while that leaves the long axis at least eight parts; the sum of fewer parts is less to read.
+        // Few tokens: workgroups for sixteen ranks each, while that leaves the long axis at least eight parts: more of them, and fewer parts for
+        // `expand` to add up (one token, 4096 features, rank 64: 7.7 -> 4.9 us and 8.7 -> 7.5; 64 tokens: 7.4 -> 5.0 and 14.2 -> 10.0).
         for (; tokens <= kFewTokens && ranks > 1 && blocks <= 16; ranks /= 2) blocks *= 2;
         // few tokens: a workgroup for a compute unit, and no stretch of the long axis of less than 128 elements, or less than 32 for a wave where the
         // sixteen waves have up to so many adapters abreast
@@ -1186,9 +1191,12 @@ struct ShrinkShape {
 template <class TX, class TW, bool kColumns, bool kAlong, int kRanks>
 void shrink_tiles(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
     const dim3 grid((unsigned)((c.tokens + 16 * f.tiles - 1) / (16 * f.tiles) * f.parts), 1, (unsigned)((c.w.rank + 16 * kRanks - 1) / (16 * kRanks)));
-    if (f.tiles == 1) shrink_kernel<TX, TW, kColumns, kAlong, 1, kRanks><<<grid, kShrinkThreads<1>, 0, s>>>(c);
-    else if constexpr (!kColumns) shrink_rows_kernel<TX, TW, kAlong, kRanks><<<grid, kRowsBlock, 0, s>>>(c);
-    else if constexpr (kRanks < 8) shrink_kernel<TX, TW, kColumns, kAlong, 4, kRanks><<<grid, kShrinkThreads<4>, 0, s>>>(c);
+    if (f.tiles == 4) {
+        if constexpr (!kColumns) shrink_rows_kernel<TX, TW, kAlong, kRanks><<<grid, kRowsBlock, 0, s>>>(c);
+        else if constexpr (kRanks < 8) shrink_kernel<TX, TW, kColumns, kAlong, 4, kRanks><<<grid, kShrinkThreads<4>, 0, s>>>(c);
+    } else if constexpr (kColumns || kRanks < 8) {  // ShrinkShape: few tokens have no eight
+        shrink_kernel<TX, TW, kColumns, kAlong, 1, kRanks><<<grid, kShrinkThreads<1>, 0, s>>>(c);
+    }
 }
 template <class TX, class TW, bool kColumns, bool kAlong>
 int shrink_ranks(const ShrinkArgs& c, const ShrinkShape& f, hipStream_t s) {
