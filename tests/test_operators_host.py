@@ -153,3 +153,16 @@ def test_clip_refusals():
         assert call([good], max_norm=most) == B.CER_E_INVALID
     assert call([good], norm=0) == B.CER_E_INVALID
     assert call([Gradient(AT, AT, 1 << 50, F32)]) == B.CER_E_TOO_LARGE
+
+
+@pytest.mark.parametrize("where", ["tokens", "ld_a", "ld_b", "x", "y", "base"])
+def test_adapter_sizes_past_the_kernels_offsets(where):
+    """Offsets inside a tile of 64 tokens have 32 bits, and so has a grid: what could pass them is refused before a launch."""
+    L, most = B.lib(), 1 << 22
+
+    def call(n_tokens=3, ld_a=8, ld_b=4, x=8, y=6, base=6):
+        X, Y, base = tokens(ld=x), tokens(ld=y, at=4 * AT), tokens(ld=base, at=8 * AT)
+        w = adapters(ld_a=ld_a, ld_b=ld_b, stride_a=max(32, 4 * ld_a), stride_b=max(24, 6 * ld_b))
+        return L.adapter_matmul(ctypes.byref(w), ctypes.c_void_p(AT), ctypes.c_int64(n_tokens), ctypes.byref(X), ctypes.byref(base), ctypes.byref(Y), None, None, ctypes.c_int64(0), None)
+
+    assert call(**{"n_tokens" if where == "tokens" else where: (1 << 24) + 1 if where == "tokens" else most + 1}) == B.CER_E_TOO_LARGE
