@@ -26,7 +26,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "operators.hpp"
+#include "adapter_weights.hpp"
 
 namespace cer {
 namespace {
@@ -95,19 +95,6 @@ __device__ __forceinline__ void list_adapters(Present& p, const int32_t* index, 
 __device__ __forceinline__ F4 product(float a, float b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ F4 product(Vec<__bf16, 8> a, Vec<__bf16, 8> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ F4 product(Vec<_Float16, 8> a, Vec<_Float16, 8> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
-// Elements at a wave's own address (a scalar) and a lane's offset in bytes from it.
-template <class T>
-__device__ __forceinline__ const T* at(const T* base, uint32_t bytes) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
-template <class T>
-__device__ __forceinline__ T* at(T* base, uint32_t bytes) { return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes); }
-
-// The same offset, as a number of its own: sums with it are made where they stand, as a scalar and an offset that the load adds up, and not kept in two registers each
-// through the loops around them (32 of those: 64 registers).
-__device__ __forceinline__ uint32_t here(uint32_t bytes) {
-    asm volatile("" : "+v"(bytes));
-    return bytes;
-}
 
 // Workgroup n of `all` as neighbours want it: the eight XCDs take workgroups in turn and have an L2 each, so that an eighth of the work items, one after the
 // other, goes to each: neighbouring tokens mostly have the same adapter, and its weights then come into one L2 or two and not into all of them.
@@ -758,38 +745,11 @@ __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kern
             const int a = q < slots ? __builtin_amdgcn_readfirstlane(present.slot[q]) : -1;
             const int rank = a >= 0 ? rank_of(c.w, a) : 0;
             const TW* w = static_cast<const TW*>(c.w.w) + (a >= 0 ? a * c.w.stride : 0) + (kAlong ? o0 : o0 * c.w.ld);
-            // Past the rank: 0, whatever is there.  Lanes whose ranks are past the rows' end read the first ones again.
             auto weights = [&](int r0, Pieces8 (&ws)[4][kW]) {
-                const int low = r0 + 8 * g;
-                auto place = [&](int r) { return here(w_lane) + (uint32_t)(r < c.w.rank ? kAlong ? r * c.w.ld : r : 0) * sizeof(TW); };
                 Vec<TW, 8> u[4];
-                if constexpr (kAlong) {  // w[r * ld + o]; the rows' number is a multiple of four
-                    const uint32_t first = place(low), second = place(low + 4);
+                weights_of<TW, kAlong>(w, w_lane, c.w.ld, rank, r0 + 8 * g, u);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const Vec<TW, 4> v = load<TW, 4>(at(w + e % 4 * c.w.ld, e < 4 ? first : second));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) u[j][e] = v[j];
-                    }
-                } else if (c.w.rank % 8 == 0) {
-                    const uint32_t first = place(low);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) u[j] = load<TW, 8>(at(w + j * c.w.ld, first));
-                } else {
-                    const uint32_t first = place(low), second = place(low + 4);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        u[j] = __builtin_shufflevector(load<TW, 4>(at(w + j * c.w.ld, first)), load<TW, 4>(at(w + j * c.w.ld, second)), 0, 1, 2, 3, 4, 5, 6, 7);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (rank % 8)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) u[j][e] = low + e < rank ? u[j][e] : (TW)0.f;
-                    else if (low >= rank)
-                        u[j] = (TW)0.f;
-                    weight_operands<TW>(u[j], ws[j]);
-                }
+                for (int j = 0; j < 4; ++j) weight_operands<TW>(u[j], ws[j]);
             };
             auto operand = [&](int k, int t, int r0) { return *reinterpret_cast<const Pieces8*>(&planes[(k * kTile + t) * pitch + r0 + 8 * g]); };
             Pieces8 held[kHeld][4][kW];

@@ -88,7 +88,7 @@ struct Packed {
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 template <class T, int N>
-__device__ __forceinline__ Vec<T, N> load(const T* p) {
+__host__ __device__ __forceinline__ Vec<T, N> load(const T* p) {
     return *reinterpret_cast<const typename Packed<T, N>::type*>(p);
 }
 template <class T, int N>
@@ -129,7 +129,7 @@ __device__ __forceinline__ void store_some(T* p, Vec<float, N> v, int64_t left) 
 }
 // As they are in memory.
 template <class T, int N>
-__device__ __forceinline__ Vec<T, N> load_own(const T* p, int64_t left) {
+__host__ __device__ __forceinline__ Vec<T, N> load_own(const T* p, int64_t left) {
     if (left >= N) return load<T, N>(p);
     Vec<T, N> v;
 #pragma unroll
