@@ -651,14 +651,14 @@ __device__ __forceinline__ void weight_operands(const Vec<TW, 8> v, Pieces8 (&ou
 
 // 64 tokens.  A wave takes 64 elements of the long axis at a time, with what base has there in registers, and goes through the adapters, each
 // one's weights (ranks up to kChunks * 32; 0: any, loaded again for every tile of 16 tokens) in registers.  Element o0 + 4 i + j is row (column) i of
-// tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as bf16 pieces by the weights' pieces in the 16-bit instruction, at an
-// eighth to a fifth of the 32-bit one's time: three pieces where y has 32 bits, two where it has 16 (2^-16 of hidden, an eighth of half a
-// step of y in fp16); products of pieces that are together below that are left out.
+// tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as three bf16 pieces by the weights' one (bf16), two
+// (fp16) or three in the 16-bit instruction, at a fifth to a half of the 32-bit one's time.  The pieces are cut from the number, so that the second is below 2^-7 of it, the third below
+// 2^-14, and three hold all its bits: only the product of both third ones is left out, 2^-28 of a product.
 // Base and y of 8192 x 4096 bf16, rank 64: 49 us, 2.7 TB/s; of 3136 x 4096 fp32 columns, rank 16: 34 us, 3.0 TB/s; with the 32-bit instruction, which takes its 16
 // rows of y from memory one line a lane, 201 and 66.
 template <class TX, class TW, bool kColumns, bool kAlong, int kChunks>
 __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kernel(ExpandArgs c) {
-    constexpr int kTile = 64, kH = sizeof(TX) == 4 ? 3 : 2, kW = kWeightPieces<TW>, kHeld = kChunks ? kChunks : 1;
+    constexpr int kTile = 64, kH = 3, kW = kWeightPieces<TW>, kHeld = kChunks ? kChunks : 1;
     extern __shared__ float room[];
     __shared__ Present present;
     // the last workgroups take what the tiles of 64 by 64 leave: the last tokens, and the end of the long axis of the others
@@ -773,15 +773,15 @@ __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kern
                     for (int e = 0; e < 4; ++e) acc[v][e] = (float)raw[u % 2][e][v];
                 auto chunk = [&](int r0, const Pieces8 (&ws)[4][kW]) {
 #pragma unroll
-                    for (int k = 0; k < kH; ++k) {
+                    for (int k = kH - 1; k >= 0; --k) {  // the largest product last: the roundings of the sums before it are small (the order of the others: registers)
                         Pieces8 h;
                         if constexpr (!kColumns) h = operand(k, 16 * u + i, r0);
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
                             if constexpr (kColumns) h = operand(k, 4 * i + v, r0);
 #pragma unroll
-                            for (int l = 0; l < kW; ++l)
-                                if (k + l < kH) acc[v] = kColumns ? product(ws[u][l], h, acc[v]) : product(h, ws[v][l], acc[v]);
+                            for (int m = 0; m < kW; ++m)
+                                if (const int l = k ? m : kW - 1 - m; k + l < 4) acc[v] = kColumns ? product(ws[u][l], h, acc[v]) : product(h, ws[v][l], acc[v]);
                         }
                     }
                 };
@@ -1204,7 +1204,7 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
         c.blocks = (uint32_t)std::max<int64_t>(kWaves, (whole + most - 1) / most);
         c.groups = (uint32_t)((whole + c.blocks - 1) / c.blocks);
         const int64_t ends = (c.tokens % 64 + 15) / 16 * blocks + (c.length % 64 ? across * 4 : 0);
-        const size_t lds = std::max(few, (size_t)(sizeof(TX) == 4 ? 3 : 2) * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
+        const size_t lds = std::max(few, (size_t)3 * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
         // An adapter's weights stay in registers for a block's 64 tokens where they are few; ranks over 64 in half as many waves then, which
         // pays in rows (4096 tokens of 64 features -> 4096, rank 128, 8 requests: 52 -> 40 us) and not in columns (rank 128, one: 65 -> 70).
         constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1, kRows = !kColumns && kWeightPieces<TW> == 1 ? 4 : kMost;  // times 32 ranks
@@ -1212,7 +1212,7 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
                             : c.w.rank <= 32 * kMost ? expand_wide_kernel<TX, TW, kColumns, kAlong, kMost>
                             : c.w.rank <= 32 * kRows ? expand_wide_kernel<TX, TW, kColumns, kAlong, kRows>
                                                      : expand_wide_kernel<TX, TW, kColumns, kAlong, 0>;
-        if (lds > 60 * 1024)  // ranks over 160 in 32 bits
+        if (lds > 60 * 1024)  // ranks over 128
             if (int e = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
         kernel<<<(unsigned)(across * c.groups + ends), kBlock, lds, s>>>(c);
     }

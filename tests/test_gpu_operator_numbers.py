@@ -1,0 +1,75 @@
+"""What the operators beside a projection compute where it shows: single products of full 32-bit numbers, outputs in which base cancels nearly everything,
+infinities, ranks that are an adapter's own.  Every kernel that a call may be given to is asked: up to 256 tokens and over them, rows and columns, all types.
+
+The oracle and the bounds are those of test_gpu_operators.py."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1805_10692_amd import binding as B
+from test_gpu_operators import ADAPTER_TYPES, BF16, F16, F32, NAN, U, adapters_oracle, backward_oracle, host, index_of, near, on_gpu, put, rand, room_for, stored
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+types_id = lambda t: f"{t[0]}-{t[1]}-{int(t[2])}".replace("torch.", "")  # noqa: E731
+TYPES = pytest.mark.parametrize("types", ADAPTER_TYPES, ids=types_id)
+TOKENS = pytest.mark.parametrize("tokens", [200, 330])
+
+
+def short(x, bits):
+    """Numbers of so many significant bits: a product of two of 12 is exact in 32."""
+    m, e = torch.frexp(x)
+    return torch.ldexp(torch.round(m * 2 ** bits), e - bits)
+
+
+# ---- bits of `expand` ---------------------------------------------------------------------------------------------------------------
+@TOKENS
+@TYPES
+@pytest.mark.parametrize("few", [1, 3])
+@pytest.mark.parametrize("back", [False, True], ids=["y", "dx"])
+def test_base_cancels_the_adapter(tokens, types, back, few):
+    """One feature on the short side makes hidden (d) exact, a few make it a number of all bits, off by few - 1 additions, and base takes away what is added to
+    it but for its own rounding: R products and base are R + 1 additions, and their pieces, if a kernel has such, some more of a hundredth of the size."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens)
+    R, long, N = 4, 130, 3
+    index = index_of("runs", tokens, N, 7)
+    one, wide = short(rand(gen, N, R, few), 12).to(tw).double(), rand(gen, N, long, R).to(tw).double()
+    v = short(rand(gen, tokens, few), 12).to(ta).double()
+    A, Bm = (wide.transpose(1, 2), one.transpose(1, 2)) if back else (one, wide)
+    whole, _, size = adapters_oracle(one, wide, None, None, index, v, None)
+    base = (-whole).to(ta).double()
+    want, size = base + whole, size + base.abs()
+    Y, Bs = room_for(tokens, long, ta, columns), put(base, ta, columns)
+    GA, GB, I, V = A.contiguous().to(tw).cuda(), Bm.contiguous().to(tw).cuda(), index.cuda(), put(v, ta, columns)
+    if back:
+        X, H = put(rand(gen, tokens, long), ta, columns), torch.zeros((tokens, R), device="cuda")
+        B.adapter_backward(GA, GB, I, V, X, H, base=Bs, dX=Y)
+    else:
+        B.adapter_matmul(GA, GB, I, V, Y, base=Bs)
+    near(Y, want, stored(want, ta, (R + 1 + few) * U * size), "y")
+
+
+@TOKENS
+@pytest.mark.parametrize("types", [t for t in ADAPTER_TYPES if t[0] == F32], ids=types_id)
+@pytest.mark.parametrize("back", [False, True], ids=["y", "dx"])
+def test_single_products_in_32_bits(tokens, types, back):
+    """Each output is one product of two numbers of all their bits: its own rounding, 2^-23, and additions of pieces below 2^-6 of it (7 . 2^-29 and less)."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 1)
+    long, N = 130, 3
+    index, ranks = index_of("runs", tokens, N, 8), torch.ones(N, dtype=torch.int32)
+    one, wide = torch.zeros((N, 4, 1)), torch.full((N, long, 4), NAN)  # three ranks that nobody has
+    one[:, :1], wide[:, :, :1] = short(rand(gen, N, 1, 1), 12), rand(gen, N, long, 1)
+    one, wide = one.to(tw).double(), wide.to(tw).double()
+    v = short(rand(gen, tokens, 1), 12).to(ta).double()
+    A, Bm = (wide.transpose(1, 2), one.transpose(1, 2)) if back else (one, wide)
+    want, _, _ = adapters_oracle(one, wide, None, ranks, index, v, None)
+    Y = room_for(tokens, long, ta, columns)
+    GA, GB, I, V = A.contiguous().to(tw).cuda(), Bm.contiguous().to(tw).cuda(), index.cuda(), put(v, ta, columns)
+    if back:
+        X, H = put(rand(gen, tokens, long), ta, columns), torch.zeros((tokens, 4), device="cuda")
+        B.adapter_backward(GA, GB, I, V, X, H, ranks=ranks.cuda(), dX=Y)
+    else:
+        B.adapter_matmul(GA, GB, I, V, Y, ranks=ranks.cuda())
+    near(Y, want, 1.25 * U * want.abs(), "y")
