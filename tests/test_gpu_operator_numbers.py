@@ -73,3 +73,21 @@ def test_single_products_in_32_bits(tokens, types, back):
     else:
         B.adapter_matmul(GA, GB, I, V, Y, ranks=ranks.cuda())
     near(Y, want, 1.25 * U * want.abs(), "y")
+
+
+# ---- bits of the outer products -------------------------------------------------------------------------------------------------------
+@TOKENS
+@TYPES
+def test_single_outer_products_in_32_bits(tokens, types):
+    """An adapter of its own for every token: each element of dA and dB is one product of two numbers of all their bits, bound as above."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 2)
+    R, n = 4, 70
+    index = torch.randperm(tokens, generator=gen).to(torch.int32)
+    A, Bm = rand(gen, tokens, R, n).to(tw).double(), short(rand(gen, tokens, 1, R), 12).to(tw).double()
+    x, dy, hidden = rand(gen, tokens, n).to(ta).double(), short(rand(gen, tokens, 1), 12).to(ta).double(), rand(gen, tokens, R).double()
+    _, _, dA, _, dB, _ = backward_oracle(A, Bm, None, None, index, dy, x, hidden, None)
+    GdA, GdB = torch.empty((tokens, R, n), device="cuda"), torch.empty((tokens, 1, R), device="cuda")
+    B.adapter_backward(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(dy, ta, columns), put(x, ta, columns), hidden.float().cuda(), dA=GdA, dB=GdB)
+    near(GdA, dA, 1.25 * U * dA.abs(), "dA")
+    near(GdB, dB, 1.25 * U * dB.abs(), "dB")
