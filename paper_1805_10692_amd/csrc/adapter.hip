@@ -613,16 +613,18 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs c) {
 
 // ---- expand, many tokens --------------------------------------------------------------------------------------------------------
 // A number as bf16 pieces that add up to it, the high bits first: each is cut (the last one rounded), so that none of them is larger
-// than the number and three hold all 24 bits of it down to 2^-133.  Infinities and NaN are their first piece alone.
+// than the number and three hold all 24 bits of it down to 2^-133.  Where the first ones hold all of it the others are 2^-60 of it and not 0: an infinity
+// or NaN on the other side makes the same of each piece, and an infinity's pieces are infinities, as the product of the numbers is.
 template <int kPieces>
 __device__ __forceinline__ void pieces_of(float x, uint16_t (&p)[kPieces]) {
+    const float least = x * 0x1p-60f;
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         if (k + 1 < kPieces) {
             const uint32_t high = x == x ? __float_as_uint(x) & 0xFFFF0000u : 0x7FC00000u;
             p[k] = (uint16_t)(high >> 16);
-            x -= __uint_as_float(high);
-            x = x == x ? x : 0.f;
+            const float rest = x - __uint_as_float(high);
+            x = fabsf(rest) > 0.f ? rest : least;
         } else {
             p[k] = __builtin_bit_cast(uint16_t, (__bf16)x);
         }

@@ -91,3 +91,86 @@ def test_single_outer_products_in_32_bits(tokens, types):
     B.adapter_backward(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(dy, ta, columns), put(x, ta, columns), hidden.float().cuda(), dA=GdA, dB=GdB)
     near(GdA, dA, 1.25 * U * dA.abs(), "dA")
     near(GdB, dB, 1.25 * U * dB.abs(), "dB")
+
+
+# ---- infinities -----------------------------------------------------------------------------------------------------------------------
+def same(got, want, what=""):
+    """Infinities of the same sign in the same places, and NaN in the same places."""
+    got = host(got)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    assert torch.equal(torch.where(torch.isinf(got), got, 0.0), torch.where(torch.isinf(want), want, 0.0)), what
+
+
+def powers(gen, *shape):
+    """Of two, of either sign: one piece of any of the kernels' makes them up."""
+    return torch.ldexp(torch.randint(0, 2, shape, generator=gen) * 2.0 - 1, torch.randint(-2, 3, shape, generator=gen)).double()
+
+
+@TOKENS
+@TYPES
+@pytest.mark.parametrize("where", ["x", "A", "B", "base"])
+def test_infinities_forward(tokens, types, where):
+    """One rank, so that an infinity meets one other number, which is not 0: an infinity of the product's sign, in the token and feature that have it."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 3)
+    N, R, n, m = 3, 4, 3, 130
+    index, ranks = index_of("runs", tokens, N, 9), torch.ones(N, dtype=torch.int32)
+    A, Bm, x, base = powers(gen, N, R, n), powers(gen, N, m, R), powers(gen, tokens, n), powers(gen, tokens, m)
+    if where == "x":
+        x[::7, 1], x[3::7, 2] = INF, -INF
+    elif where == "A":
+        A[1, :, 0] = INF
+    elif where == "B":
+        Bm[0, ::5], Bm[2, 3::64] = -INF, INF
+    else:
+        base[::3, ::4] = -INF
+    want, _, _ = adapters_oracle(A, Bm, None, ranks, index, x, base)
+    Y = room_for(tokens, m, ta, columns)
+    B.adapter_matmul(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(x, ta, columns), Y, ranks=ranks.cuda(), base=put(base, ta, columns))
+    same(Y, want, where)
+
+
+@TOKENS
+@TYPES
+@pytest.mark.parametrize("where", ["x", "dy", "hidden", "A", "B"])
+def test_infinities_backward(tokens, types, where):
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 4)
+    N, R, n, m = 5, 4, 140, 2
+    index, ranks = index_of("runs", tokens, N, 10), torch.ones(N, dtype=torch.int32)
+    A, Bm, x, dy, hidden = powers(gen, N, R, n), powers(gen, N, m, R), powers(gen, tokens, n), powers(gen, tokens, m), powers(gen, tokens, R)
+    if where == "x":
+        x[5, ::3], x[tokens - 9, 1::3] = INF, -INF
+    elif where == "dy":
+        dy[tokens // 2, 0] = INF
+    elif where == "hidden":
+        hidden[11], hidden[tokens - 4] = -INF, INF
+    elif where == "A":
+        A[:, :, ::9] = INF
+    else:
+        Bm[2, 1] = -INF
+    dx, _, dA, _, dB, _ = backward_oracle(A, Bm, None, ranks, index, dy, x, hidden, None)
+    DX, GdA, GdB = room_for(tokens, n, ta, columns), torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
+    B.adapter_backward(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(dy, ta, columns), put(x, ta, columns), hidden.float().cuda(), ranks=ranks.cuda(), dX=DX, dA=GdA, dB=GdB)
+    same(DX, dx, "dx")
+    same(GdA[:, :1], dA[:, :1], "dA")
+    same(GdB[:, :, :1], dB[:, :, :1], "dB")
+
+
+@TOKENS
+@TYPES
+def test_infinities_beside_full_numbers(tokens, types):
+    """Sums that hold an infinity and others, of weights and activations of all their bits: what is finite beside them keeps its bound."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 5)
+    N, R, n, m = 3, 36, 70, 200
+    index = index_of("runs", tokens, N, 11)
+    A, Bm, x, base = rand(gen, N, R, n).to(tw).double(), rand(gen, N, m, R).to(tw).double(), rand(gen, tokens, n).to(ta).double(), rand(gen, tokens, m).to(ta).double()
+    base[::5, ::7] = INF
+    Bm[1, 17], Bm[2, 150, 3] = INF, -INF
+    x[4] = NAN
+    want, _, size = adapters_oracle(A, Bm, None, None, index, x, base)
+    Y = room_for(tokens, m, ta, columns)
+    B.adapter_matmul(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(x, ta, columns), Y, base=put(base, ta, columns))
+    same(Y, want, "y")
+    near(Y, want, stored(want, ta, (n + R + 8) * U * size), "y")
