@@ -894,6 +894,16 @@ __device__ __forceinline__ void add_waves(F4 (&acc)[kSums], F4 (*room)[kSums][64
     }
 }
 
+// Gradients of ranks at .. at + 3, `some` registers of them from `first` on: 0 past the adapter's rank, where 0 has been multiplied by whatever the
+// tokens hold, an infinity or a NaN too.
+template <int kSums>
+__device__ __forceinline__ void past_rank(F4 (&acc)[kSums], int first, int some, int at, int rank) {
+#pragma unroll
+    for (int j = 0; j < some; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[first + j][e] = at + e < rank ? acc[first + j][e] : 0.f;
+}
+
 // Adapter blockIdx.y, 64 elements of the long axis, kRanks * 16 ranks; the waves share out the groups of 16 tokens in which the adapter occurs.
 // 999 tokens, 2048 -> 4608, rank 8, 4 adapters, columns: 15 us, the adapter's tokens and then their x and d one after the other.
 template <class TX, bool kColumns, int kRanks>
@@ -970,6 +980,7 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
 #pragma unroll
     for (int r = 0; r < kRanks; ++r) {
         const int at = r0 + 16 * r + 4 * g;
+        past_rank(acc, 4 * r, 4, at, rank);
         if (c.rank_last) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -1074,7 +1085,7 @@ __global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterPair pair)
 #pragma unroll
     for (int r = 0; r < kRanks; ++r) {
         const int at = 16 * (tile0 + r) + 4 * g;
-        // a rank past the adapter's own: the planes have 0 there
+        past_rank(acc, r * kCols, kCols, at, rank);
         if (c.rank_last) {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)

@@ -174,3 +174,21 @@ def test_infinities_beside_full_numbers(tokens, types):
     B.adapter_matmul(A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(x, ta, columns), Y, base=put(base, ta, columns))
     same(Y, want, "y")
     near(Y, want, stored(want, ta, (n + R + 8) * U * size), "y")
+
+
+# ---- ranks of an adapter's own, adapters that nobody has ------------------------------------------------------------------------------
+@TOKENS
+@TYPES
+def test_gradients_past_an_adapters_rank_are_zero(tokens, types):
+    """Also where the tokens' activations are infinite or NaN."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 6)
+    N, R, n, m = 4, 24, 70, 66
+    index, ranks = index_of("runs", tokens, N, 12), torch.tensor([5, 0, 17, 24], dtype=torch.int32)
+    A, Bm = rand(gen, N, R, n).to(tw), rand(gen, N, m, R).to(tw)
+    x, dy, hidden = rand(gen, tokens, n), rand(gen, tokens, m), rand(gen, tokens, R)
+    x[::9, ::2], x[1::9, 1::2], dy[::11, ::3], dy[3::11, 1::3] = INF, NAN, -INF, NAN
+    GdA, GdB = torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
+    B.adapter_backward(A.cuda(), Bm.cuda(), index.cuda(), put(dy, ta, columns), put(x, ta, columns), hidden.cuda(), ranks=ranks.cuda(), dA=GdA, dB=GdB)
+    for a, r in enumerate(ranks):
+        assert (host(GdA)[a, int(r):] == 0).all() and (host(GdB)[a, :, int(r):] == 0).all(), a
