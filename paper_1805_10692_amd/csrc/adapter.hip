@@ -923,8 +923,10 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
     F4 acc[kRanks * 4];  // [rank tile][j]
 #pragma unroll
     for (int r = 0; r < kRanks * 4; ++r) acc[r] = 0.f;
+    bool any = false;  // whether the adapter occurs
     for (int64_t first = from; first < to; first += kOuterBlock * 16) {
         const int groups = list_groups<16>(c.index, first, to, a, list, count);
+        any |= groups > 0;
         if (rank > r0)
             for (int q = wave; q < groups; q += kOuterBlock / 64) {
                 const int64_t t = first + list[q] * 16 + 4 * g;  // lane group g has tokens t .. t + 3
@@ -975,23 +977,25 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
     }
     add_waves(acc, room);
     if (wave) return;
-    const float scale = c.scale ? scale_of(c.w, a) : 1.f;
+    const float scale = c.scale && any ? scale_of(c.w, a) : 1.f;  // an adapter that nobody has gets 0 whatever its factor is
     float* out = c.out + ((int64_t)blockIdx.z * c.w.adapters + a) * c.w.rank * c.length;
 #pragma unroll
     for (int r = 0; r < kRanks; ++r) {
         const int at = r0 + 16 * r + 4 * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[4 * r + j] *= scale;
         past_rank(acc, 4 * r, 4, at, rank);
         if (c.rank_last) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (4 * i + j < left && at < c.w.rank) store_some<float, 4>(out + (o0 + 4 * i + j) * c.w.rank + at, acc[4 * r + j] * scale, c.w.rank - at);
+                if (4 * i + j < left && at < c.w.rank) store_some<float, 4>(out + (o0 + 4 * i + j) * c.w.rank + at, acc[4 * r + j], c.w.rank - at);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (at + k >= c.w.rank) continue;
                 F4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[4 * r + j][k] * scale;
+                for (int j = 0; j < 4; ++j) v[j] = acc[4 * r + j][k];
                 store_some<float, 4>(out + (at + k) * c.length + o0 + 4 * i, v, left - 4 * i);
             }
         }

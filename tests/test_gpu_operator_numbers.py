@@ -192,3 +192,23 @@ def test_gradients_past_an_adapters_rank_are_zero(tokens, types):
     B.adapter_backward(A.cuda(), Bm.cuda(), index.cuda(), put(dy, ta, columns), put(x, ta, columns), hidden.cuda(), ranks=ranks.cuda(), dA=GdA, dB=GdB)
     for a, r in enumerate(ranks):
         assert (host(GdA)[a, int(r):] == 0).all() and (host(GdB)[a, :, int(r):] == 0).all(), a
+
+
+@TOKENS
+@TYPES
+@pytest.mark.parametrize("factor", [NAN, INF])
+def test_factor_of_an_adapter_that_nobody_has(tokens, types, factor):
+    """A place in `scales` that was never written: the adapter's gradients are 0 all the same, and so are those of an adapter without ranks."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 7)
+    N, R, n, m = 4, 8, 70, 66
+    index = index_of("runs", tokens, 2, 13)
+    index[-3:] = 3
+    ranks, scales = torch.tensor([8, 5, 8, 0], dtype=torch.int32), torch.tensor([1.0, 0.5, factor, factor])
+    A, Bm = rand(gen, N, R, n).to(tw), rand(gen, N, m, R).to(tw)
+    GdA, GdB = torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
+    B.adapter_backward(A.cuda(), Bm.cuda(), index.cuda(), put(rand(gen, tokens, m), ta, columns), put(rand(gen, tokens, n), ta, columns), rand(gen, tokens, R).cuda(),
+                       scales=scales.cuda(), ranks=ranks.cuda(), dA=GdA, dB=GdB)
+    assert torch.isfinite(GdA).all() and torch.isfinite(GdB).all()
+    for a in (2, 3):
+        assert (GdA[a] == 0).all() and (GdB[a] == 0).all()
