@@ -613,18 +613,17 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs c) {
 
 // ---- expand, many tokens --------------------------------------------------------------------------------------------------------
 // A number as bf16 pieces that add up to it, the high bits first: each is cut (the last one rounded), so that none of them is larger
-// than the number and three hold all 24 bits of it down to 2^-133.  Where the first ones hold all of it the others are 2^-60 of it and not 0: an infinity
-// or NaN on the other side makes the same of each piece, and an infinity's pieces are infinities, as the product of the numbers is.
+// than the number and three hold all 24 bits of it down to 2^-133.  Infinities and NaN are their first piece alone; beside a piece that is 0 an infinity
+// gives NaN, so that sums of pieces' products that are not finite are formed again from whole numbers.
 template <int kPieces>
 __device__ __forceinline__ void pieces_of(float x, uint16_t (&p)[kPieces]) {
-    const float least = x * 0x1p-60f;
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         if (k + 1 < kPieces) {
             const uint32_t high = x == x ? __float_as_uint(x) & 0xFFFF0000u : 0x7FC00000u;
             p[k] = (uint16_t)(high >> 16);
-            const float rest = x - __uint_as_float(high);
-            x = fabsf(rest) > 0.f ? rest : least;
+            x -= __uint_as_float(high);
+            x = x == x ? x : 0.f;
         } else {
             p[k] = __builtin_bit_cast(uint16_t, (__bf16)x);
         }
@@ -760,6 +759,7 @@ __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kern
 #pragma unroll
                     for (int r = 0; r < kChunks; ++r)
                         if (kChunks < 4 || 32 * r < rank32) weights(32 * r, held[r]);
+            unsigned again = 0;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {  // rows: tokens 16 u .. + 15, four tiles of elements; columns: elements 4 (0 .. 15) + u, four tiles of tokens
                 if (u < 3) get(block, u + 1, raw[(u + 1) % 2]);
@@ -800,6 +800,19 @@ __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kern
                         }
                     }
                 }
+                // A sum that is not finite is formed again below.  0 times it is not 0: of[e] is the token of acc[.][e] (rows) or acc[e] (columns).
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float zero = 0.f;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) zero = fmaf(kColumns ? acc[e][v] : acc[v][e], 0.f, zero);
+                    odd |= of[e] == a && zero != 0.f;
+                }
+                if (rank > 0 && __any(odd)) {
+                    again |= 1u << u;
+                    continue;
+                }
                 const uint32_t to = here(y_lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -818,6 +831,36 @@ __global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kern
                     }
                 }
             }
+            // Quarters with an infinity or NaN, tile by tile from whole numbers by the 32-bit instruction, four ranks at a time, one for each g.
+            if (__builtin_expect(again != 0, 0))
+#pragma unroll 1
+                for (int n = 0; n < 16; ++n) {
+                    const int u = n / 4, v = n % 4;
+                    if (!(again >> u & 1)) continue;
+                    // the tokens and elements of sum[e]
+                    auto token = [&](int e) { return kColumns ? 4 * i + v : 16 * u + 4 * g + e; };
+                    auto element = [&](int e) { return o0 + (kColumns ? 16 * g + 4 * e + u : 4 * i + v); };
+                    auto place = [&](int e, int64_t ld) { return kColumns ? element(e) * ld + t0 + token(e) : (t0 + token(e)) * ld + element(e); };
+                    F4 sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (base) sum[e] = (float)base[place(e, c.ldbase)];  // it may be y: nobody has written what this adapter's tokens get
+#pragma unroll 1
+                    for (int r0 = 0; r0 < rank; r0 += 4) {
+                        const int r = r0 + g;
+                        float h = 0.f, x = 0.f;
+                        if (r < rank) {
+                            const int t = kColumns ? 4 * i + v : 16 * u + i, o = 4 * i + (kColumns ? u : v);
+#pragma unroll
+                            for (int k = kH - 1; k >= 0; --k) h += __uint_as_float((uint32_t)planes[(k * kTile + t) * pitch + r] << 16);
+                            x = (float)w[kAlong ? r * c.w.ld + o : o * c.w.ld + r];
+                        }
+                        sum = kColumns ? product(x, h, sum) : product(h, x, sum);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (present.adapter[token(e)] == a) y[place(e, c.ldy)] = (TX)sum[e];
+                }
         }
     }
 }
@@ -904,20 +947,11 @@ __device__ __forceinline__ void past_rank(F4 (&acc)[kSums], int first, int some,
         for (int e = 0; e < 4; ++e) acc[first + j][e] = at + e < rank ? acc[first + j][e] : 0.f;
 }
 
-// Adapter blockIdx.y, 64 elements of the long axis, kRanks * 16 ranks; the waves share out the groups of 16 tokens in which the adapter occurs.
-// 999 tokens, 2048 -> 4608, rank 8, 4 adapters, columns: 15 us, the adapter's tokens and then their x and d one after the other.
+// Adapter blockIdx.y, 64 elements of the long axis from o0 on, kRanks * 16 ranks from r0 on; the waves share out the groups of 16 tokens in which the adapter occurs.
 template <class TX, bool kColumns, int kRanks>
-__global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
-    OuterArgs c;
-    unsigned block;
-    if (!outer_of(pair, c, block)) return;
-    __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
-    __shared__ F4 room[kOuterBlock / 128][kRanks * 4][64];
+__device__ __forceinline__ void outer_some(const OuterArgs& c, int64_t o0, int r0, int* list, int* count, F4 (*room)[kRanks * 4][64]) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
-    const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks);
-    const int64_t o0 = (int64_t)(block / rank_blocks) * 64;
     const int left = (int)std::min<int64_t>(c.length - o0, 64);
-    const int r0 = (int)(block % rank_blocks) * 16 * kRanks;
     const int rank = rank_of(c.w, a);
     const int64_t from = blockIdx.z * c.range, to = from + c.range < c.tokens ? from + c.range : c.tokens;
     F4 acc[kRanks * 4];  // [rank tile][j]
@@ -1002,6 +1036,18 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
     }
 }
 
+// 999 tokens, 2048 -> 4608, rank 8, 4 adapters, columns: 15 us, the adapter's tokens and then their x and d one after the other.
+template <class TX, bool kColumns, int kRanks>
+__global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
+    OuterArgs c;
+    unsigned block;
+    if (!outer_of(pair, c, block)) return;
+    __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
+    __shared__ F4 room[kOuterBlock / 128][kRanks * 4][64];
+    const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks);
+    outer_some<TX, kColumns, kRanks>(c, (int64_t)(block / rank_blocks) * 64, (int)(block % rank_blocks) * 16 * kRanks, list, count, room);
+}
+
 // Activations in 16 bits, rows: the 16-bit instruction over 32 tokens.  It wants eight tokens of one element in a lane where memory has eight
 // elements of one token: a lane loads eight by eight (kCols = 8; 16 bytes of 8 tokens, sixteen lanes 256 bytes side by side) and
 // turns them in its registers.  The other operand, d or hidden as three bf16 pieces, lies in `planes` as lanes take it (planes_kernel); fp16
@@ -1013,7 +1059,7 @@ __global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterPair pair)
     unsigned block;
     if (!outer_of(pair, c, block)) return;
     constexpr int kX = kWeightPieces<TX>, kSums = kRanks * kCols;
-    __shared__ int list[kOuterBlock], count[kOuterBlock / 64];
+    __shared__ int list[kOuterBlock], count[kOuterBlock / 64], again;
     __shared__ F4 room[kOuterBlock / 128][kSums][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, a = blockIdx.y;
     const int rank_blocks = (c.w.rank + 16 * kRanks - 1) / (16 * kRanks), rank_tiles = (c.w.rank + 15) / 16;
@@ -1084,12 +1130,33 @@ __global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterPair pair)
         __syncthreads();  // the list is made anew
     }
     add_waves(acc, room);
+    // Sums that are not finite (0 times them is not 0): an infinity has met pieces that are 0.  Again, all of them, from whole numbers by the 32-bit instruction.
+    if (wave == 0) {
+        float zero = 0.f;
+#pragma unroll
+        for (int r = 0; r < kRanks; ++r) {
+            past_rank(acc, r * kCols, kCols, 16 * (tile0 + r) + 4 * g, rank);
+#pragma unroll
+            for (int k = 0; k < kCols; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) zero = fmaf(acc[r * kCols + k][e], 0.f, zero);
+        }
+        const bool odd = __any(zero != 0.f);
+        if (lane == 0) again = odd;
+    }
+    __syncthreads();
+    if (__builtin_expect(again, 0)) {
+        for (int64_t o = o0; o < std::min<int64_t>(o0 + 16 * kCols, c.length); o += 64)
+#pragma unroll 1
+            for (int tile = tile0; tile < std::min(tile0 + kRanks, rank_tiles); ++tile)
+                outer_some<TX, false, 1>(c, o, 16 * tile, list, count, reinterpret_cast<F4(*)[4][64]>(&room[0][0][0]));
+        return;
+    }
     if (wave) return;
     float* out = c.out + ((int64_t)blockIdx.z * c.w.adapters + a) * c.w.rank * c.length;
 #pragma unroll
     for (int r = 0; r < kRanks; ++r) {
         const int at = 16 * (tile0 + r) + 4 * g;
-        past_rank(acc, r * kCols, kCols, at, rank);
         if (c.rank_last) {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)

@@ -212,3 +212,23 @@ def test_factor_of_an_adapter_that_nobody_has(tokens, types, factor):
     assert torch.isfinite(GdA).all() and torch.isfinite(GdB).all()
     for a in (2, 3):
         assert (GdA[a] == 0).all() and (GdB[a] == 0).all()
+
+
+@TOKENS
+@TYPES
+def test_whole_numbers_are_exact(tokens, types):
+    """Sums of small whole numbers have no rounding in 32 bits, in whichever order and pieces they are formed."""
+    ta, tw, columns = types
+    gen = torch.Generator().manual_seed(tokens + 8)
+    N, R, n, m = 3, 24, 70, 130
+    index = index_of("runs", tokens, N, 14)
+    A, Bm, x, dy, base = (torch.randint(-2, 3, s, generator=gen).double() for s in ((N, R, n), (N, m, R), (tokens, n), (tokens, m), (tokens, m)))
+    y, hidden, _ = adapters_oracle(A, Bm, None, None, index, x, base)
+    dx, _, dA, _, dB, _ = backward_oracle(A, Bm, None, None, index, dy, x, hidden, None)
+    GA, GB, I, X = A.to(tw).cuda(), Bm.to(tw).cuda(), index.cuda(), put(x, ta, columns)
+    Y, DX, H = room_for(tokens, m, ta, columns), room_for(tokens, n, ta, columns), torch.empty((tokens, R), device="cuda")
+    GdA, GdB = torch.empty((N, R, n), device="cuda"), torch.empty((N, m, R), device="cuda")
+    B.adapter_matmul(GA, GB, I, X, Y, base=put(base, ta, columns), hidden=H)
+    B.adapter_backward(GA, GB, I, put(dy, ta, columns), X, H, dX=DX, dA=GdA, dB=GdB)
+    for got, want in ((Y, y.to(ta)), (H, hidden), (DX, dx.to(ta)), (GdA, dA), (GdB, dB)):
+        assert torch.equal(host(got), want.double())
