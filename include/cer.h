@@ -498,8 +498,10 @@ int cer_stream_read(const void* src_dev, int64_t bytes, void* sink_dev, void* st
  * `stream`, nothing is waited for; buffers have to live until the stream has run it.  Arithmetic, sums and norms are in 32 bits or more
  * whatever the types, and outputs in fewer bits are rounded once (nearest even).  Results do not depend on the order in which
  * workgroups run.  tokens = 0 is allowed and does what is left of the work (gradients of weights become 0).
- * Errors: CER_E_INVALID (null pointers, sizes below 1, unknown or unsuitable types and orders, ld too small), CER_E_TOO_LARGE (norm: tokens
- * over 2^28, features over 65536; adapters: tokens over 2^24, features over 2^22), CER_E_HIP.
+ * Errors: CER_E_INVALID (null pointers, sizes below 1, unknown or unsuitable types and orders, ld too small, or so large that ld times the vectors
+ * passes 2^60), CER_E_TOO_LARGE (norm: tokens over 2^28, features over 65536; adapters: tokens over 2^24, tokens . rank from 2^31 on, features over
+ * 2^22, adapters . rank . max(in, out) over 2^33, leading dimensions of activations over 2^22 in rows or 2^24 in columns, of adapters over 2^22, adapters
+ * over 2^40 elements apart; a gradient of more than 2^48 numbers), CER_E_HIP.
  */
 enum { CER_TYPE_F32 = 0, CER_TYPE_BF16 = 1, CER_TYPE_F16 = 2, CER_TYPE_F8 = 3 };
 enum { CER_ORDER_ROWS = 0, CER_ORDER_COLUMNS = 1 };

@@ -46,7 +46,8 @@ int check_adapters(const cer_adapters_t* w, int64_t tokens) {
     if (std::max(w->stride_a, w->stride_b) > (int64_t)1 << 40 || std::max(w->ld_a, w->ld_b) > kMostLd) return CER_E_TOO_LARGE;
     return CER_OK;
 }
-bool near(const cer_tokens_t* m) { return !there(m) || m->ld <= kMostLd; }
+// Offsets within a tile of 64 vectors fit 32 bits.  Columns of the most tokens lie as far apart as there are tokens: a lane's offset there is at most 48 columns.
+bool near(const cer_tokens_t* m) { return !there(m) || m->ld <= (m->order == CER_ORDER_COLUMNS ? kMostAdapterTokens : kMostLd); }
 // Activations beside adapters of this type.
 bool fits(const cer_tokens_t* m, const cer_adapters_t* w) { return m->type == CER_TYPE_F32 || m->type == w->type; }
 }  // namespace
