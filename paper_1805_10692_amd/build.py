@@ -49,8 +49,13 @@ def build_binding(verbose: bool = True) -> str:
 
 
 def build_operators_binding(verbose: bool = True) -> str:
-    """_cerops.so: host code only, the interpreter's C API and torch's C++ interface (whose libraries are there when it is imported, after torch)."""
-    import torch
+    """_cerops.so: host code only, the interpreter's C API and torch's C++ interface (whose libraries are there when it is imported, after torch).  Where torch is
+    not installed it is left out, and "" returned: the library and the rest of its binding work without."""
+    try:
+        import torch
+    except ImportError:
+        print("torch is not installed: _cerops.so (operators beside a projection, on torch tensors) is not built", flush=True)
+        return ""
     at = os.path.dirname(torch.__file__)
     tmp = NATIVE_OPERATORS + f".tmp{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
