@@ -650,6 +650,12 @@ __device__ __forceinline__ void weight_operands(const Vec<TW, 8> v, Pieces8 (&ou
     }
 }
 
+// Waves for a SIMD: what an adapter's weights in registers leave of them.  32-bit weights: three waves and not four, whose registers spill (8000 tokens of 30 requests in
+// columns, 2048 -> 4096, rank 32: 161 -> 137 us); fp16 rows of ranks (kAlong) over 32 likewise (backward of 3000 tokens, rank 64: 118 -> 112), but not otherwise (8192
+// tokens, forward: 97 -> 102).
+template <class TX, class TW, bool kAlong, int kChunks>
+constexpr int kWideWaves = kChunks == 4 ? 2 : (kChunks && sizeof(TW) == 4) || (kChunks == 2 && kAlong && std::is_same_v<TX, _Float16>) ? 3 : 4;
+
 // 64 tokens.  A wave takes 64 elements of the long axis at a time, with what base has there in registers, and goes through the adapters, each
 // one's weights (ranks up to kChunks * 32; 0: any, loaded again for every tile of 16 tokens) in registers.  Element o0 + 4 i + j is row (column) i of
 // tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as three bf16 pieces by the weights' one (bf16), two
@@ -658,7 +664,7 @@ __device__ __forceinline__ void weight_operands(const Vec<TW, 8> v, Pieces8 (&ou
 // Base and y of 8192 x 4096 bf16, rank 64: 49 us, 2.7 TB/s; of 3136 x 4096 fp32 columns, rank 16: 34 us, 3.0 TB/s; with the 32-bit instruction, which takes its 16
 // rows of y from memory one line a lane, 201 and 66.
 template <class TX, class TW, bool kColumns, bool kAlong, int kChunks>
-__global__ __launch_bounds__(kBlock, kChunks == 4 ? 2 : 4) void expand_wide_kernel(ExpandArgs c) {
+__global__ __launch_bounds__(kBlock, (kWideWaves<TX, TW, kAlong, kChunks>)) void expand_wide_kernel(ExpandArgs c) {
     constexpr int kTile = 64, kH = 3, kW = kWeightPieces<TW>, kHeld = kChunks ? kChunks : 1;
     extern __shared__ float room[];
     __shared__ Present present;
