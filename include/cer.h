@@ -497,7 +497,7 @@ int cer_stream_read(const void* src_dev, int64_t bytes, void* sink_dev, void* st
  * All pointers but the structs themselves (and grad_clip's list) are device pointers on the current device.  Work is enqueued on
  * `stream`, nothing is waited for; buffers have to live until the stream has run it.  Arithmetic, sums and norms are in 32 bits or more
  * whatever the types, and outputs in fewer bits are rounded once (nearest even).  Results do not depend on the order in which
- * workgroups run.  tokens = 0 is allowed and does what is left of the work (gradients of weights become 0).
+ * workgroups run.  Every call may be recorded into a HIP graph after one eager call (temporaries become nodes of it).  tokens = 0 is allowed and does what is left of the work (gradients of weights become 0).
  * Errors: CER_E_INVALID (null pointers, sizes below 1, unknown or unsuitable types and orders, ld too small, or so large that ld times the vectors
  * passes 2^60), CER_E_TOO_LARGE (norm: tokens over 2^28, features over 65536; adapters: tokens over 2^24, tokens . rank from 2^31 on, features over
  * 2^22, adapters . rank . max(in, out) over 2^33, leading dimensions of activations over 2^22 in rows or 2^24 in columns, of adapters over 2^22, adapters
@@ -552,7 +552,7 @@ int rms_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_t
  * adapter_matmul -- hidden_t = A_a x_t;  Y_t = base_t + scales_a B_a hidden_t (base NULL: 0); Y_t = base_t for a token without an adapter.  base
  * may be Y's own place (the product of cer_matmul, say).  base, Y: X's type and order.  hidden: [tokens][rank] fp32, without the factor, for the
  * backward pass, or NULL.  workspace: adapter_workspace_bytes() bytes of device memory, or NULL (a stream-ordered temporary); with it
- * the call only launches two kernels and may be recorded into a HIP graph after one eager call.
+ * the call only launches two kernels.
  *
  * adapter_backward -- d_t = scales_a B_a^T dY_t;  dX_t = base_t + A_a^T d_t (what the projection sends back; NULL: 0; may be dX's own place);
  * dA_a = sum over a's tokens of d_t x_t^T;  dB_a = scales_a . sum over a's tokens of dY_t hidden_t^T.  dX, dA, dB: any may be NULL.

@@ -19,10 +19,12 @@
 //
 // Measured, per call back to back (a large copy reaches 5.0 TB/s on the same card): one token, 2048 -> 2048, rank 16: 9.7 us, two launches that depend on one
 // another; 64 requests of 48 adapters, 9216 -> 4096, rank 16: 21 us; 3136 tokens in columns, 4096 -> 4096, rank 16: 62 us, 2.4 TB/s; 8192 tokens in bf16
-// rows, rank 64: 83 us, 2.5 TB/s; backward of 4096 tokens in bf16 rows, 9216 -> 4096, rank 32: 105 us, 2.5 TB/s.
+// rows, rank 64: 84 us, 2.5 TB/s; backward of 4096 tokens in bf16 rows, 9216 -> 4096, rank 32: 107 us, 2.5 TB/s.
 //
-// Activations in 32 bits are multiplied by the 32-bit matrix instruction, and so is everything behind `hidden` and d, which are kept in 32 bits;
-// activations in 16 bits meet weights of the same type in `shrink` in the 16-bit instruction, which adds up in 32.
+// `shrink`: activations in 32 bits are multiplied by the 32-bit matrix instruction, in 16 bits by the 16-bit one, by weights of the same type; both add up in 32.
+// hidden and d are kept in 32 bits.  What follows them, `expand` and `outer`, uses the 32-bit instruction for up to 256 tokens and for the gradients of activations in
+// 32 bits; else numbers go into the 16-bit one as bf16 pieces that hold all their bits (pieces_of), and a sum that an infinity has reached is formed again by
+// the 32-bit one.
 #include <algorithm>
 #include <type_traits>
 
@@ -37,8 +39,9 @@ template <int kTiles>
 constexpr int kShrinkThreads = kTiles == 1 ? 1024 : 512;
 constexpr int kOuterBlock = 256, kRowsBlock = 512;
 constexpr int kMostTile = 64;  // tokens of a workgroup
-// Up to so many tokens the kernels for 16 of them run, tiles of 64 would be too few for the chip.  4096 -> 4096 features, these kernels against those:
-// 320 tokens of 8 requests, columns, rank 16: 21.5 and 31.7 us, of one request, bf16, rank 64: 27.4 and 19.8; 512 tokens: 26.4 and 18.0, 36.1 and 19.0.
+// Up to so many tokens the kernels for 16 of them run, tiles of 64 would be too few for the chip.  Where the one is as fast as the other depends on the order and the
+// requests too: 4096 -> 4096 features, these kernels against those, 320 tokens of 8 requests, columns, rank 16: 21.5 and 31.7 us, of one request, bf16, rank 64: 27.4
+// and 19.8; 512 tokens: 26.4 and 18.0, 36.1 and 19.0.  The line is where neither loses yet, and the first of these cases is slower than it could be.
 constexpr int64_t kFewTokens = 256;
 
 // One side's weights: element (long axis k, rank r) of adapter a at w[a * stride + (kAlong ? r * ld + k : k * ld + r)].
@@ -661,7 +664,7 @@ constexpr int kWideWaves = kChunks == 4 ? 2 : (kChunks && sizeof(TW) == 4) || (k
 // tile j of four; in columns, token t0 + 4 i + s that of tile s.  hidden is multiplied as three bf16 pieces by the weights' one (bf16), two
 // (fp16) or three in the 16-bit instruction, at a fifth to a half of the 32-bit one's time.  The pieces are cut from the number, so that the second is below 2^-7 of it, the third below
 // 2^-14, and three hold all its bits: only the product of both third ones is left out, 2^-28 of a product.
-// Base and y of 8192 x 4096 bf16, rank 64: 49 us, 2.7 TB/s; of 3136 x 4096 fp32 columns, rank 16: 34 us, 3.0 TB/s; with the 32-bit instruction, which takes its 16
+// Base and y of 8192 x 4096 bf16, rank 64: 51 us, 2.6 TB/s; of 3136 x 4096 fp32 columns, rank 16: 35 us, 3.0 TB/s; with the 32-bit instruction, which takes its 16
 // rows of y from memory one line a lane, 201 and 66.
 template <class TX, class TW, bool kColumns, bool kAlong, int kChunks>
 __global__ __launch_bounds__(kBlock, (kWideWaves<TX, TW, kAlong, kChunks>)) void expand_wide_kernel(ExpandArgs c) {
@@ -1057,7 +1060,7 @@ __global__ __launch_bounds__(kOuterBlock) void outer_kernel(OuterPair pair) {
 // Activations in 16 bits, rows: the 16-bit instruction over 32 tokens.  It wants eight tokens of one element in a lane where memory has eight
 // elements of one token: a lane loads eight by eight (kCols = 8; 16 bytes of 8 tokens, sixteen lanes 256 bytes side by side) and
 // turns them in its registers.  The other operand, d or hidden as three bf16 pieces, lies in `planes` as lanes take it (planes_kernel); fp16
-// activations are two bf16 pieces.  All products of pieces are taken, so that nothing is lost against products in 32 bits.  dA and dB of 4096 tokens, 9216 -> 4096, rank 32, 8 adapters: 38 us,
+// activations are two bf16 pieces.  All products of pieces are taken, so that nothing is lost against products in 32 bits.  dA and dB of 4096 tokens, 9216 -> 4096, rank 32, 8 adapters: 39 us,
 // 2.9 TB/s of x and dy; 158 in the kernel above.
 template <class TX, int kRanks, int kCols>
 __global__ __launch_bounds__(kOuterBlock, 3) void outer16_kernel(OuterPair pair) {
@@ -1295,7 +1298,7 @@ int expand_tiles(ExpandArgs c, hipStream_t s) {
         const int64_t ends = (c.tokens % 64 + 15) / 16 * blocks + (c.length % 64 ? across * 4 : 0);
         const size_t lds = std::max(few, (size_t)3 * 64 * ((c.w.rank + 31) / 32 * 32 + 8) * 2);
         // An adapter's weights stay in registers for a block's 64 tokens where they are few; ranks over 64 in half as many waves then, which
-        // pays in rows (4096 tokens of 64 features -> 4096, rank 128, 8 requests: 52 -> 40 us) and not in columns (rank 128, one: 65 -> 70).
+        // pays in rows (4096 tokens of 64 features -> 4096, rank 128, 8 requests: 52 -> 40 us, with two pieces of hidden) and not in columns (rank 128, one: 65 -> 70).
         constexpr int kMost = sizeof(TX) == 2 || kWeightPieces<TW> == 1 ? 2 : 1, kRows = !kColumns && kWeightPieces<TW> == 1 ? 4 : kMost;  // times 32 ranks
         const auto kernel = c.w.rank <= 32           ? expand_wide_kernel<TX, TW, kColumns, kAlong, 1>
                             : c.w.rank <= 32 * kMost ? expand_wide_kernel<TX, TW, kColumns, kAlong, kMost>
@@ -1435,7 +1438,7 @@ int launch_adapters_backward(const AdapterBackwardCall& c, hipStream_t s) {
         shrink_sum_kernel<<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, part, (uint32_t)f.parts);
         if (int e = (int)hipGetLastError()) return e;
     }
-    if (c.dA || c.dB) {  // before dx, which may lie where x or dy does
+    if (c.dA || c.dB) {
         OuterArgs of_a{}, of_b{};
         of_a.g = d, of_a.planes = d_planes, of_a.w = side_a(c.w), of_a.index = c.index, of_a.tokens = c.tokens, of_a.length = c.w.in, of_a.out = c.dA;
         of_b.g = c.hidden, of_b.planes = hidden_planes, of_b.w = side_b(c.w), of_b.index = c.index, of_b.tokens = c.tokens, of_b.length = c.w.out, of_b.out = c.dB;

@@ -12,8 +12,9 @@
 // differ in their order.  That reads x (and r) twice, the second time mostly from the caches.
 //
 // Measured, per call back to back (a large copy reaches 5.0 TB/s on the same card): one token of 4096 features 4.2 us, the launch; 8192 x 4096 bf16 with
-// residual and 8-bit outputs 61 us, 3.8 TB/s; backward of 4096 x 4608 bf16 38.5 us, 3.9 TB/s; 99 tokens x 9216, bf16 rows to fp32 columns 9.7 us, two launches.
+// residual and 8-bit outputs 61 us, 3.8 TB/s; backward of 4096 x 4608 bf16 38.5 us, 3.9 TB/s; 99 tokens x 9216, bf16 rows to fp32 columns 9.8 us, two launches.
 // Persistent workgroups that request the next token's inputs ahead were slower (63 and 43 us).
+// Backward, over 16384 features: a token's three copies do not fit the registers of 1024 threads and spill (1024 x 25088 bf16 309 us, fp32 1650; x 16384 35 and 67).
 #include <algorithm>
 
 #include "operators.hpp"
