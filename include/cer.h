@@ -588,6 +588,76 @@ typedef struct {
 int grad_norm(const cer_gradient_t* grads, int64_t count, float* norm, void* stream);
 int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float* norm, void* stream);
 
+/*
+ * Operators of a block around projections.  Matrices, types, orders, streams, graphs and errors as above; CER_E_TOO_LARGE: tokens over 2^28
+ * (linear: 2^24), features over 2^22 (block_norm: 32768), tokens . features or in . out over 2^40.
+ */
+
+/*
+ * linear_matmul -- the product with a dense matrix that is not compressed, and what follows it:
+ *   Z_t = W x_t + bias (NULL: 0);  pre = Z (NULL: not kept);  Y = residual (NULL: 0) + activation(Z), from the unrounded Z.
+ *   W     [out][in] of `type` (fp32, bf16, fp16), rows contiguous: element (o, i) at W[o * ldw + i]
+ *   X, Y, residual, pre: of W's type, all in the same order (columns: fp32).  Y may be residual's own place.
+ *   bias  [out] of bias_type: fp32, bf16 or fp16
+ *   activation  CER_ACTIVATION_*: none, max(z, 0), z (1 + erf(z / sqrt 2)) / 2, the same with tanh(sqrt(2/pi) (z + 0.044715 z^3)) for erf, z / (1 + exp(-z)).
+ *         An infinite z has the function's limit (-inf: 0).
+ *
+ * linear_backward -- with dZ = dY . activation'(pre), 0 where that is 0 whatever dY is (rounded to the type before the products):
+ *   dX = base (NULL: 0; may be dX's own place) + W^T dZ;  dW = sum_t dZ_t x_t^T;  dbias = sum_t dZ_t (fp32, from the unrounded dZ).
+ *   dX, dW, dbias: any may be NULL.  residual's gradient is dY itself.
+ *   pre   what linear_matmul wrote (relu: its Y does as well, without a residual); NULL for CER_ACTIVATION_NONE
+ *   dY, X, pre, base, dX: of W's type and all in the same order; X only for dW.  dW: W's type, rows contiguous, lddw >= in.
+ *
+ * Temporaries: dZ with an activation; sums of parts where the product has few outputs (forward: up to 64 . tokens . out floats, 13 MB in all at most).
+ */
+enum { CER_ACTIVATION_NONE = 0, CER_ACTIVATION_RELU = 1, CER_ACTIVATION_GELU = 2, CER_ACTIVATION_GELU_TANH = 3, CER_ACTIVATION_SILU = 4 };
+int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* X, const cer_tokens_t* Y,
+                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* stream);
+int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* dY, const cer_tokens_t* X,
+                    int32_t activation, const cer_tokens_t* pre, const cer_tokens_t* base, const cer_tokens_t* dX, void* dW, int64_t lddw, float* dbias,
+                    void* stream);
+
+/*
+ * block_norm -- where a block's output joins the residual stream:
+ *   U_ti = F_ti . rstd_post_t . post_weight_i (post = 0: U = F);  H = scale . X + gate . U;  Y_ti = H_ti . rstd_pre_t . pre_weight_i, from the unrounded H,
+ *   rstd_post_t = 1 / sqrt(mean_i F_ti^2 + eps), rstd_pre_t the same of H.
+ *   X, H  the residual stream: fp32, bf16 or fp16, rows.  H may be X's own place.
+ *   F, Y  fp32 or X's type, each in rows, or (fp32) in columns, as cer_matmul writes and reads them.  Y in rows may be F's own place.
+ *   gate  one of: NULL, NULL: 1;  gate_vector [n] of gate_type;  gate, a number per token and feature, of X's type in rows
+ *   post_weight, pre_weight  [n], or NULL: 1 (post_weight only with post)
+ *   rstd_post, rstd_pre      [tokens] fp32 for the backward pass, or NULL
+ *
+ * block_norm_backward -- with K = dY . pre_weight, Hhat = H . rstd_pre, Fhat = F . rstd_post:  D = dsum (NULL: 0; the gradient of H that the residual stream
+ * sends back) + rstd_pre (K - Hhat . mean_i(K . Hhat));  dX = scale . D;  dgate = D . U (of a vector: summed over the tokens);  dU = D . gate;
+ * dF = rstd_post (E - Fhat . mean_i(E . Fhat)), E = dU . post_weight;  dpre_weight_i = sum_t dY . Hhat;  dpost_weight_i = sum_t dU . Fhat.
+ *   H, dX, dsum, gate, dgate: one type, rows;  dY: fp32 or H's type, rows or (fp32) columns;  F, dF: the same type and order, as block_norm's F
+ *   rstd_post  NULL: no norm behind the block (then no post_weight and no dpost_weight)
+ *   dgate, dgate_vector, dpost_weight, dpre_weight (the last three fp32): wanted where not NULL;  dgate only with gate, dgate_vector with gate_vector.
+ *   No output may be an input's place.
+ *
+ * Rows alone: one launch forward; backward one, and another (two over 8192 features) where sums over the tokens are wanted, with a temporary of up to
+ * 1536 . n floats.  A matrix in columns costs a temporary of its size and a launch.
+ */
+int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t* H, const cer_tokens_t* Y, int64_t tokens, int64_t n, const cer_tokens_t* gate,
+               const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
+               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* stream);
+int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_tokens_t* F, const float* rstd_pre, const float* rstd_post,
+                        const cer_tokens_t* dX, const cer_tokens_t* dF, int64_t tokens, int64_t n, const cer_tokens_t* gate, const void* gate_vector,
+                        int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
+                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* stream);
+
+/*
+ * dropout_add -- Y_ti = residual_ti (NULL: 0) + (keep_ti ? X_ti . 65536 / (65536 - d) : 0), d = p . 65536 rounded to nearest even, 0 <= p <= 1 (d = 65536: nothing is
+ * kept).  keep_ti = (R_ti >= d), R_ti the 16-bit number of Philox 4x32-10 (Salmon et al., 2011): key = the two halves of key[0], lower first; counter = the halves of
+ * t . ceil(n / 8) + floor(i / 8), then those of key[1] + call (modulo 2^64); number i mod 8 of the four result words, the lower half of each first.
+ *   key   [2] on the device, read when the call runs: a recorded graph has new masks when its owner writes new numbers there
+ *   call  tells the dropouts of one step apart: two with the same key and call have the same numbers
+ *   X, Y, residual: one type and order (columns: fp32); Y may be X's or residual's own place
+ * The backward pass of X is the same call on the gradient (residual: what other paths send back).  A dropped NaN or infinity is 0.  One launch, no temporary.
+ */
+int dropout_add(const cer_tokens_t* X, const cer_tokens_t* residual, const cer_tokens_t* Y, int64_t tokens, int64_t n, const int64_t* key, double p, int64_t call,
+                void* stream);
+
 const char* cer_strerror(int code);
 int cer_last_hip_error(void);
 

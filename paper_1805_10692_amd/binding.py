@@ -47,6 +47,9 @@ EXPORTS = [
 # operators beside a projection
 OPERATOR_EXPORTS = ["rms_norm", "rms_norm_backward", "adapter_workspace_bytes", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip"]
 
+# operators of a block around projections
+BLOCK_EXPORTS = ["linear_matmul", "linear_backward", "block_norm", "block_norm_backward", "dropout_add"]
+
 CER_FORMAT_CER, CER_FORMAT_CSER = 0, 1
 
 CER_PATH_AUTO, CER_PATH_GEMV, CER_PATH_GEMM, CER_PATH_XTILE, CER_PATH_DENSE, CER_PATH_GEMV_EXPAND, CER_PATH_STRIP = -1, 0, 1, 2, 3, 4, 5
@@ -243,7 +246,14 @@ else:
 #   adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)
 #   grad_norm(grads, norm, stream=None)
 #   grad_clip(grads, max_norm, norm, outs=None, stream=None)
-_OPERATORS = ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip")
+# and those of a block around projections (activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'; gate: (n,) or (tokens, n); key: int64, (2,)):
+#   linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, stream=None)
+#   linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, stream=None)
+#   block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, stream=None)
+#   block_norm_backward(dY, H, F, rstd_pre, dX, dF, rstd_post=None, gate=None, post_weight=None, pre_weight=None, scale=1.0, dsum=None, dgate=None,
+#                       dpost_weight=None, dpre_weight=None, stream=None)
+#   dropout_add(X, Y, key, p, residual=None, call=0, stream=None)
+_OPERATORS = ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip", *BLOCK_EXPORTS)
 
 
 def __getattr__(name: str):

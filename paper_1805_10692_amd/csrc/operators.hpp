@@ -63,6 +63,65 @@ struct ClipCall {
 };
 int launch_clip(const ClipCall& c, hipStream_t s);
 
+struct BlockCall {
+    cer_tokens_t x, f, h, y, gate;  // gate: per token and feature
+    int64_t tokens, n;
+    const void* gate_vector;
+    int32_t gate_vector_type;
+    const void *post_weight, *pre_weight;
+    int32_t post_weight_type, pre_weight_type;
+    float scale, eps;
+    bool post;
+    float *rstd_post, *rstd_pre;
+};
+int launch_block_norm(const BlockCall& c, hipStream_t s);
+
+struct BlockBackwardCall {
+    cer_tokens_t dy, h, f, gate, dsum, dx, df, dgate;
+    int64_t tokens, n;
+    const float *rstd_post, *rstd_pre;  // rstd_post == nullptr: no norm behind the block
+    const void* gate_vector;
+    int32_t gate_vector_type;
+    const void *post_weight, *pre_weight;
+    int32_t post_weight_type, pre_weight_type;
+    float scale;
+    float *dgate_vector, *dpost_weight, *dpre_weight;
+};
+int launch_block_norm_backward(const BlockBackwardCall& c, hipStream_t s);
+
+struct DropoutCall {
+    cer_tokens_t x, r, y;
+    int64_t tokens, n;
+    const int64_t* key;
+    uint32_t dropped;  // of 65536
+    int64_t call;
+};
+int launch_dropout(const DropoutCall& c, hipStream_t s);
+
+struct LinearCall {
+    const void* w;
+    int64_t ldw;
+    int32_t type;
+    int64_t tokens, in, out;
+    cer_tokens_t x, residual, y, pre;
+    const void* bias;
+    int32_t bias_type, activation;
+};
+int launch_linear(const LinearCall& c, hipStream_t s);
+
+struct LinearBackwardCall {
+    const void* w;
+    int64_t ldw;
+    int32_t type;
+    int64_t tokens, in, out;
+    cer_tokens_t dy, x, pre, base, dx;
+    int32_t activation;
+    void* dw;
+    int64_t lddw;
+    float* dbias;
+};
+int launch_linear_backward(const LinearBackwardCall& c, hipStream_t s);
+
 // A temporary for the length of a call, ordered on the stream.
 struct Temporary {
     Temporary(size_t bytes, hipStream_t s) : stream(s) { error = bytes ? temp_alloc(&p, bytes, s) : 0; }

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <limits>
 
 #include "operators.hpp"
@@ -9,6 +10,7 @@
 namespace {
 using namespace cer;
 
+constexpr int64_t kMostBlockFeatures = 32768, kMostNumbers = (int64_t)1 << 40;
 constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostAdapterTokens = (int64_t)1 << 24, kMostNormFeatures = 65536, kMostFeatures = (int64_t)1 << 22, kMostRank = 256, kMostAdapters = 65535, kMostLd = (int64_t)1 << 22;
 
 int bytes_of(int type) { return type == CER_TYPE_F32 ? 4 : type == CER_TYPE_F8 ? 1 : 2; }
@@ -50,6 +52,27 @@ int check_adapters(const cer_adapters_t* w, int64_t tokens) {
 bool near(const cer_tokens_t* m) { return !there(m) || m->ld <= (m->order == CER_ORDER_COLUMNS ? kMostAdapterTokens : kMostLd); }
 // Activations beside adapters of this type.
 bool fits(const cer_tokens_t* m, const cer_adapters_t* w) { return m->type == CER_TYPE_F32 || m->type == w->type; }
+// An input, or one that may be missing, of another matrix' type and order.
+bool like(const cer_tokens_t* m, const cer_tokens_t* as, int64_t tokens, int64_t features, bool output) { return good(m, tokens, features, output) && alike(m, as); }
+bool none_or_like(const cer_tokens_t* m, const cer_tokens_t* as, int64_t tokens, int64_t features, bool output) { return !there(m) || like(m, as, tokens, features, output); }
+bool rows_of(const cer_tokens_t* m, int type) { return m->order == CER_ORDER_ROWS && m->type == type; }
+bool apart(const void* out, std::initializer_list<const cer_tokens_t*> others) {
+    return !out || std::none_of(others.begin(), others.end(), [&](const cer_tokens_t* m) { return there(m) && m->data == out; });
+}
+bool vector(const void* p, int type) { return !p || (number_type(type) && reinterpret_cast<uintptr_t>(p) % bytes_of(type) == 0); }
+
+int check_linear(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, int32_t activation) {
+    if (!W || !number_type(type) || tokens < 0 || in < 1 || out < 1 || ldw < 0) return CER_E_INVALID;
+    if (activation < CER_ACTIVATION_NONE || activation > CER_ACTIVATION_SILU || reinterpret_cast<uintptr_t>(W) % bytes_of(type)) return CER_E_INVALID;
+    if (tokens > kMostAdapterTokens || in > kMostFeatures || out > kMostFeatures || tokens * std::max(in, out) > kMostNumbers || in * out > kMostNumbers) return CER_E_TOO_LARGE;
+    return out > 1 && ldw > std::numeric_limits<int64_t>::max() / 8 / out ? CER_E_INVALID : CER_OK;
+}
+// What block_norm and its gradient have in common.
+int check_block(int64_t tokens, int64_t n, const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale) {
+    if (tokens < 0 || n < 1 || !std::isfinite(scale)) return CER_E_INVALID;
+    if (tokens > kMostTokens || n > kMostBlockFeatures || tokens * n > kMostNumbers) return CER_E_TOO_LARGE;
+    return vector(gate_vector, gate_type) && vector(post_weight, post_type) && vector(pre_weight, pre_type) ? CER_OK : CER_E_INVALID;
+}
 }  // namespace
 
 extern "C" {
@@ -135,6 +158,90 @@ static int clip(const cer_gradient_t* grads, int64_t count, float max_norm, floa
 int grad_norm(const cer_gradient_t* grads, int64_t count, float* norm, void* stream) { return clip(grads, count, 0.f, norm, false, stream); }
 int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float* norm, void* stream) {
     return clip(grads, count, max_norm, norm, true, stream);
+}
+
+
+int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* X, const cer_tokens_t* Y,
+                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* stream) {
+    if (int e = check_linear(W, ldw, type, tokens, in, out, activation)) return e;
+    if (!vector(bias, bias_type)) return CER_E_INVALID;
+    if (tokens == 0) return CER_OK;
+    if (!good(X, tokens, in, false) || X->type != type || !like(Y, X, tokens, out, true)) return CER_E_INVALID;
+    if (!none_or_like(residual, X, tokens, out, false) || !none_or_like(pre, X, tokens, out, true)) return CER_E_INVALID;
+    if (there(residual) && !same_or_apart(residual, Y)) return CER_E_INVALID;
+    if (Y->data == W || !apart(Y->data, {X, pre}) || (there(pre) && (pre->data == W || !apart(pre->data, {X, residual})))) return CER_E_INVALID;
+    LinearCall c{W, ldw, type, tokens, in, out, *X, or_none(residual), *Y, or_none(pre), bias, bias_type, activation};
+    return result(launch_linear(c, static_cast<hipStream_t>(stream)));
+}
+
+int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* dY, const cer_tokens_t* X,
+                    int32_t activation, const cer_tokens_t* pre, const cer_tokens_t* base, const cer_tokens_t* dX, void* dW, int64_t lddw, float* dbias,
+                    void* stream) {
+    if (int e = check_linear(W, ldw, type, tokens, in, out, activation)) return e;
+    if (dW && (lddw < in || (out > 1 && lddw > std::numeric_limits<int64_t>::max() / 8 / out) || reinterpret_cast<uintptr_t>(dW) % bytes_of(type) || dW == W)) return CER_E_INVALID;
+    if (reinterpret_cast<uintptr_t>(dbias) % 4) return CER_E_INVALID;
+    if (tokens) {
+        if (!good(dY, tokens, out, false) || dY->type != type) return CER_E_INVALID;
+        if (activation != CER_ACTIVATION_NONE && !like(pre, dY, tokens, out, false)) return CER_E_INVALID;
+        if (dW && !like(X, dY, tokens, in, false)) return CER_E_INVALID;
+        if (!none_or_like(dX, dY, tokens, in, true) || (there(dX) && !none_or_like(base, dX, tokens, in, false))) return CER_E_INVALID;
+        if (there(dX) && there(base) && !same_or_apart(base, dX)) return CER_E_INVALID;
+        if (there(dX) && (dX->data == W || dX->data == dW || !apart(dX->data, {dY, X, pre}))) return CER_E_INVALID;
+        if (!apart(dW, {dY, X, pre, base}) || !apart(dbias, {dY, X, pre, base, dX})) return CER_E_INVALID;
+    }
+    const cer_tokens_t none{nullptr, 0, 0, 0};
+    LinearBackwardCall c{W, ldw, type, tokens, in, out, or_none(dY), or_none(X), activation != CER_ACTIVATION_NONE ? or_none(pre) : none, or_none(base), or_none(dX), activation, dW, lddw, dbias};
+    return result(launch_linear_backward(c, static_cast<hipStream_t>(stream)));
+}
+
+int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t* H, const cer_tokens_t* Y, int64_t tokens, int64_t n, const cer_tokens_t* gate,
+               const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
+               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* stream) {
+    if (int e = check_block(tokens, n, gate_vector, gate_type, post_weight, post_type, pre_weight, pre_type, scale)) return e;
+    if (!(eps >= 0.f) || std::isinf(eps) || (!post && (post_weight || rstd_post)) || (gate_vector && there(gate))) return CER_E_INVALID;
+    if (tokens == 0) return CER_OK;
+    if (!good(X, tokens, n, false) || X->order != CER_ORDER_ROWS || !like(H, X, tokens, n, true) || !same_or_apart(H, X)) return CER_E_INVALID;
+    if (!good(F, tokens, n, false) || !good(Y, tokens, n, true)) return CER_E_INVALID;
+    if ((F->type != CER_TYPE_F32 && F->type != X->type) || (Y->type != CER_TYPE_F32 && Y->type != X->type)) return CER_E_INVALID;
+    if (F->data == Y->data && (!same_or_apart(F, Y) || F->order != CER_ORDER_ROWS)) return CER_E_INVALID;
+    if (!none_or_like(gate, X, tokens, n, false)) return CER_E_INVALID;
+    if (!apart(H->data, {F, Y, gate}) || !apart(Y->data, {X, gate})) return CER_E_INVALID;
+    BlockCall c{*X, *F, *H, *Y, or_none(gate), tokens, n, gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, eps, post != 0, rstd_post, rstd_pre};
+    return result(launch_block_norm(c, static_cast<hipStream_t>(stream)));
+}
+
+int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_tokens_t* F, const float* rstd_pre, const float* rstd_post,
+                        const cer_tokens_t* dX, const cer_tokens_t* dF, int64_t tokens, int64_t n, const cer_tokens_t* gate, const void* gate_vector,
+                        int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
+                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* stream) {
+    if (int e = check_block(tokens, n, gate_vector, gate_type, post_weight, post_type, pre_weight, pre_type, scale)) return e;
+    if (gate_vector && there(gate)) return CER_E_INVALID;
+    if (dgate_vector && !gate_vector) return CER_E_INVALID;
+    if (tokens) {
+        if (!rstd_pre || (!rstd_post && (post_weight || dpost_weight))) return CER_E_INVALID;
+        if (!good(H, tokens, n, false) || H->order != CER_ORDER_ROWS || !like(dX, H, tokens, n, true)) return CER_E_INVALID;
+        if (!good(dY, tokens, n, false) || (dY->type != CER_TYPE_F32 && dY->type != H->type)) return CER_E_INVALID;
+        if (!good(F, tokens, n, false) || (F->type != CER_TYPE_F32 && F->type != H->type) || !like(dF, F, tokens, n, true)) return CER_E_INVALID;
+        if (!none_or_like(dsum, H, tokens, n, false) || !none_or_like(gate, H, tokens, n, false) || !none_or_like(dgate, H, tokens, n, true)) return CER_E_INVALID;
+        if (there(dgate) && !there(gate)) return CER_E_INVALID;
+        if (!apart(dX->data, {dY, H, F, gate, dsum, dF, dgate}) || !apart(dF->data, {dY, H, F, gate, dsum, dgate})) return CER_E_INVALID;
+        if (there(dgate) && !apart(dgate->data, {dY, H, F, gate, dsum})) return CER_E_INVALID;
+    }
+    BlockBackwardCall c{or_none(dY), or_none(H), or_none(F), or_none(gate), or_none(dsum), or_none(dX), or_none(dF), or_none(dgate), tokens, n, rstd_post, rstd_pre,
+                        gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, dgate_vector, dpost_weight, dpre_weight};
+    return result(launch_block_norm_backward(c, static_cast<hipStream_t>(stream)));
+}
+
+int dropout_add(const cer_tokens_t* X, const cer_tokens_t* residual, const cer_tokens_t* Y, int64_t tokens, int64_t n, const int64_t* key, double p, int64_t call,
+                void* stream) {
+    if (tokens < 0 || n < 1 || !(p >= 0.0 && p <= 1.0)) return CER_E_INVALID;
+    if (tokens > kMostTokens || n > kMostFeatures || tokens * n > kMostNumbers) return CER_E_TOO_LARGE;
+    if (tokens == 0) return CER_OK;
+    if (!good(X, tokens, n, false) || !like(Y, X, tokens, n, true) || !none_or_like(residual, X, tokens, n, false)) return CER_E_INVALID;
+    if (!same_or_apart(Y, X) || (there(residual) && !same_or_apart(Y, residual))) return CER_E_INVALID;
+    if (!key || reinterpret_cast<uintptr_t>(key) % 8) return CER_E_INVALID;
+    DropoutCall c{*X, or_none(residual), *Y, tokens, n, key, (uint32_t)std::nearbyint(p * 65536.0), call};
+    return result(launch_dropout(c, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

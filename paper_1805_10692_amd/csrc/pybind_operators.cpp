@@ -1,5 +1,5 @@
 // The operators beside a projection as native functions of the binding (_cerops): rms_norm, rms_norm_backward, adapter_matmul, adapter_backward,
-// grad_norm, grad_clip.
+// grad_norm, grad_clip; and those of a block around projections: linear_matmul, linear_backward, block_norm, block_norm_backward, dropout_add.
 //
 // A call takes up to eight tensors and a decode step's call lasts some microseconds on the GPU.  Read through their Python attributes, a
 // tensor's shape, strides, type, device and address cost 0.6 us (torch makes a new object for each); torch's C++ interface gives them in some
@@ -21,6 +21,11 @@ using AdapterFn = decltype(&adapter_matmul);
 using AdapterBackwardFn = decltype(&adapter_backward);
 using NormOfFn = decltype(&grad_norm);
 using ClipFn = decltype(&grad_clip);
+using LinearFn = decltype(&linear_matmul);
+using LinearBackwardFn = decltype(&linear_backward);
+using BlockFn = decltype(&block_norm);
+using BlockBackwardFn = decltype(&block_norm_backward);
+using DropoutFn = decltype(&dropout_add);
 struct {
     NormFn norm;
     NormBackwardFn norm_backward;
@@ -28,13 +33,18 @@ struct {
     AdapterBackwardFn adapter_backward;
     NormOfFn grad_norm;
     ClipFn grad_clip;
+    LinearFn linear;
+    LinearBackwardFn linear_backward;
+    BlockFn block;
+    BlockBackwardFn block_backward;
+    DropoutFn dropout;
 } g_fn = {};
 
 PyObject* g_check = nullptr;       // binding._check(rc, name): raises for an error code
 PyObject* g_get_device = nullptr;  // torch._C._cuda_getDevice, ._cuda_getCurrentRawStream
 PyObject* g_raw_stream = nullptr;
 PyObject* s_cuda_stream = nullptr;
-constexpr int kInt32 = 100;  // beside CER_TYPE_*
+constexpr int kInt32 = 100, kInt64 = 101;  // beside CER_TYPE_*
 
 bool fail(const char* what, const char* why) {
     PyErr_Format(PyExc_ValueError, "%s %s", what, why);
@@ -96,6 +106,7 @@ int type_of(const at::Tensor& t) {  // -1: another one
         case at::kHalf: return CER_TYPE_F16;
         case at::kFloat8_e4m3fn: return CER_TYPE_F8;
         case at::kInt: return kInt32;
+        case at::kLong: return kInt64;
         default: return -1;
     }
 }
@@ -142,7 +153,7 @@ bool tokens_of(PyObject* o, const char* what, Device& dev, cer_tokens_t* out, in
     if (!t || !dev.has(*t, what)) return false;
     if (t->dim() != 2) return fail(what, "must have 2 dimensions");
     const int type = type_of(*t);
-    if (type < 0 || type == kInt32) return fail(what, "must be float32, bfloat16, float16 or float8_e4m3fn");
+    if (type < 0 || type >= kInt32) return fail(what, "must be float32, bfloat16, float16 or float8_e4m3fn");
     const int64_t size[2] = {t->sizes()[0], t->sizes()[1]}, stride[2] = {t->strides()[0], t->strides()[1]};
     if (*tokens < 0) *tokens = size[0];
     if (*features < 0) *features = size[1];
@@ -186,7 +197,7 @@ bool flat_of(PyObject* o, const char* what, Device& dev, int type, int64_t numbe
     if (!t || !dev.has(*t, what)) return false;
     const int have = type_of(*t);
     if (type >= 0 ? have != type : (have != CER_TYPE_F32 && have != CER_TYPE_BF16 && have != CER_TYPE_F16))
-        return fail(what, type == kInt32 ? "must be int32" : type == CER_TYPE_F32 ? "must be float32" : "must be float32, bfloat16 or float16");
+        return fail(what, type == kInt32 ? "must be int32" : type == kInt64 ? "must be int64" : type == CER_TYPE_F32 ? "must be float32" : "must be float32, bfloat16 or float16");
     if (!t->is_contiguous()) return fail(what, "must be contiguous");
     if (numbers >= 0 && t->numel() != numbers) return fail(what, "has another number of elements than the other arguments ask for");
     if (type_out) *type_out = have;
@@ -390,6 +401,206 @@ PyObject* py_grad_clip(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObj
     return call(g_fn.grad_clip, f.name, list.data(), (int64_t)list.size(), (float)most, static_cast<float*>(norm), stream);
 }
 
+// ---- operators of a block around projections
+// (out, in), rows contiguous
+bool weights_of(PyObject* o, const char* what, Device& dev, const void** at, int64_t* ld, int* type, int64_t* out, int64_t* in) {
+    const at::Tensor* t = tensor_of(o, what);
+    if (!t || !dev.has(*t, what)) return false;
+    if (t->dim() != 2) return fail(what, "must have 2 dimensions");
+    const int have = type_of(*t);
+    if (have != CER_TYPE_F32 && have != CER_TYPE_BF16 && have != CER_TYPE_F16) return fail(what, "must be float32, bfloat16 or float16");
+    if (*type >= 0 && have != *type) return fail(what, "must have W's type");
+    const auto size = t->sizes(), stride = t->strides();
+    if (*out < 0) *out = size[0], *in = size[1];
+    if (size[0] != *out || size[1] != *in) return fail(what, "must have W's shape");
+    if (stride[1] != 1 && size[1] > 1) return fail(what, "must have contiguous rows");
+    *type = have;
+    *ld = size[0] > 1 ? stride[0] : size[1];
+    *at = t->data_ptr();
+    return true;
+}
+bool activation_of(PyObject* o, int* kind) {
+    static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+    *kind = CER_ACTIVATION_NONE;
+    if (!o) return true;
+    if (PyUnicode_Check(o))
+        for (int k = 0; k < 5; ++k)
+            if (PyUnicode_CompareWithASCIIString(o, names[k]) == 0) {
+                *kind = k;
+                return true;
+            }
+    return fail("activation", "must be 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'");
+}
+bool number_of(PyObject* o, double otherwise, double* v) {
+    *v = o ? PyFloat_AsDouble(o) : otherwise;
+    return *v != -1.0 || !PyErr_Occurred();
+}
+// Matrices that a call wants in one order: a single token's or feature's is both, so that those of them that have a choice follow one that has none.
+template <int kMany>
+void one_order(cer_tokens_t* const (&m)[kMany], const int64_t (&features)[kMany], int64_t tokens) {
+    const cer_tokens_t* lead = nullptr;
+    for (int k = 0; k < kMany && !lead; ++k)
+        if (m[k]->data && tokens > 1 && features[k] > 1) lead = m[k];
+    if (!lead) {  // vectors of one token or of one feature: rows
+        for (int k = 0; k < kMany; ++k) {
+            const cer_tokens_t rows{nullptr, 0, 0, CER_ORDER_ROWS};
+            same_order(m[k], rows, tokens, features[k]);
+        }
+        return;
+    }
+    for (int k = 0; k < kMany; ++k) same_order(m[k], *lead, tokens, features[k]);
+}
+
+PyObject* py_linear_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"W", "X", "Y", "bias", "residual", "activation", "pre", "stream"};
+    enum { W, X, Y, kBias, kResidual, kActivation, kPre, kStream, kCount };
+    static const Signature f = {"linear_matmul", 3, kCount, names};
+    PyObject* a[kCount];
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
+    void* stream;
+    Device dev;
+    const void* w;
+    int64_t ldw, out = -1, in = -1, tokens = -1;
+    int type = -1, bias_type = CER_TYPE_F32, kind;
+    if (!weights_of(a[W], "W", dev, &w, &ldw, &type, &out, &in)) return nullptr;
+    cer_tokens_t x{}, y{}, r{}, pre{};
+    if (!tokens_of(a[X], "X", dev, &x, &tokens, &in) || !tokens_of(a[Y], "Y", dev, &y, &tokens, &out)) return nullptr;
+    if (a[kResidual] && !tokens_of(a[kResidual], "residual", dev, &r, &tokens, &out)) return nullptr;
+    if (a[kPre] && !tokens_of(a[kPre], "pre", dev, &pre, &tokens, &out)) return nullptr;
+    one_order<4>({&x, &y, &r, &pre}, {in, out, out, out}, tokens);
+    void* bias = nullptr;
+    if (a[kBias] && !flat_of(a[kBias], "bias", dev, -1, out, &bias, &bias_type)) return nullptr;
+    if (!activation_of(a[kActivation], &kind) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.linear, f.name, w, ldw, type, tokens, in, out, &x, &y, static_cast<const void*>(bias), bias_type, &r, kind, &pre, stream);
+}
+
+PyObject* py_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"W", "dY", "X", "activation", "pre", "base", "dX", "dW", "dbias", "stream"};
+    enum { W, kDY, X, kActivation, kPre, kBase, kDX, kDW, kDBias, kStream, kCount };
+    static const Signature f = {"linear_backward", 2, kCount, names};
+    PyObject* a[kCount];
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
+    void* stream;
+    Device dev;
+    const void *w, *dw = nullptr;
+    int64_t ldw, lddw = 0, out = -1, in = -1, tokens = -1;
+    int type = -1, kind;
+    if (!weights_of(a[W], "W", dev, &w, &ldw, &type, &out, &in)) return nullptr;
+    cer_tokens_t dy{}, x{}, pre{}, base{}, dx{};
+    if (!tokens_of(a[kDY], "dY", dev, &dy, &tokens, &out)) return nullptr;
+    if (a[X] && !tokens_of(a[X], "X", dev, &x, &tokens, &in)) return nullptr;
+    if (a[kPre] && !tokens_of(a[kPre], "pre", dev, &pre, &tokens, &out)) return nullptr;
+    if (a[kBase] && !tokens_of(a[kBase], "base", dev, &base, &tokens, &in)) return nullptr;
+    if (a[kDX] && !tokens_of(a[kDX], "dX", dev, &dx, &tokens, &in)) return nullptr;
+    one_order<5>({&dy, &x, &pre, &base, &dx}, {out, in, out, in, in}, tokens);
+    if (a[kDW] && !weights_of(a[kDW], "dW", dev, &dw, &lddw, &type, &out, &in)) return nullptr;
+    void* dbias = nullptr;
+    if (a[kDBias] && !flat_of(a[kDBias], "dbias", dev, CER_TYPE_F32, out, &dbias)) return nullptr;
+    if (!activation_of(a[kActivation], &kind) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.linear_backward, f.name, w, ldw, type, tokens, in, out, &dy, &x, kind, &pre, &base, &dx, const_cast<void*>(dw), lddw, static_cast<float*>(dbias), stream);
+}
+
+// gate: (n,) of any type, or (tokens, n)
+struct Gate {
+    cer_tokens_t each{};
+    void* vector = nullptr;
+    int type = CER_TYPE_F32;
+    bool of(PyObject* o, const char* what, Device& dev, int only, int64_t tokens, int64_t n) {
+        if (!o) return true;
+        const at::Tensor* t = tensor_of(o, what);
+        if (!t) return false;
+        if (t->dim() == 1) return flat_of(o, what, dev, only, n, &vector, &type);
+        if (!tokens_of(o, what, dev, &each, &tokens, &n)) return false;
+        rows(&each, tokens, n);
+        return true;
+    }
+    static void rows(cer_tokens_t* m, int64_t tokens, int64_t n) { same_order(m, cer_tokens_t{nullptr, 0, 0, CER_ORDER_ROWS}, tokens, n); }
+};
+
+PyObject* py_block_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"X", "F", "H", "Y", "gate", "post_weight", "pre_weight", "scale", "eps", "post", "rstd_post", "rstd_pre", "stream"};
+    enum { X, F, H, Y, kGate, kPostWeight, kPreWeight, kScale, kEps, kPost, kRstdPost, kRstdPre, kStream, kCount };
+    static const Signature f = {"block_norm", 4, kCount, names};
+    PyObject* a[kCount];
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
+    void* stream;
+    Device dev;
+    int64_t tokens = -1, n = -1;
+    cer_tokens_t x{}, o{}, h{}, y{};
+    if (!tokens_of(a[X], "X", dev, &x, &tokens, &n) || !tokens_of(a[F], "F", dev, &o, &tokens, &n) || !tokens_of(a[H], "H", dev, &h, &tokens, &n) ||
+        !tokens_of(a[Y], "Y", dev, &y, &tokens, &n))
+        return nullptr;
+    for (cer_tokens_t* m : {&x, &h, &o, &y}) Gate::rows(m, tokens, n);
+    Gate gate;
+    if (!gate.of(a[kGate], "gate", dev, -1, tokens, n)) return nullptr;
+    void *post_weight = nullptr, *pre_weight = nullptr, *rstd_post = nullptr, *rstd_pre = nullptr;
+    int post_type = CER_TYPE_F32, pre_type = CER_TYPE_F32;
+    if (a[kPostWeight] && !flat_of(a[kPostWeight], "post_weight", dev, -1, n, &post_weight, &post_type)) return nullptr;
+    if (a[kPreWeight] && !flat_of(a[kPreWeight], "pre_weight", dev, -1, n, &pre_weight, &pre_type)) return nullptr;
+    if (a[kRstdPost] && !flat_of(a[kRstdPost], "rstd_post", dev, CER_TYPE_F32, tokens, &rstd_post)) return nullptr;
+    if (a[kRstdPre] && !flat_of(a[kRstdPre], "rstd_pre", dev, CER_TYPE_F32, tokens, &rstd_pre)) return nullptr;
+    double scale, eps;
+    if (!number_of(a[kScale], 1.0, &scale) || !number_of(a[kEps], 1e-6, &eps)) return nullptr;
+    const int post = a[kPost] ? PyObject_IsTrue(a[kPost]) : 1;
+    if (post < 0 || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.block, f.name, &x, &o, &h, &y, tokens, n, &gate.each, static_cast<const void*>(gate.vector), gate.type, static_cast<const void*>(post_weight), post_type,
+                static_cast<const void*>(pre_weight), pre_type, (float)scale, (float)eps, post, static_cast<float*>(rstd_post), static_cast<float*>(rstd_pre), stream);
+}
+
+PyObject* py_block_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"dY", "H", "F", "rstd_pre", "dX", "dF", "rstd_post", "gate", "post_weight", "pre_weight", "scale", "dsum", "dgate", "dpost_weight", "dpre_weight", "stream"};
+    enum { kDY, H, F, kRstdPre, kDX, kDF, kRstdPost, kGate, kPostWeight, kPreWeight, kScale, kDSum, kDGate, kDPostWeight, kDPreWeight, kStream, kCount };
+    static const Signature f = {"block_norm_backward", 6, kCount, names};
+    PyObject* a[kCount];
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
+    void* stream;
+    Device dev;
+    int64_t tokens = -1, n = -1;
+    cer_tokens_t dy{}, h{}, o{}, dx{}, df{}, dsum{};
+    if (!tokens_of(a[kDY], "dY", dev, &dy, &tokens, &n) || !tokens_of(a[H], "H", dev, &h, &tokens, &n) || !tokens_of(a[F], "F", dev, &o, &tokens, &n) ||
+        !tokens_of(a[kDX], "dX", dev, &dx, &tokens, &n) || !tokens_of(a[kDF], "dF", dev, &df, &tokens, &n))
+        return nullptr;
+    if (a[kDSum] && !tokens_of(a[kDSum], "dsum", dev, &dsum, &tokens, &n)) return nullptr;
+    for (cer_tokens_t* m : {&dy, &h, &o, &dx, &df, &dsum}) Gate::rows(m, tokens, n);
+    Gate gate, dgate;
+    if (!gate.of(a[kGate], "gate", dev, -1, tokens, n) || !dgate.of(a[kDGate], "dgate", dev, CER_TYPE_F32, tokens, n)) return nullptr;
+    if (a[kDGate] && (!dgate.vector) != (!gate.vector)) return fail("dgate", "must have gate's shape"), nullptr;
+    void *rstd_pre = nullptr, *rstd_post = nullptr, *post_weight = nullptr, *pre_weight = nullptr, *dpost = nullptr, *dpre = nullptr;
+    int post_type = CER_TYPE_F32, pre_type = CER_TYPE_F32;
+    if (!flat_of(a[kRstdPre], "rstd_pre", dev, CER_TYPE_F32, tokens, &rstd_pre)) return nullptr;
+    if (a[kRstdPost] && !flat_of(a[kRstdPost], "rstd_post", dev, CER_TYPE_F32, tokens, &rstd_post)) return nullptr;
+    if (a[kPostWeight] && !flat_of(a[kPostWeight], "post_weight", dev, -1, n, &post_weight, &post_type)) return nullptr;
+    if (a[kPreWeight] && !flat_of(a[kPreWeight], "pre_weight", dev, -1, n, &pre_weight, &pre_type)) return nullptr;
+    if (a[kDPostWeight] && !flat_of(a[kDPostWeight], "dpost_weight", dev, CER_TYPE_F32, n, &dpost)) return nullptr;
+    if (a[kDPreWeight] && !flat_of(a[kDPreWeight], "dpre_weight", dev, CER_TYPE_F32, n, &dpre)) return nullptr;
+    double scale;
+    if (!number_of(a[kScale], 1.0, &scale) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.block_backward, f.name, &dy, &h, &o, static_cast<const float*>(rstd_pre), static_cast<const float*>(rstd_post), &dx, &df, tokens, n, &gate.each,
+                static_cast<const void*>(gate.vector), gate.type, static_cast<const void*>(post_weight), post_type, static_cast<const void*>(pre_weight), pre_type, (float)scale, &dsum,
+                &dgate.each, static_cast<float*>(dgate.vector), static_cast<float*>(dpost), static_cast<float*>(dpre), stream);
+}
+
+PyObject* py_dropout_add(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"X", "Y", "key", "p", "residual", "call", "stream"};
+    enum { X, Y, kKey, P, kResidual, kCall, kStream, kCount };
+    static const Signature f = {"dropout_add", 4, kCount, names};
+    PyObject* a[kCount];
+    if (!take(f, args, nargs, kwnames, a)) return nullptr;
+    void *stream, *key;
+    Device dev;
+    int64_t tokens = -1, n = -1;
+    cer_tokens_t x{}, y{}, r{};
+    if (!tokens_of(a[X], "X", dev, &x, &tokens, &n) || !tokens_of(a[Y], "Y", dev, &y, &tokens, &n)) return nullptr;
+    if (a[kResidual] && !tokens_of(a[kResidual], "residual", dev, &r, &tokens, &n)) return nullptr;
+    one_order<3>({&x, &y, &r}, {n, n, n}, tokens);
+    if (!flat_of(a[kKey], "key", dev, kInt64, 2, &key)) return nullptr;
+    double p;
+    if (!number_of(a[P], 0.0, &p)) return nullptr;
+    const long long which = a[kCall] ? PyLong_AsLongLong(a[kCall]) : 0;
+    if ((which == -1 && PyErr_Occurred()) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.dropout, f.name, &x, &r, &y, tokens, n, static_cast<const int64_t*>(key), p, (int64_t)which, stream);
+}
+
 // setup(check): binding.py's function
 PyObject* setup(PyObject*, PyObject* check) {
     Py_INCREF(check);
@@ -399,11 +610,14 @@ PyObject* setup(PyObject*, PyObject* check) {
 
 // bind(addresses): where the loaded library has the operators, in the order of g_fn
 PyObject* bind(PyObject*, PyObject* args) {
-    unsigned long long at[6];
-    if (!PyArg_ParseTuple(args, "KKKKKK", &at[0], &at[1], &at[2], &at[3], &at[4], &at[5])) return nullptr;
+    unsigned long long at[11];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKK", &at[0], &at[1], &at[2], &at[3], &at[4], &at[5], &at[6], &at[7], &at[8], &at[9], &at[10])) return nullptr;
     g_fn = {reinterpret_cast<NormFn>((uintptr_t)at[0]),    reinterpret_cast<NormBackwardFn>((uintptr_t)at[1]),
             reinterpret_cast<AdapterFn>((uintptr_t)at[2]), reinterpret_cast<AdapterBackwardFn>((uintptr_t)at[3]),
-            reinterpret_cast<NormOfFn>((uintptr_t)at[4]),  reinterpret_cast<ClipFn>((uintptr_t)at[5])};
+            reinterpret_cast<NormOfFn>((uintptr_t)at[4]),  reinterpret_cast<ClipFn>((uintptr_t)at[5]),
+            reinterpret_cast<LinearFn>((uintptr_t)at[6]),  reinterpret_cast<LinearBackwardFn>((uintptr_t)at[7]),
+            reinterpret_cast<BlockFn>((uintptr_t)at[8]),   reinterpret_cast<BlockBackwardFn>((uintptr_t)at[9]),
+            reinterpret_cast<DropoutFn>((uintptr_t)at[10])};
     Py_RETURN_NONE;
 }
 
@@ -432,6 +646,15 @@ PyMethodDef g_methods[] = {
                  "adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_norm", py_grad_norm, "grad_norm(grads, norm, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_clip", py_grad_clip, "grad_clip(grads, max_norm, norm, outs=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("linear_matmul", py_linear_matmul, "linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("linear_backward", py_linear_backward,
+                 "linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("block_norm", py_block_norm,
+                 "block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("block_norm_backward", py_block_norm_backward,
+                 "block_norm_backward(dY, H, F, rstd_pre, dX, dF, rstd_post=None, gate=None, post_weight=None, pre_weight=None, scale=1.0, dsum=None, dgate=None, "
+                 "dpost_weight=None, dpre_weight=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("dropout_add", py_dropout_add, "dropout_add(X, Y, key, p, residual=None, call=0, stream=None)\n--\n\n"),
     {"setup", setup, METH_O, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
