@@ -83,9 +83,10 @@ struct Product {
     int64_t lda, ldb;  // from a row to the next, or from one k to the next
     int64_t rows, columns, depth;
     Epilogue to;
-    float* part;          // [parts][rows][columns], or nullptr: one part, through the epilogue
-    int64_t depth_of_part;
     uint32_t tiles_i, tiles_j;
+    uint32_t whole, parts;  // the first `whole` tiles go through the epilogue; the contraction of the others is cut into parts
+    int64_t depth_of_part;
+    float* part;            // [tiles - whole][parts][rows of a tile][columns of a tile]
 };
 
 // Four neighbouring j of row i, `left` of them in the matrix.
@@ -118,57 +119,71 @@ __device__ __forceinline__ F16 multiply(Chunk a, Chunk b, F16 c) {
     }
 }
 
-// One operand's way from memory to LDS: kRows rows of 128 bytes of k.  Rows past the matrix repeat its last one or are 0 (their results are dropped);
-// k past the end is 0 on both sides.
-template <class T, int kRows, int kThreads, bool kTurn>
+// One operand's way from memory to LDS: kRows rows of 128 bytes of k, kAhead tiles of them on their way in registers.  Of rows past the matrix any others are
+// read in their place (their results are dropped); k past the end is 0 on both sides.
+template <class T, int kRows, int kThreads, bool kTurn, int kAhead>
 struct Stage {
     static constexpr int E = 16 / sizeof(T), kDepth = 8 * E;
     static constexpr int kPieces = kTurn ? kRows * 2 : kRows * 8, kCount = (kPieces + kThreads - 1) / kThreads;  // turned: 4 rows by a chunk
     const T* at[kCount];
-    int left[kTurn ? kCount : 1];
-    Chunk held[kTurn ? 1 : kCount];
-    Vec<T, 4> lines[kTurn ? kCount : 1][kTurn ? E : 1];
+    uint32_t to[kCount][kTurn ? 4 : 1];  // chunks of LDS
+    Chunk held[kAhead][kTurn ? 1 : kCount];
+    Vec<T, 4> lines[kAhead][kTurn ? kCount : 1][kTurn ? E : 1];
 
     static __device__ __forceinline__ unsigned piece(int n) { return threadIdx.x + n * kThreads; }
     static __device__ __forceinline__ bool busy(int n) { return kPieces % kThreads == 0 || piece(n) < (unsigned)kPieces; }
     static __device__ __forceinline__ unsigned row(int n) { return kTurn ? piece(n) % (kRows / 4) * 4 : piece(n) / 8; }
     static __device__ __forceinline__ unsigned chunk(int n) { return kTurn ? piece(n) / (kRows / 4) : piece(n) % 8; }
 
+    // Turned, four rows are read at once: the last four instead of any that pass the end, where the tile has four.
+    static __device__ __forceinline__ bool inside(int64_t row0, int64_t rows) { return !kTurn || rows - row0 >= 4; }
     __device__ __forceinline__ void start(const void* base, int64_t ld, int64_t row0, int64_t rows, int64_t k0) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
-            const int64_t i = row0 + row(n), k = k0 + chunk(n) * E;
+            const int64_t k = k0 + chunk(n) * E, most = rows - row0;
             if constexpr (kTurn) {
-                at[n] = static_cast<const T*>(base) + k * ld + i;
-                left[n] = (int)(rows - i < 4 ? rows - i : 4);
+                const int i = inside(row0, rows) && row(n) + 4 > most ? (int)most - 4 : (int)row(n);
+                at[n] = static_cast<const T*>(base) + k * ld + row0 + i;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) to[n][r] = place(i + r, chunk(n));
             } else {
-                at[n] = static_cast<const T*>(base) + (i < rows ? i : rows - 1) * ld + k;
+                at[n] = static_cast<const T*>(base) + (row0 + (row(n) < most ? row(n) : most - 1)) * ld + k;
+                to[n][0] = place(row(n), chunk(n));
             }
         }
     }
-    // The next kDepth of k; `remain`: how many there are up to the end.
-    __device__ __forceinline__ void load_next(int64_t ld, int64_t remain) {
+    // The kDepth of k at hand, all of them in the matrix.
+    __device__ __forceinline__ void load_whole(int slot, int64_t ld) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             if (!busy(n)) continue;
             if constexpr (kTurn) {
-                const int64_t k = remain - chunk(n) * E;
-                if (remain >= kDepth && left[n] == 4) {
 #pragma unroll
-                    for (int q = 0; q < E; ++q) lines[n][q] = load<T, 4>(at[n] + q * ld);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < E; ++q) lines[n][q] = load_own<T, 4>(at[n] + q * ld, q < k ? left[n] : 0);
-                }
-                at[n] += kDepth * ld;
+                for (int q = 0; q < E; ++q) lines[slot][n][q] = load<T, 4>(at[n] + q * ld);
             } else {
-                if (remain >= kDepth) held[n] = __builtin_bit_cast(Chunk, (load<T, E>(at[n])));
-                else held[n] = __builtin_bit_cast(Chunk, (load_own<T, E>(at[n], remain - chunk(n) * E)));
-                at[n] += kDepth;
+                held[slot][n] = __builtin_bit_cast(Chunk, (load<T, E>(at[n])));
             }
         }
     }
-    __device__ __forceinline__ void to_lds(Chunk* room) const {
+    // The same where `remain` of k are left, and (turned) fewer than four rows may be.
+    __device__ __forceinline__ void load_some(int slot, int64_t ld, int64_t remain, int64_t row0, int64_t rows) {
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) {
+            if (!busy(n)) continue;
+            const int64_t k = remain - chunk(n) * E, most = inside(row0, rows) ? 4 : rows - row0 - row(n);
+            if constexpr (kTurn) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) lines[slot][n][q] = load_own<T, 4>(at[n] + q * ld, q < k ? most : 0);
+            } else {
+                held[slot][n] = __builtin_bit_cast(Chunk, (load_own<T, E>(at[n], k)));
+            }
+        }
+    }
+    __device__ __forceinline__ void advance(int64_t ld) {
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) at[n] += kDepth * (kTurn ? ld : 1);
+    }
+    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             if (!busy(n)) continue;
@@ -177,40 +192,47 @@ struct Stage {
                 for (int r = 0; r < 4; ++r) {
                     Vec<T, E> line;
 #pragma unroll
-                    for (int q = 0; q < E; ++q) line[q] = lines[n][q][r];
-                    room[place(row(n) + r, chunk(n))] = __builtin_bit_cast(Chunk, line);
+                    for (int q = 0; q < E; ++q) line[q] = lines[slot][n][q][r];
+                    room[to[n][r]] = __builtin_bit_cast(Chunk, line);
                 }
             } else {
-                room[place(row(n), chunk(n))] = held[n];
+                room[to[n][0]] = held[slot][n];
             }
         }
     }
 };
 
 // Neighbouring workgroups run on different dies, each with a cache of its own: a die gets neighbouring tiles, eight rows of tiles at a time.
-__device__ __forceinline__ void tile_of(unsigned id, unsigned tiles_i, unsigned tiles_j, unsigned* ti, unsigned* tj) {
-    const unsigned all = tiles_i * tiles_j, die = id % 8, each = all / 8, more = all % 8;
-    id = die * each + (die < more ? die : more) + id / 8;
-    const unsigned group = id / (8 * tiles_j), first = group * 8, high = tiles_i - first < 8 ? tiles_i - first : 8;
-    id -= first * tiles_j;
-    *ti = first + id % high;
-    *tj = id / high;
+__device__ __forceinline__ unsigned on_dies(unsigned id, unsigned all) {
+    const unsigned die = id % 8, each = all / 8, more = all % 8;
+    return die * each + (die < more ? die : more) + id / 8;
+}
+__device__ __forceinline__ void tile_of(unsigned at, unsigned tiles_i, unsigned tiles_j, unsigned* ti, unsigned* tj) {
+    const unsigned group = at / (8 * tiles_j), first = group * 8, high = tiles_i - first < 8 ? tiles_i - first : 8;
+    at -= first * tiles_j;
+    *ti = first + at % high;
+    *tj = at / high;
 }
 
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB>
+// A barrier for LDS alone: __syncthreads would also wait for the loads from memory that are on their way for the tile after next.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead, bool kTurnA, bool kTurnB>
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
-    using StageA = Stage<T, kI, kThreads, kTurnA>;
-    using StageB = Stage<T, kJ, kThreads, kTurnB>;
+    using StageA = Stage<T, kI, kThreads, kTurnA, kAhead>;
+    using StageB = Stage<T, kJ, kThreads, kTurnB, kAhead>;
     constexpr int kDepth = StageA::kDepth;
     __shared__ Chunk room[2][(kI + kJ) * 8];
     static_assert(sizeof(room) >= sizeof(float) * kWavesI * kWavesJ * 32 * kPitch, "");
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wave_i = wave / kWavesJ, wave_j = wave % kWavesJ;
+    const bool cut = blockIdx.x >= p.whole;
+    const unsigned piece = cut ? blockIdx.x - p.whole : 0;
     unsigned ti, tj;
-    tile_of(blockIdx.x, p.tiles_i, p.tiles_j, &ti, &tj);
-    const int64_t i0 = (int64_t)ti * kI, j0 = (int64_t)tj * kJ, k0 = (int64_t)blockIdx.y * p.depth_of_part;
-    int64_t remain = p.depth - k0 < p.depth_of_part ? p.depth - k0 : p.depth_of_part;
+    tile_of(cut ? p.whole + piece / p.parts : on_dies(blockIdx.x, p.whole), p.tiles_i, p.tiles_j, &ti, &tj);
+    const int64_t i0 = (int64_t)ti * kI, j0 = (int64_t)tj * kJ, k0 = cut ? piece % p.parts * p.depth_of_part : 0;
+    int64_t remain = cut && p.depth - k0 > p.depth_of_part ? p.depth_of_part : p.depth - k0;
     StageA a;
     StageB b;
     a.start(p.a, p.lda, i0, p.rows, k0);
@@ -220,38 +242,90 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     for (int x = 0; x < kTilesI; ++x)
 #pragma unroll
         for (int y = 0; y < kTilesJ; ++y) sums[x][y] = 0.f;
-    if (remain > 0) {
-        a.load_next(p.lda, remain);
-        b.load_next(p.ldb, remain);
-        a.to_lds(room[0]);
-        b.to_lds(room[0] + kI * 8);
-        __syncthreads();
-    }
-    for (unsigned turn = 0; remain > 0; turn ^= 1) {
-        remain -= kDepth;
-        if (remain > 0) {
-            a.load_next(p.lda, remain);
-            b.load_next(p.ldb, remain);
+    const unsigned at_lane = place(lane & 31, lane >> 5);  // chunk 2 . step + (lane >> 5): the permutation is an exclusive or
+    Chunk x[2][kTilesI], y[2][kTilesJ];
+    const auto operands = [&](const Chunk* half, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
+        const Chunk* from = half + (at_lane ^ 2 * step);
+#pragma unroll
+        for (int k = 0; k < kTilesI; ++k) u[k] = from[(wave_i * kWideI + k * 32) * 8];
+#pragma unroll
+        for (int k = 0; k < kTilesJ; ++k) v[k] = from[(kI + wave_j * kWideJ + k * 32) * 8];
+    };
+    const auto products = [&](const Chunk(&u)[kTilesI], const Chunk(&v)[kTilesJ]) {
+#pragma unroll
+        for (int i = 0; i < kTilesI; ++i)
+#pragma unroll
+            for (int j = 0; j < kTilesJ; ++j) sums[i][j] = multiply<T>(v[j], u[i], sums[i][j]);
+    };
+    // Whole tiles.  While tile k is multiplied out of one half of LDS, tile k + 1 goes from registers into the other half and the kAhead after it are on their
+    // way from memory; past the last one the last is read again, for nobody.
+    unsigned turn = 0;
+    const int64_t whole = StageA::inside(i0, p.rows) && StageB::inside(j0, p.columns) && remain > 0 ? remain / kDepth : 0;
+    if (whole) {
+        a.load_whole(0, p.lda);
+        b.load_whole(0, p.ldb);
+        a.to_lds(0, room[0]);
+        b.to_lds(0, room[0] + kI * 8);
+#pragma unroll
+        for (int ahead = 0; ahead < kAhead; ++ahead) {
+            if (ahead + 1 < whole) a.advance(p.lda), b.advance(p.ldb);
+            a.load_whole(ahead, p.lda);
+            b.load_whole(ahead, p.ldb);
         }
-        const Chunk *from_a = room[turn] + wave_i * kWideI * 8, *from_b = room[turn] + (kI + wave_j * kWideJ) * 8;
+        lds_barrier();
+        operands(room[0], 0, x[0], y[0]);
+        for (int64_t k0 = 0; k0 < whole; k0 += kAhead) {
+#pragma unroll
+            for (int slot = 0; slot < kAhead; ++slot) {
+                if (k0 + slot >= whole) break;
+                const bool more = k0 + slot + kAhead + 1 < whole;
+#pragma unroll
+                for (unsigned step = 0; step < 4; ++step) {
+                    if (step < 3) {
+                        operands(room[turn], step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
+                    } else {  // every operand of this tile is in registers: the next tile's first ones come while the last products run
+                        lds_barrier();
+                        operands(room[turn ^ 1], 0, x[0], y[0]);
+                    }
+                    if (step == 0) {
+                        a.to_lds(slot, room[turn ^ 1]);
+                        if (more) a.advance(p.lda);
+                        a.load_whole(slot, p.lda);
+                    } else if (step == 1) {
+                        b.to_lds(slot, room[turn ^ 1] + kI * 8);
+                        if (more) b.advance(p.ldb);
+                        b.load_whole(slot, p.ldb);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);  // the compiler would move requests down to where their answers are needed
+                    products(x[step & 1], y[step & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                turn ^= 1;
+            }
+        }
+        lds_barrier();
+        remain -= whole * kDepth;
+        a.advance(p.lda);
+        b.advance(p.ldb);
+    }
+    // What is left: a part of a tile, or all of them where rows end inside a turned operand.
+    while (remain > 0) {
+        a.load_some(0, p.lda, remain, i0, p.rows);
+        b.load_some(0, p.ldb, remain, j0, p.columns);
+        a.to_lds(0, room[turn]);
+        b.to_lds(0, room[turn] + kI * 8);
+        lds_barrier();
 #pragma unroll
         for (unsigned step = 0; step < 4; ++step) {
-            Chunk x[kTilesI], y[kTilesJ];
-#pragma unroll
-            for (int k = 0; k < kTilesI; ++k) x[k] = from_a[place(lane & 31, 2 * step + (lane >> 5)) + k * 256];
-#pragma unroll
-            for (int k = 0; k < kTilesJ; ++k) y[k] = from_b[place(lane & 31, 2 * step + (lane >> 5)) + k * 256];
-#pragma unroll
-            for (int i = 0; i < kTilesI; ++i)
-#pragma unroll
-                for (int j = 0; j < kTilesJ; ++j) sums[i][j] = multiply<T>(y[j], x[i], sums[i][j]);
+            operands(room[turn], step, x[0], y[0]);
+            products(x[0], y[0]);
         }
-        if (remain > 0) {
-            a.to_lds(room[turn ^ 1]);
-            b.to_lds(room[turn ^ 1] + kI * 8);
-        }
-        __syncthreads();
+        remain -= kDepth;
+        a.advance(p.lda);
+        b.advance(p.ldb);
+        turn ^= 1;
     }
+    __syncthreads();
     // 32 rows of each wave at a time through LDS, so that neighbouring lanes have neighbouring numbers of a row
     float* own = reinterpret_cast<float*>(room) + wave * 32 * kPitch;
 #pragma unroll
@@ -269,56 +343,219 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
 #pragma unroll 1
         for (int row = lane / kAbreast; row < 32; row += 64 / kAbreast) {
             const int64_t i = i0 + wave_i * kWideI + x * 32 + row;
-            if (i >= p.rows || j >= p.columns) continue;
             const Vec<float, 4> z = *reinterpret_cast<const Vec<float, 4>*>(own + row * kPitch + lane % kAbreast * 4);
-            if (p.part) store_some<float, 4>(p.part + (blockIdx.y * p.rows + i) * p.columns + j, z, p.columns - j);
-            else finish<T>(p.to, i, j, z, p.columns - j);
+            if (cut) {
+                store<float, 4>(p.part + ((int64_t)piece * kI + (i - i0)) * kJ + (j - j0), z);
+                continue;
+            }
+            if (i < p.rows && j < p.columns) finish<T>(p.to, i, j, z, p.columns - j);
         }
     }
 }
 
-// The parts added up in their order, then the epilogue: four neighbouring numbers of C a thread.
-template <class T>
-__global__ __launch_bounds__(256) void parts_kernel(Product p, uint32_t parts) {
-    const int64_t abreast = (p.columns + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x, i = at / abreast, j = at % abreast * 4;
-    if (i >= p.rows) return;
+// The parts of the tiles that were cut, added up in their order, then the epilogue: four neighbouring numbers of C a thread.  Workgroup (b, t): 1024 numbers of tile t.
+template <class T, int kI, int kJ>
+__global__ __launch_bounds__(256) void parts_kernel(Product p) {
+    unsigned ti, tj;
+    tile_of(p.whole + blockIdx.y, p.tiles_i, p.tiles_j, &ti, &tj);
+    const unsigned at = blockIdx.x * 1024 + threadIdx.x * 4;
+    const int64_t i = (int64_t)ti * kI + at / kJ, j = (int64_t)tj * kJ + at % kJ;
+    if (i >= p.rows || j >= p.columns) return;
+    const float* from = p.part + (int64_t)blockIdx.y * p.parts * (kI * kJ) + at;
     Vec<float, 4> z = 0.f;
 #pragma unroll 8
-    for (uint32_t k = 0; k < parts; ++k) z += load_some<float, 4>(p.part + (k * p.rows + i) * p.columns + j, p.columns - j);
+    for (uint32_t k = 0; k < p.parts; ++k) z += load<float, 4>(from + (int64_t)k * (kI * kJ));
     finish<T>(p.to, i, j, z, p.columns - j);
 }
 
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ>
-int launch_tiles(Product p, bool turn_a, bool turn_b, unsigned parts, hipStream_t s) {
+// How a product is cut: tiles of a size, the last of them in parts along the contraction.
+struct Plan {
+    int side = 0;
+    int64_t tiles = 0, whole = 0, parts = 1;
+    double time = 0;  // microseconds, estimated
+};
+constexpr int64_t kComputeUnits = 256;
+
+template <class T>
+Plan plan_of(int64_t rows, int64_t columns, int64_t depth) {
+    constexpr int64_t kDepth = 128 / sizeof(T);
+    // Per k, in nanoseconds: what `at_once` workgroups on a compute unit take at least (a step's way through LDS and its barrier, whatever it multiplies), and what each
+    // adds once they share the matrix cores.  Measured with 2048 and 4096 tokens of 4096 -> 4096 (16 bits), 999 of 2048 -> 4608 (fp32).
+    struct Size {
+        int side, at_once;
+        double alone, each;
+    };
+    constexpr Size wide[] = {{256, 1, 21.0, 30.7}, {128, 2, 10.3, 9.7}, {64, 4, 6.9, 3.4}}, exact[] = {{128, 2, 60.0, 62.0}, {64, 4, 18.0, 17.0}};
+    const int64_t steps = (depth + kDepth - 1) / kDepth;
+    Plan best;
+    const auto consider = [&](const Size& size, int64_t tiles, int64_t whole, int64_t parts) {
+        const auto rounds = [&](int64_t workgroups, double k) {
+            const int64_t most = (workgroups + kComputeUnits - 1) / kComputeUnits;
+            const bool one = workgroups <= kComputeUnits / 2;
+            return k * 1e-3 * std::max((double)((most + size.at_once - 1) / size.at_once) * size.alone, most * (size.at_once == 1 && one ? size.alone : size.each));
+        };
+        double time = 6.0 + (whole ? rounds(whole, (double)depth) : 0.0);
+        if (tiles > whole) {
+            const int64_t of_part = (steps + parts - 1) / parts;
+            time += rounds((tiles - whole) * parts, (double)(of_part * kDepth));
+            if (parts > 1) time += 5.0 + (double)((tiles - whole) * parts) * size.side * size.side * 8 / 2.5e6;  // written and read again, at 2.5 TB/s in bursts
+        }
+        if (!best.side || time < best.time) best = {size.side, tiles, whole, parts, time};
+    };
+    const auto of = [&](const Size& size) {
+        const int64_t tiles = ((rows + size.side - 1) / size.side) * ((columns + size.side - 1) / size.side);
+        consider(size, tiles, tiles, 1);
+        const int64_t room = kComputeUnits * size.at_once, whole = tiles / room * room, left = tiles - whole;
+        if (left == 0) return;
+        for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * left <= room; ++parts) consider(size, tiles, whole, parts);
+    };
+    if constexpr (sizeof(T) == 2) {
+        for (const Size& size : wide) of(size);
+    } else {
+        for (const Size& size : exact) of(size);
+    }
+    return best;
+}
+
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead>
+int launch_tiles(Product p, const Plan& plan, bool turn_a, bool turn_b, hipStream_t s) {
+    constexpr int64_t kDepth = 128 / sizeof(T);
     p.tiles_i = (uint32_t)((p.rows + kI - 1) / kI), p.tiles_j = (uint32_t)((p.columns + kJ - 1) / kJ);
-    const dim3 grid(p.tiles_i * p.tiles_j, parts);
+    const int64_t steps = (p.depth + kDepth - 1) / kDepth, of_part = std::max<int64_t>(1, (steps + plan.parts - 1) / plan.parts), left = plan.tiles - plan.whole;
+    p.whole = (uint32_t)plan.whole;
+    p.parts = (uint32_t)std::max<int64_t>(1, (steps + of_part - 1) / of_part);  // none without a step
+    p.depth_of_part = of_part * kDepth;
+    Temporary t((size_t)left * p.parts * kI * kJ * 4, s);
+    if (t.error) return t.error;
+    p.part = t.floats();
+    const unsigned grid = (unsigned)(plan.whole + left * p.parts);
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false><<<grid, kThreads, 0, s>>>(p);
-    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, true><<<grid, kThreads, 0, s>>>(p);
-    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, true, true><<<grid, kThreads, 0, s>>>(p);
+    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, false><<<grid, kThreads, 0, s>>>(p);
+    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, true><<<grid, kThreads, 0, s>>>(p);
+    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, true, true><<<grid, kThreads, 0, s>>>(p);
+    if (int e = (int)hipGetLastError()) return e;
+    if (left) parts_kernel<T, kI, kJ><<<dim3(kI * kJ / 1024, (unsigned)left), 256, 0, s>>>(p);
     return (int)hipGetLastError();
 }
 
 template <class T>
-int launch_product(Product p, bool turn_a, bool turn_b, hipStream_t s) {
-    constexpr int64_t kDepth = 128 / sizeof(T);
-    const auto tiles = [&](int64_t side) { return ((p.rows + side - 1) / side) * ((p.columns + side - 1) / side); };
-    const int64_t side = sizeof(T) == 2 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64, steps = (p.depth + kDepth - 1) / kDepth;
-    int64_t parts = 1;
-    if (tiles(side) < 384 && side == 64) parts = std::max<int64_t>(1, std::min<int64_t>({768 / tiles(side), steps / 4, 64}));
-    const int64_t of_part = (std::max<int64_t>(steps, 1) + parts - 1) / parts;
-    parts = std::max<int64_t>(1, (steps + of_part - 1) / of_part);
-    p.depth_of_part = of_part * kDepth;
-    Temporary t(parts > 1 ? (size_t)parts * p.rows * p.columns * 4 : 0, s);
-    if (t.error) return t.error;
-    p.part = t.floats();
-    int e;
-    if (side == 64) e = launch_tiles<T, 64, 64, 2, 2>(p, turn_a, turn_b, (unsigned)parts, s);
-    else if (side == 128) e = launch_tiles<T, 128, 128, 2, 2>(p, turn_a, turn_b, (unsigned)parts, s);
-    else if constexpr (sizeof(T) == 2) e = launch_tiles<T, 256, 256, 2, 4>(p, turn_a, turn_b, (unsigned)parts, s);
-    else return (int)hipErrorInvalidValue;
-    if (e || parts == 1) return e;
-    parts_kernel<T><<<(unsigned)((p.rows * ((p.columns + 3) / 4) + 255) / 256), 256, 0, s>>>(p, (uint32_t)parts);
+int launch_product(const Product& p, bool turn_a, bool turn_b, hipStream_t s) {
+    const Plan plan = plan_of<T>(p.rows, p.columns, p.depth);
+    if (plan.side == 64) return launch_tiles<T, 64, 64, 2, 2, 1>(p, plan, turn_a, turn_b, s);
+    if (plan.side == 128) return launch_tiles<T, 128, 128, 2, 2, 1>(p, plan, turn_a, turn_b, s);
+    if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 1>(p, plan, turn_a, turn_b, s);
+    return (int)hipErrorInvalidValue;
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------------------
+// A decode step reads W once and does little else.  A workgroup takes 16 rows of W and every wave a part of the contraction: its operands come from memory in the
+// matrix instruction's own layout, 16 bytes a lane (four lanes have 64 bytes of a row), eight requests of W on their way before
+// the first product.  The waves' sums meet in LDS, in their order.
+template <class T>
+__device__ __forceinline__ F4 multiply16(Chunk a, Chunk b, F4 c) {
+    if constexpr (sizeof(T) == 4) {
+        const F4 x = __builtin_bit_cast(F4, a), y = __builtin_bit_cast(F4, b);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[q], y[q], c, 0, 0, 0);
+        return c;
+    } else if constexpr (__is_same(T, __bf16)) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), __builtin_bit_cast(B8, b), c, 0, 0, 0);
+    } else {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(H8, a), __builtin_bit_cast(H8, b), c, 0, 0, 0);
+    }
+}
+struct FewArgs {
+    const void *w, *x;
+    int64_t ldw, ldx;
+    int64_t tokens, in, out;
+    int64_t lines_of_wave;  // of 128 bytes of k
+    Epilogue to;
+};
+template <class T, int kTiles, bool kColumns>
+__global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
+    constexpr int E = 16 / sizeof(T), kLine = 8 * E, kAtOnce = kTiles > 1 ? 2 : 4;
+    __shared__ Vec<float, 4> room[16][kTiles][64];
+    const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, of = lane & 15, group = lane >> 4;
+    const int64_t row0 = (int64_t)blockIdx.x * 16, row = row0 + of < a.out ? row0 + of : a.out - 1;
+    int64_t k = wave * a.lines_of_wave * kLine;
+    const int64_t last = k + a.lines_of_wave * kLine < a.in ? k + a.lines_of_wave * kLine : a.in;
+    const T* w = static_cast<const T*>(a.w) + row * a.ldw + group * E;
+    const T* x[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+        const int64_t t = n * 16 + of < a.tokens ? n * 16 + of : a.tokens - 1;  // others' results are dropped
+        x[n] = static_cast<const T*>(a.x) + (kColumns ? t + group * E * a.ldx : t * a.ldx + group * E);
+    }
+    const auto chunk_of_x = [&](int n, int64_t at, int64_t left) {
+        if constexpr (kColumns) {
+            Vec<T, E> v;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                v[j] = (T)0.f;
+                if (j < left) v[j] = x[n][(at + j) * a.ldx];
+            }
+            return __builtin_bit_cast(Chunk, v);
+        } else {
+            return __builtin_bit_cast(Chunk, (load_own<T, E>(x[n] + at, left)));
+        }
+    };
+    F4 sums[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) sums[n] = 0.f;
+    for (; k + kAtOnce * kLine <= last; k += kAtOnce * kLine) {
+        Chunk u[kAtOnce * 2], v[kAtOnce * 2][kTiles];
+#pragma unroll
+        for (int q = 0; q < kAtOnce * 2; ++q) u[q] = __builtin_bit_cast(Chunk, (load<T, E>(w + k + q * 4 * E)));
+#pragma unroll
+        for (int q = 0; q < kAtOnce * 2; ++q)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) v[q][n] = chunk_of_x(n, k + q * 4 * E, E);
+#pragma unroll
+        for (int q = 0; q < kAtOnce * 2; ++q)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) sums[n] = multiply16<T>(u[q], v[q][n], sums[n]);
+    }
+    for (; k < last; k += kLine)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int64_t left = last - k - (q * 4 + group) * E;
+            const Chunk u = __builtin_bit_cast(Chunk, (load_own<T, E>(w + k + q * 4 * E, left)));
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) sums[n] = multiply16<T>(u, chunk_of_x(n, k + q * 4 * E, left), sums[n]);
+        }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) room[wave][n][lane] = sums[n];
+    __syncthreads();
+    // lane: token `of` of its tile, features 4 group ..
+    const unsigned waves = blockDim.x >> 6;
+    if (wave >= kTiles) return;
+    const int64_t t = wave * 16 + of, j = row0 + group * 4;
+    if (t >= a.tokens || j >= a.out) return;
+    F4 z = room[0][wave][lane];
+    for (unsigned k = 1; k < waves; ++k) z += room[k][wave][lane];
+    if constexpr (kColumns) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (j + q < a.out) finish<T>(a.to, j + q, t, F4(z[q]), 1);
+    } else {
+        finish<T>(a.to, t, j, z, a.out - j);
+    }
+}
+// Two tiles of 16 tokens only where W is short: there the other kernel's two launches take longer (32 tokens, 640 -> 640 bf16: 6.8 against 11.1 us; 9216 -> 4096 33 against 22).
+// Few rows of a long W leave most compute units without a workgroup (one token, 12800 -> 640: 18 us against 15 in parts).
+bool few_tokens(int64_t tokens, int64_t in, int64_t out, int64_t item) {
+    const bool brief = in * item <= 48 * 128;
+    return tokens <= (brief ? 32 : 16) && (brief || out >= 2048);
+}
+template <class T, bool kColumns>
+int launch_few_tokens(FewArgs a, hipStream_t s) {
+    constexpr int64_t kLine = 128 / sizeof(T);
+    const int64_t lines = (a.in + kLine - 1) / kLine;
+    const int64_t waves = std::min<int64_t>(16, std::max<int64_t>(a.tokens > 16 ? 2 : 1, lines));
+    a.lines_of_wave = (lines + waves - 1) / waves;
+    const unsigned grid = (unsigned)((a.out + 15) / 16), threads = (unsigned)waves * 64;
+    if (a.tokens <= 16) few_tokens_kernel<T, 1, kColumns><<<grid, threads, 0, s>>>(a);
+    else few_tokens_kernel<T, 2, kColumns><<<grid, threads, 0, s>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -404,11 +641,18 @@ __global__ __launch_bounds__(1024) void bias_totals_kernel(const float* part, ui
 template <class T>
 int linear_of(const LinearCall& c, hipStream_t s) {
     const bool columns = c.x.order == CER_ORDER_COLUMNS;
+    const Epilogue to{c.bias, c.bias_type, columns, c.activation, c.residual.data, c.pre.data, c.y.data, c.residual.ld, c.pre.ld, c.y.ld};
+    if (few_tokens(c.tokens, c.in, c.out, sizeof(T))) {
+        const FewArgs a{c.w, c.x.data, c.ldw, c.x.ld, c.tokens, c.in, c.out, 0, to};
+        if constexpr (sizeof(T) == 4)
+            if (columns) return launch_few_tokens<float, true>(a, s);
+        return launch_few_tokens<T, false>(a, s);
+    }
     Product p{};
     p.a = columns ? c.w : c.x.data, p.lda = columns ? c.ldw : c.x.ld;
     p.b = columns ? c.x.data : c.w, p.ldb = columns ? c.x.ld : c.ldw;
     p.rows = columns ? c.out : c.tokens, p.columns = columns ? c.tokens : c.out, p.depth = c.in;
-    p.to = {c.bias, c.bias_type, columns, c.activation, c.residual.data, c.pre.data, c.y.data, c.residual.ld, c.pre.ld, c.y.ld};
+    p.to = to;
     return launch_product<T>(p, false, columns, s);
 }
 
