@@ -10,6 +10,8 @@
 // Activations in columns (the order of cer_matmul's X and Y) are turned through LDS, before and behind: a token's features lie a whole line of
 // tokens apart there.
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "operators.hpp"
 
@@ -52,6 +54,19 @@ __global__ __launch_bounds__(1024) void block_rows_kernel(BlockArgs a) {
             u[c] = load_some<TF, V>(f + e, a.n - e);
             h[c] = load_some<TX, V>(x + e, a.n - e);
         }
+        // few registers: what follows a sum is on its way while the sum is formed
+        constexpr bool kEarly = kChunks * V <= 8;
+        Vec<float, V> w[kEarly ? kChunks : 1];
+        const auto behind = [&](int c) {  // what u is multiplied with
+            const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
+            Vec<float, V> v = a.norm_behind ? numbers_at<V>(a.post, e, a.n) : Vec<float, V>(1.f);
+            if (a.gate) v *= load_some<TX, V>(static_cast<const TX*>(a.gate) + t * a.ldgate + e, a.n - e);
+            else if (a.gate_vector.p) v *= numbers_at<V>(a.gate_vector, e, a.n);
+            return v;
+        };
+        if (kEarly)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) w[kEarly ? c : 0] = behind(c);
         if (a.norm_behind) {
             float squares = 0.f;
 #pragma unroll
@@ -61,22 +76,17 @@ __global__ __launch_bounds__(1024) void block_rows_kernel(BlockArgs a) {
             const float q = rsqrtf(fmaf(block_total(squares, room[turn]), a.inverse_n, a.eps));
             if (a.rstd_post && threadIdx.x == 0) a.rstd_post[t] = q;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-                u[c] *= q;
-                if (a.post.p) u[c] *= numbers_at<V>(a.post, e, a.n);
-            }
+            for (int c = 0; c < kChunks; ++c) u[c] *= q;
         }
         float squares = 0.f;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-            if (a.gate) u[c] *= load_some<TX, V>(static_cast<const TX*>(a.gate) + t * a.ldgate + e, a.n - e);
-            else if (a.gate_vector.p) u[c] *= numbers_at<V>(a.gate_vector, e, a.n);
-            h[c] = h[c] * a.scale + u[c];
+            h[c] = h[c] * a.scale + u[c] * (kEarly ? w[kEarly ? c : 0] : behind(c));
 #pragma unroll
             for (int j = 0; j < V; ++j) squares = fmaf(h[c][j], h[c][j], squares);
             store_some<TX, V>(static_cast<TX*>(a.h) + t * a.ldh + e, h[c], a.n - e);
+            if (kEarly) w[kEarly ? c : 0] = numbers_at<V>(a.pre, e, a.n);
         }
         const float r = rsqrtf(fmaf(block_total(squares, room[turn + 1]), a.inverse_n, a.eps));
         if (a.rstd_pre && threadIdx.x == 0) a.rstd_pre[t] = r;
@@ -84,33 +94,66 @@ __global__ __launch_bounds__(1024) void block_rows_kernel(BlockArgs a) {
         for (int c = 0; c < kChunks; ++c) {
             const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
             h[c] *= r;
-            if (a.pre.p) h[c] *= numbers_at<V>(a.pre, e, a.n);
+            h[c] *= kEarly ? w[kEarly ? c : 0] : numbers_at<V>(a.pre, e, a.n);
             store_some<TY, V>(static_cast<TY*>(a.y) + t * a.ldy + e, h[c], a.n - e);
         }
     }
 }
 
-// to[j * ldt + i] = from[i * ldf + j], i < rows, j < columns: a tile of 64 by 64 through LDS.
-__global__ __launch_bounds__(256) void block_turn_kernel(const float* from, int64_t ldf, int64_t rows, int64_t columns, float* to, int64_t ldt) {
-    __shared__ float tile[64][65];
-    const unsigned tiles = (unsigned)((columns + 63) / 64);
+// to[j * ldt + i] = from[i * ldf + j], i < rows, j < columns, of one matrix or two: a tile of 64 by 64 through LDS, 16 bytes a lane on both sides.
+struct Turn {
+    const float* from;
+    float* to;
+    int64_t ldf, ldt;
+};
+struct Turns {
+    Turn each[2];
+    int64_t rows, columns;
+};
+__global__ __launch_bounds__(256) void block_turn_kernel(Turns w) {
+    __shared__ float tile[64][68];  // [j][i]
+    const Turn m = w.each[blockIdx.y];
+    const unsigned tiles = (unsigned)((w.columns + 63) / 64);
     const int64_t i0 = (int64_t)(blockIdx.x / tiles) * 64, j0 = (int64_t)(blockIdx.x % tiles) * 64;
-    const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned along = threadIdx.x % 16 * 4, line = threadIdx.x / 16;
+    Vec<float, 4> v[4];
 #pragma unroll
-    for (unsigned k = 0; k < 16; ++k) {
-        const int64_t i = i0 + wave * 16 + k, j = j0 + lane;
-        if (i < rows && j < columns) tile[lane][wave * 16 + k] = from[i * ldf + j];
+    for (unsigned k = 0; k < 4; ++k) {
+        const int64_t i = i0 + line + 16 * k, j = j0 + along;
+        v[k] = i < w.rows ? load_some<float, 4>(m.from + i * m.ldf + j, w.columns - j) : Vec<float, 4>(0.f);
     }
+#pragma unroll
+    for (unsigned k = 0; k < 4; ++k)
+#pragma unroll
+        for (unsigned q = 0; q < 4; ++q) tile[along + q][line + 16 * k] = v[k][q];
     __syncthreads();
 #pragma unroll
-    for (unsigned k = 0; k < 16; ++k) {
-        const int64_t j = j0 + wave * 16 + k, i = i0 + lane;
-        if (i < rows && j < columns) to[j * ldt + i] = tile[wave * 16 + k][lane];
+    for (unsigned k = 0; k < 4; ++k) {
+        const int64_t j = j0 + line + 16 * k, i = i0 + along;
+        if (j < w.columns) store_some<float, 4>(m.to + j * m.ldt + i, *reinterpret_cast<const Vec<float, 4>*>(&tile[line + 16 * k][along]), w.rows - i);
     }
 }
-int turn(const float* from, int64_t ldf, int64_t rows, int64_t columns, float* to, int64_t ldt, hipStream_t s) {
-    block_turn_kernel<<<(unsigned)((rows + 63) / 64 * ((columns + 63) / 64)), 256, 0, s>>>(from, ldf, rows, columns, to, ldt);
+int turn(const Turns& w, unsigned many, hipStream_t s) {
+    block_turn_kernel<<<dim3((unsigned)((w.rows + 63) / 64 * ((w.columns + 63) / 64)), many), 256, 0, s>>>(w);
     return (int)hipGetLastError();
+}
+
+// How many workgroups of a kernel the chip holds at once.  A grid of that size takes tokens in turn and reads the next one while others write: 8192 x 4096 bf16 forward
+// 62 us, 67 with a workgroup for each token, 72 - 80 with a grid of two thirds or four thirds of it.
+template <auto kernel>
+unsigned resident(unsigned threads) {
+    static std::atomic<unsigned> known[17];  // by waves
+    unsigned v = known[threads / 64].load(std::memory_order_relaxed);
+    if (!v) {
+        int blocks = 0;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, (int)threads, 0) != hipSuccess || blocks < 1) {
+            (void)hipGetLastError();
+            blocks = 1;
+        }
+        v = 256u * (unsigned)blocks;
+        known[threads / 64].store(v, std::memory_order_relaxed);
+    }
+    return v;
 }
 
 // As few vectors of 16 bytes of the residual stream a thread as the 1024 threads of a workgroup allow, up to 32768 features.
@@ -128,11 +171,15 @@ struct Threads {
 template <class TX, class TF, class TY>
 int block_rows(const BlockArgs& a, hipStream_t s) {
     const Threads w(a.n, 16 / sizeof(TX));
-    const unsigned grid = (unsigned)std::min<int64_t>(a.tokens, 1 << 20);
-    if (w.chunks == 1) block_rows_kernel<TX, TF, TY, 1><<<grid, w.threads, 0, s>>>(a);
-    else if (w.chunks == 2) block_rows_kernel<TX, TF, TY, 2><<<grid, w.threads, 0, s>>>(a);
-    else if (w.chunks == 4) block_rows_kernel<TX, TF, TY, 4><<<grid, w.threads, 0, s>>>(a);
-    else if constexpr (sizeof(TX) == 4) block_rows_kernel<TX, TF, TY, 8><<<grid, w.threads, 0, s>>>(a);
+    const auto launch = [&](auto chunks) {
+        constexpr int kChunks = decltype(chunks)::value;
+        const unsigned grid = (unsigned)std::min<int64_t>(a.tokens, resident<block_rows_kernel<TX, TF, TY, kChunks>>(w.threads));
+        block_rows_kernel<TX, TF, TY, kChunks><<<grid, w.threads, 0, s>>>(a);
+    };
+    if (w.chunks == 1) launch(std::integral_constant<int, 1>());
+    else if (w.chunks == 2) launch(std::integral_constant<int, 2>());
+    else if (w.chunks == 4) launch(std::integral_constant<int, 4>());
+    else if constexpr (sizeof(TX) == 4) launch(std::integral_constant<int, 8>());
     return (int)hipGetLastError();
 }
 
@@ -144,7 +191,7 @@ int block_of(const BlockCall& c, BlockArgs a, hipStream_t s) {
     if (f.error || y.error) return f.error ? f.error : y.error;
     if (f_columns) {
         a.f = f.p, a.ldf = c.n;
-        if (int e = turn(static_cast<const float*>(c.f.data), c.f.ld, c.n, c.tokens, f.floats(), c.n, s)) return e;
+        if (int e = turn({{{static_cast<const float*>(c.f.data), f.floats(), c.f.ld, c.n}, {}}, c.n, c.tokens}, 1, s)) return e;
     }
     if (y_columns) a.y = y.p, a.ldy = c.n;
     int e;
@@ -156,10 +203,13 @@ int block_of(const BlockCall& c, BlockArgs a, hipStream_t s) {
                    : wide_y ? block_rows<TX, TX, float>(a, s) : block_rows<TX, TX, TX>(a, s);
     }
     if (e || !y_columns) return e;
-    return turn(y.floats(), c.n, c.tokens, c.n, static_cast<float*>(c.y.data), c.y.ld, s);
+    return turn({{{y.floats(), static_cast<float*>(c.y.data), c.n, c.y.ld}, {}}, c.tokens, c.n}, 1, s);
 }
 
 // ---- backward -------------------------------------------------------------------------------------------------------------------
+// With K = dy b, B = dsum + r K and W = g a:   d = B - r H c,  so that  n c' = sum d W F = sum B W F - r c sum H W F.  All three sums of a token come from its inputs alone: one
+// pass and one barrier.  Each is off by its own rounding only: |c| is at most mean |K H|, by whose rounding d is off in any order of the steps.
+// Of the sums over tokens, those of da and of a gate vector are one, sum d F, times g and times a; with a gate for every token da's is sum d g F.
 struct BlockBackArgs {
     const void *dy, *h, *f, *gate, *dsum;
     void *dx, *df, *dgate;
@@ -168,117 +218,223 @@ struct BlockBackArgs {
     const float *rstd_post, *rstd_pre;
     Numbers gate_vector, post, pre;
     float scale, inverse_n;
-    float* part[3];  // [workgroups][n] sums over the workgroup's tokens: of dpre, dpost, dgate
-    float* along;    // [tokens] c, where the sums have a launch of their own
-    uint32_t parts;
+    float* part[2];  // [parts][n] sums over a part's tokens: dy H, d F (g)
+    float* means;    // [tokens][2] c and c', where they have a launch of their own
 };
 
-// One token's share of the three sums, from what both kernels have in registers.
-enum { kPre = 0, kPost = 1, kGate = 2 };
-
-// kSums: a workgroup takes tokens blockIdx.x, + gridDim.x, ... and holds its share of the sums over tokens for its own features in registers: no
-// atomics, whose order would change them, and no second pass over the inputs.
-template <class TX, class TF, class TD, int kChunks, bool kSums>
-__global__ __launch_bounds__(1024) void block_back_rows_kernel(BlockBackArgs a) {
-    constexpr int V = 16 / sizeof(TX);
-    __shared__ float room[4][16];
-    unsigned turn = 0;
-    Vec<float, V> sums[3][kSums ? kChunks : 1];
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-        for (int c = 0; c < (kSums ? kChunks : 1); ++c) sums[k][c] = 0.f;
-    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x, turn ^= 2) {
-        const float r = a.rstd_pre[t], q = a.rstd_post ? a.rstd_post[t] : 1.f;
-        Vec<float, V> d[kChunks], hat[kChunks], f[kChunks];
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-            d[c] = load_some<TD, V>(static_cast<const TD*>(a.dy) + t * a.lddy + e, a.n - e);
-            hat[c] = load_some<TX, V>(static_cast<const TX*>(a.h) + t * a.ldh + e, a.n - e);
-            f[c] = load_some<TF, V>(static_cast<const TF*>(a.f) + t * a.ldf + e, a.n - e);
-        }
-        float along = 0.f;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-            hat[c] *= r;
-            f[c] *= q;
-            if constexpr (kSums) sums[kPre][c] += d[c] * hat[c];
-            if (a.pre.p) d[c] *= numbers_at<V>(a.pre, e, a.n);
-#pragma unroll
-            for (int j = 0; j < V; ++j) along = fmaf(d[c][j], hat[c][j], along);
-        }
-        along = block_total(along, room[turn]) * a.inverse_n;
-        if (!kSums && a.along && threadIdx.x == 0) a.along[t] = along;
-        float across = 0.f;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-            d[c] = (d[c] - hat[c] * along) * r;
-            if (a.dsum) d[c] += load_some<TX, V>(static_cast<const TX*>(a.dsum) + t * a.lddsum + e, a.n - e);
-            store_some<TX, V>(static_cast<TX*>(a.dx) + t * a.lddx + e, d[c] * a.scale, a.n - e);
-            const Vec<float, V> w = numbers_at<V>(a.post, e, a.n);
-            if (a.gate) {
-                const Vec<float, V> g = load_some<TX, V>(static_cast<const TX*>(a.gate) + t * a.ldgate + e, a.n - e);
-                if (a.dgate) store_some<TX, V>(static_cast<TX*>(a.dgate) + t * a.lddgate + e, d[c] * f[c] * w, a.n - e);
-                d[c] *= g;
-            } else if (a.gate_vector.p) {
-                if constexpr (kSums) sums[kGate][c] += d[c] * f[c] * w;
-                d[c] *= numbers_at<V>(a.gate_vector, e, a.n);
-            }
-            if constexpr (kSums) sums[kPost][c] += d[c] * f[c];
-            d[c] *= w;
-#pragma unroll
-            for (int j = 0; j < V; ++j) across = fmaf(d[c][j], f[c][j], across);
-        }
-        if (a.rstd_post) across = block_total(across, room[turn + 1]) * a.inverse_n;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-            if (a.rstd_post) d[c] = (d[c] - f[c] * across) * q;
-            store_some<TF, V>(static_cast<TF*>(a.df) + t * a.lddf + e, d[c], a.n - e);
-        }
+// V features of a token as they are in memory.
+template <class TX, class TF, class TD>
+struct BackInputs {
+    static constexpr int V = 16 / sizeof(TX);
+    using F = Vec<float, V>;
+    Vec<TD, V> dy_;
+    Vec<TX, V> h_, dsum_, gate_;
+    Vec<TF, V> f_;
+    __device__ __forceinline__ void request(const BlockBackArgs& a, int64_t t, int64_t e) {
+        const int64_t left = a.n - e;
+        dy_ = load_own<TD, V>(static_cast<const TD*>(a.dy) + t * a.lddy + e, left);
+        h_ = load_own<TX, V>(static_cast<const TX*>(a.h) + t * a.ldh + e, left);
+        f_ = load_own<TF, V>(static_cast<const TF*>(a.f) + t * a.ldf + e, left);
+        if (a.dsum) dsum_ = load_own<TX, V>(static_cast<const TX*>(a.dsum) + t * a.lddsum + e, left);
+        if (a.gate) gate_ = load_own<TX, V>(static_cast<const TX*>(a.gate) + t * a.ldgate + e, left);
     }
-    if constexpr (kSums) {
+};
+// The same in 32 bits, and what is formed of it: B, H, F, W.
+template <class TX, class TF, class TD>
+struct BackToken {
+    static constexpr int V = 16 / sizeof(TX);
+    using F = Vec<float, V>;
+    F base, hat, f, w, gate;
+    float sums[3];
+    // `with_pre`: b; `with_gate`: g a of vectors; both 1 where there are none.  Returns dy H.
+    __device__ __forceinline__ F take(const BackInputs<TX, TF, TD>& in, const BlockBackArgs& a, float r, float q, F with_pre, F with_gate) {
+        const F dy = __builtin_convertvector(in.dy_, F), k = dy * with_pre;
+        hat = __builtin_convertvector(in.h_, F) * r;
+        f = __builtin_convertvector(in.f_, F) * q;
+        base = k * r;
+        if (a.dsum) base += __builtin_convertvector(in.dsum_, F);
+        w = with_gate;
+        if (a.gate) {
+            gate = __builtin_convertvector(in.gate_, F);
+            w *= gate;
+        }
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (a.part[k])
+        for (int j = 0; j < V; ++j) {
+            sums[0] = fmaf(k[j], hat[j], sums[0]);
+            sums[1] = fmaf(base[j] * w[j], f[j], sums[1]);
+            sums[2] = fmaf(hat[j] * w[j], f[j], sums[2]);
+        }
+        return dy * hat;
+    }
+    // Writes what belongs to the token; returns d F (g).
+    __device__ __forceinline__ F give(const BlockBackArgs& a, int64_t t, int64_t e, float r, float q, float c, float across, F with_gate, bool write) {
+        const int64_t left = a.n - e;
+        const F d = base - hat * (r * c);
+        F df = d * w;
+        if (a.rstd_post) df = (df - f * across) * q;
+        F sum = d * f;
+        if (write) {
+            store_some<TX, V>(static_cast<TX*>(a.dx) + t * a.lddx + e, d * a.scale, left);
+            store_some<TF, V>(static_cast<TF*>(a.df) + t * a.lddf + e, df, left);
+            if (a.gate && a.dgate) store_some<TX, V>(static_cast<TX*>(a.dgate) + t * a.lddgate + e, sum * with_gate, left);
+        }
+        if (a.gate) sum *= gate;
+        return sum;
+    }
+};
+// c and c' from the three sums over a token's features.
+__device__ __forceinline__ void means_of(const BlockBackArgs& a, float s0, float s1, float s2, float r, float* c, float* across) {
+    *c = s0 * a.inverse_n;
+    *across = (s1 - r * *c * s2) * a.inverse_n;
+}
+
+// Three totals over the waves of a token; `room`: 48 floats that nothing else uses until the next barrier but one.
+__device__ __forceinline__ void three_totals(float* v, float* room) {
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * V;
-                    store_some<float, V>(a.part[k] + blockIdx.x * a.n + e, sums[k][c], a.n - e);
-                }
+    for (int k = 0; k < 3; ++k) v[k] = wave_total(v[k]);
+    const unsigned waves = blockDim.x >> 6;
+    if (waves == 1) return;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) room[k * 16 + (threadIdx.x >> 6)] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        v[k] = room[k * 16];
+        for (unsigned w = 1; w < waves; ++w) v[k] += room[k * 16 + w];
     }
 }
 
-// Over 8192 features three sums, beside three copies of a token, do not fit the registers of 1024 threads: they are formed here from the inputs again and
-// c of each token.  A workgroup: 64 lanes of V features by 4 waves, each of every fourth token of the workgroup's part.
-template <class TX, class TF, class TD>
-__global__ __launch_bounds__(256) void block_back_sums_kernel(BlockBackArgs a, int64_t tokens_of_part) {
+// Up to 6144 features of 16 bits, 8192 of fp32.  Workgroups take tokens in turn, blockDim.y of them abreast (narrow ones), and hold their share of the sums over tokens for their own features in
+// registers: no atomics, whose order would change them, and no second pass.  The next token's inputs are requested before this one's are used; the weights lie in LDS,
+// each thread's where only it reads them.
+// (1024 threads with eight features each have no registers for the next token's inputs.)  4096 x 4608 bf16: 66 us, 5 of them the totals; with two sums and barriers a
+// token, and one a token at a time, 92.
+constexpr int kMostThreads = 1024;
+template <class TX, class TF, class TD, int kChunks, int kThreads>
+__global__ __launch_bounds__(kThreads) void block_back_rows_kernel(BlockBackArgs a) {
     constexpr int V = 16 / sizeof(TX);
-    __shared__ Vec<float, V> room[4][64];
-    const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t e = ((int64_t)blockIdx.x * 64 + lane) * V;
-    const int64_t first = blockIdx.y * tokens_of_part, last = first + tokens_of_part < a.tokens ? first + tokens_of_part : a.tokens;
-    Vec<float, V> sums[3] = {Vec<float, V>(0.f), Vec<float, V>(0.f), Vec<float, V>(0.f)};
-    if (e < a.n) {
-        const Vec<float, V> pre = numbers_at<V>(a.pre, e, a.n), post = numbers_at<V>(a.post, e, a.n), gate = numbers_at<V>(a.gate_vector, e, a.n);
-        for (int64_t t = first + wave; t < last; t += 4) {
-            const float r = a.rstd_pre[t], q = a.rstd_post ? a.rstd_post[t] : 1.f;
-            const Vec<float, V> dy = load_some<TD, V>(static_cast<const TD*>(a.dy) + t * a.lddy + e, a.n - e);
-            const Vec<float, V> hat = load_some<TX, V>(static_cast<const TX*>(a.h) + t * a.ldh + e, a.n - e) * r;
-            const Vec<float, V> f = load_some<TF, V>(static_cast<const TF*>(a.f) + t * a.ldf + e, a.n - e) * q;
-            sums[kPre] += dy * hat;
-            Vec<float, V> d = (dy * pre - hat * a.along[t]) * r;
-            if (a.dsum) d += load_some<TX, V>(static_cast<const TX*>(a.dsum) + t * a.lddsum + e, a.n - e);
-            sums[kGate] += d * f * post;
-            d *= a.gate ? load_some<TX, V>(static_cast<const TX*>(a.gate) + t * a.ldgate + e, a.n - e) : gate;
-            sums[kPost] += d * f;
+    constexpr bool kNext = kThreads < kMostThreads || kChunks == 1;
+    using F = Vec<float, V>;
+    extern __shared__ __align__(16) float lds[];
+    __shared__ float room[2][kThreads / 64][48];
+    F *with_pre = reinterpret_cast<F*>(lds), *with_gate = with_pre + kChunks * blockDim.x;
+    const auto feature = [&](int c) { return ((int64_t)c * blockDim.x + threadIdx.x) * V; };
+    const unsigned group = threadIdx.y, groups = blockDim.y;
+    const auto token = [&](int64_t first) { return first + group < a.tokens ? first + group : a.tokens - 1; };  // a group without one repeats the last
+    BackInputs<TX, TF, TD> in[kChunks];
+    float next_r, next_q;
+    const auto request = [&](int64_t t) {
+        next_r = a.rstd_pre[t], next_q = a.rstd_post ? a.rstd_post[t] : 1.f;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) in[c].request(a, t, feature(c));
+    };
+    if (kNext) request(token((int64_t)blockIdx.x * groups));
+    if (group == 0)
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            with_pre[c * blockDim.x + threadIdx.x] = numbers_at<V>(a.pre, feature(c), a.n);
+            with_gate[c * blockDim.x + threadIdx.x] = numbers_at<V>(a.post, feature(c), a.n) * numbers_at<V>(a.gate_vector, feature(c), a.n);
+        }
+    if (groups > 1) __syncthreads();
+    F sums[2][kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) sums[0][c] = sums[1][c] = 0.f;
+    unsigned turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * groups; first < a.tokens; first += (int64_t)gridDim.x * groups, turn ^= 1) {
+        const int64_t t = token(first);
+        const bool real = first + group < a.tokens;
+        if (!kNext) request(t);
+        const float r = next_r, q = next_q;
+        BackToken<TX, TF, TD> of[kChunks];
+        float totals[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) of[c].sums[k] = 0.f;
+            const F v = of[c].take(in[c], a, r, q, with_pre[c * blockDim.x + threadIdx.x], with_gate[c * blockDim.x + threadIdx.x]);
+            if (real) sums[0][c] += v;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) totals[k] += of[c].sums[k];
+        }
+        if (kNext) {
+            request(token(first + (int64_t)gridDim.x * groups));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        three_totals(totals, room[turn][group]);
+        float c0, across;
+        means_of(a, totals[0], totals[1], totals[2], r, &c0, &across);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const F v = of[c].give(a, t, feature(c), r, q, c0, across, with_gate[c * blockDim.x + threadIdx.x], real);
+            if (real) sums[1][c] += v;
         }
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            if (!a.part[k]) continue;
+            if (groups > 1) {
+                F* joined = reinterpret_cast<F*>(lds);
+                __syncthreads();
+                joined[group * blockDim.x + threadIdx.x] = sums[k][c];
+                __syncthreads();
+                for (unsigned g = 1; g < groups && group == 0; ++g) sums[k][c] += joined[g * blockDim.x + threadIdx.x];
+            }
+            if (group == 0) store_some<float, V>(a.part[k] + blockIdx.x * a.n + feature(c), sums[k][c], a.n - feature(c));
+        }
+}
+
+// Over that a token and the sums over tokens do not fit the registers of 1024 threads together.  Two launches then, both of which read the inputs: a workgroup for
+// the means of a token, and a workgroup for 64 lanes' features of many tokens, which needs no sum over features any more (1024 x 25088 bf16 102 us, fp32 212; in one launch with
+// spilled registers, and the sums in another, 231 and 437).
+template <class TX, class TF, class TD>
+__global__ __launch_bounds__(512) void block_back_means_kernel(BlockBackArgs a) {
+    constexpr int V = 16 / sizeof(TX);
+    using F = Vec<float, V>;
+    __shared__ float room[2][48];
+    unsigned turn = 0;
+    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x, turn ^= 1) {
+        const float r = a.rstd_pre[t], q = a.rstd_post ? a.rstd_post[t] : 1.f;
+        BackToken<TX, TF, TD> of;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) of.sums[k] = 0.f;
+#pragma unroll 2
+        for (int64_t e = (int64_t)threadIdx.x * V; e < a.n; e += (int64_t)blockDim.x * V) {
+            BackInputs<TX, TF, TD> in;
+            in.request(a, t, e);
+            of.take(in, a, r, q, numbers_at<V>(a.pre, e, a.n), numbers_at<V>(a.post, e, a.n) * numbers_at<V>(a.gate_vector, e, a.n));
+        }
+        three_totals(of.sums, room[turn]);
+        float c, across;
+        means_of(a, of.sums[0], of.sums[1], of.sums[2], r, &c, &across);
+        if (threadIdx.x == 0) a.means[2 * t] = c, a.means[2 * t + 1] = across;
+    }
+}
+template <class TX, class TF, class TD>
+__global__ __launch_bounds__(256) void block_back_strips_kernel(BlockBackArgs a, int64_t tokens_of_part) {
+    constexpr int V = 16 / sizeof(TX);
+    using F = Vec<float, V>;
+    __shared__ F room[4][64];
+    const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t e = ((int64_t)blockIdx.x * 64 + lane) * V;
+    const int64_t first = blockIdx.y * tokens_of_part, last = first + tokens_of_part < a.tokens ? first + tokens_of_part : a.tokens;
+    F sums[2] = {F(0.f), F(0.f)};
+    if (e < a.n) {
+        const F with_pre = numbers_at<V>(a.pre, e, a.n), with_gate = numbers_at<V>(a.post, e, a.n) * numbers_at<V>(a.gate_vector, e, a.n);
+#pragma unroll 2
+        for (int64_t t = first + wave; t < last; t += 4) {
+            BackInputs<TX, TF, TD> in;
+            in.request(a, t, e);
+            const float r = a.rstd_pre[t], q = a.rstd_post ? a.rstd_post[t] : 1.f;
+            BackToken<TX, TF, TD> of;
+            sums[0] += of.take(in, a, r, q, with_pre, with_gate);
+            sums[1] += of.give(a, t, e, r, q, a.means[2 * t], a.means[2 * t + 1], with_gate, true);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
         if (!a.part[k]) continue;
         room[wave][lane] = sums[k];
         __syncthreads();
@@ -287,16 +443,17 @@ __global__ __launch_bounds__(256) void block_back_sums_kernel(BlockBackArgs a, i
     }
 }
 
-struct ThreeSums {
-    const float* part[3];
-    float* out[3];
+struct Totals {
+    const float* part[2];
+    float *pre, *post, *gate;  // wanted where not null
+    Numbers with_gate, with_post;
 };
 // The parts added up in their order.  Workgroup (b, k): 64 features of sum k, 16 lanes of four features by 64 rows of parts.
-__global__ __launch_bounds__(1024) void block_back_totals_kernel(ThreeSums w, uint32_t parts, int64_t n) {
+__global__ __launch_bounds__(1024) void block_back_totals_kernel(Totals w, uint32_t parts, int64_t n) {
     __shared__ Vec<float, 4> room[64][17];
-    const float* part = w.part[blockIdx.y];
-    float* out = w.out[blockIdx.y];
-    if (!out) return;
+    const bool second = blockIdx.y == 1;
+    if (second ? !w.post && !w.gate : !w.pre) return;
+    const float* part = w.part[second];
     const unsigned lane = threadIdx.x & 15, row = threadIdx.x >> 4;
     const int64_t i = (int64_t)blockIdx.x * 64 + lane * 4;
     Vec<float, 4> all = 0.f;
@@ -310,66 +467,70 @@ __global__ __launch_bounds__(1024) void block_back_totals_kernel(ThreeSums w, ui
         if (row < k) room[row][lane] += room[row + k][lane];
         __syncthreads();
     }
-    if (row == 0 && i < n) store_some<float, 4>(out + i, room[0][lane], n - i);
+    if (row != 0 || i >= n) return;
+    all = room[0][lane];
+    if (!second) {
+        store_some<float, 4>(w.pre + i, all, n - i);
+        return;
+    }
+    // without tokens nothing is multiplied: an infinite weight is no reason for a NaN
+    if (w.post) store_some<float, 4>(w.post + i, parts ? all * numbers_at<4>(w.with_gate, i, n) : all, n - i);
+    if (w.gate) store_some<float, 4>(w.gate + i, parts ? all * numbers_at<4>(w.with_post, i, n) : all, n - i);
 }
 
-template <class TX, class TF, class TD, int kChunks, bool kSums>
-int block_back_launch(const BlockBackArgs& a, unsigned threads, hipStream_t s) {
-    const unsigned grid = kSums ? a.parts : (unsigned)std::min<int64_t>(a.tokens, 1 << 20);
-    block_back_rows_kernel<TX, TF, TD, kChunks, kSums><<<grid, threads, 0, s>>>(a);
-    return (int)hipGetLastError();
-}
-
+constexpr unsigned kFewThreads = 768;  // up to here a thread has 168 registers
 template <class TX, class TF, class TD>
-int block_back_rows(BlockBackArgs a, const ThreeSums& outs, hipStream_t s) {
+int block_back_rows(BlockBackArgs a, Totals totals, hipStream_t s) {
     constexpr int V = 16 / sizeof(TX);
     const Threads w(a.n, V);
-    const int wanted = (outs.out[0] != nullptr) + (outs.out[1] != nullptr) + (outs.out[2] != nullptr);
-    const bool inside = a.n <= 8192;  // eight features a thread
+    // 1024 threads with eight features each spill: 2048 x 8192 bf16 80 us here, 72 in strips; with four or eight of fp32 they do not, or hardly (2000 x 7680: 94 us, 110).
+    const bool inside = w.threads <= kFewThreads ? w.chunks == 1 : V == 4 && a.n <= 8192, sums[2] = {totals.pre != nullptr, totals.post || totals.gate};
+    const unsigned groups = inside && w.threads <= kFewThreads ? (unsigned)std::min<int64_t>(kFewThreads / w.threads, (a.tokens + 255) / 256) : 1;
     const int64_t tokens_of_part = (a.tokens + 63) / 64;
-    a.parts = (unsigned)(inside ? std::min<int64_t>(a.tokens, 512) : (a.tokens + tokens_of_part - 1) / tokens_of_part);
-    Temporary parts((size_t)wanted * a.parts * a.n * 4, s), along(wanted && !inside ? (size_t)a.tokens * 4 : 0, s);
-    if (parts.error || along.error) return parts.error ? parts.error : along.error;
-    ThreeSums sums = outs;
-    for (int k = 0, at = 0; k < 3; ++k) {
-        a.part[k] = outs.out[k] ? parts.floats() + (size_t)at++ * a.parts * a.n : nullptr;
-        sums.part[k] = a.part[k];
-    }
-    a.along = along.floats();
-    int e;
+    const unsigned parts = (unsigned)(inside ? std::min<int64_t>((a.tokens + groups - 1) / groups, 256) : (a.tokens + tokens_of_part - 1) / tokens_of_part);
+    Temporary room((size_t)(sums[0] + sums[1]) * parts * a.n * 4, s), means(inside ? 0 : (size_t)a.tokens * 8, s);
+    if (room.error || means.error) return room.error ? room.error : means.error;
+    for (int k = 0, at = 0; k < 2; ++k) totals.part[k] = a.part[k] = sums[k] ? room.floats() + (size_t)at++ * parts * a.n : nullptr;
+    a.means = means.floats();
     if (inside) {
-        if (w.chunks == 1) e = block_back_launch<TX, TF, TD, 1, true>(a, w.threads, s);
-        else if constexpr (V == 4) e = block_back_launch<TX, TF, TD, 2, true>(a, w.threads, s);
-        else return (int)hipErrorInvalidValue;
-    } else {
-        if (w.chunks == 2) e = block_back_launch<TX, TF, TD, 2, false>(a, w.threads, s);
-        else if (w.chunks == 4) e = block_back_launch<TX, TF, TD, 4, false>(a, w.threads, s);
-        else if constexpr (V == 4) e = block_back_launch<TX, TF, TD, 8, false>(a, w.threads, s);
-        else return (int)hipErrorInvalidValue;
-        if (!e && wanted) {
-            block_back_sums_kernel<TX, TF, TD><<<dim3((unsigned)((a.n + 64 * V - 1) / (64 * V)), a.parts), 256, 0, s>>>(a, tokens_of_part);
-            e = (int)hipGetLastError();
+        const dim3 block(w.threads, groups);
+        const auto bytes = [&](int chunks) { return (size_t)V * 4 * w.threads * std::max<size_t>(2 * chunks, groups > 1 ? groups : 0); };
+        if (w.threads <= kFewThreads && w.chunks == 1) block_back_rows_kernel<TX, TF, TD, 1, kFewThreads><<<parts, block, bytes(1), s>>>(a);
+        else if constexpr (V == 4) {
+            if (w.chunks == 1) block_back_rows_kernel<TX, TF, TD, 1, kMostThreads><<<parts, block, bytes(1), s>>>(a);
+            else block_back_rows_kernel<TX, TF, TD, 2, kMostThreads><<<parts, block, bytes(2), s>>>(a);
+        } else {
+            return (int)hipErrorInvalidValue;
         }
+    } else {
+        block_back_means_kernel<TX, TF, TD><<<(unsigned)std::min<int64_t>(a.tokens, 1 << 20), 512, 0, s>>>(a);
+        if (int e = (int)hipGetLastError()) return e;
+        block_back_strips_kernel<TX, TF, TD><<<dim3((unsigned)((a.n + 64 * V - 1) / (64 * V)), parts), 256, 0, s>>>(a, tokens_of_part);
     }
-    if (e || !wanted) return e;
-    block_back_totals_kernel<<<dim3((unsigned)((a.n + 63) / 64), 3), 1024, 0, s>>>(sums, a.parts, a.n);
+    if (int e = (int)hipGetLastError()) return e;
+    if (!sums[0] && !sums[1]) return 0;
+    block_back_totals_kernel<<<dim3((unsigned)((a.n + 63) / 64), 2), 1024, 0, s>>>(totals, parts, a.n);
     return (int)hipGetLastError();
 }
 
 template <class TX>
-int block_back_of(const BlockBackwardCall& c, BlockBackArgs a, const ThreeSums& outs, hipStream_t s) {
+int block_back_of(const BlockBackwardCall& c, BlockBackArgs a, const Totals& outs, hipStream_t s) {
     const bool dy_columns = c.dy.order == CER_ORDER_COLUMNS, f_columns = c.f.order == CER_ORDER_COLUMNS;
     const size_t room = (size_t)c.tokens * c.n * 4;
     Temporary dy(dy_columns ? room : 0, s), f(f_columns ? room : 0, s), df(f_columns ? room : 0, s);
     if (dy.error || f.error || df.error) return dy.error ? dy.error : f.error ? f.error : df.error;
+    Turns w{{}, c.n, c.tokens};
+    unsigned many = 0;
     if (dy_columns) {
         a.dy = dy.p, a.lddy = c.n;
-        if (int e = turn(static_cast<const float*>(c.dy.data), c.dy.ld, c.n, c.tokens, dy.floats(), c.n, s)) return e;
+        w.each[many++] = {static_cast<const float*>(c.dy.data), dy.floats(), c.dy.ld, c.n};
     }
     if (f_columns) {
         a.f = f.p, a.df = df.p, a.ldf = a.lddf = c.n;
-        if (int e = turn(static_cast<const float*>(c.f.data), c.f.ld, c.n, c.tokens, f.floats(), c.n, s)) return e;
+        w.each[many++] = {static_cast<const float*>(c.f.data), f.floats(), c.f.ld, c.n};
     }
+    if (many)
+        if (int e = turn(w, many, s)) return e;
     int e;
     if constexpr (sizeof(TX) == 4) {
         e = block_back_rows<float, float, float>(a, outs, s);
@@ -379,7 +540,7 @@ int block_back_of(const BlockBackwardCall& c, BlockBackArgs a, const ThreeSums& 
                    : wide_dy ? block_back_rows<TX, TX, float>(a, outs, s) : block_back_rows<TX, TX, TX>(a, outs, s);
     }
     if (e || !f_columns) return e;
-    return turn(df.floats(), c.n, c.tokens, c.n, static_cast<float*>(c.df.data), c.df.ld, s);
+    return turn({{{df.floats(), static_cast<float*>(c.df.data), c.n, c.df.ld}, {}}, c.tokens, c.n}, 1, s);
 }
 }  // namespace
 
@@ -398,10 +559,10 @@ int launch_block_norm(const BlockCall& c, hipStream_t s) {
 }
 
 int launch_block_norm_backward(const BlockBackwardCall& c, hipStream_t s) {
-    const ThreeSums outs{{nullptr, nullptr, nullptr}, {c.dpre_weight, c.dpost_weight, c.dgate_vector}};
+    const Totals outs{{nullptr, nullptr}, c.dpre_weight, c.dpost_weight, c.dgate_vector, {c.gate_vector, c.gate_vector_type}, {c.post_weight, c.post_weight_type}};
     if (c.tokens == 0) {
         if (!c.dpre_weight && !c.dpost_weight && !c.dgate_vector) return 0;
-        block_back_totals_kernel<<<dim3((unsigned)((c.n + 63) / 64), 3), 1024, 0, s>>>(outs, 0, c.n);
+        block_back_totals_kernel<<<dim3((unsigned)((c.n + 63) / 64), 2), 1024, 0, s>>>(outs, 0, c.n);
         return (int)hipGetLastError();
     }
     BlockBackArgs a{};

@@ -117,7 +117,7 @@ def backward(tokens, n, dtype, branch, gate="features", post=True, columns=(Fals
     near(df, want, off + SMALLEST[branch], HALF[branch])
 
 
-@pytest.mark.parametrize("tokens,n", SIZES + [(2, 8192), (2, 8193), (70, 12001), (2, 20000), (2, 32768)])
+@pytest.mark.parametrize("tokens,n", SIZES + [(2, 8192), (2, 8193), (70, 12001), (2, 20000), (2, 32768), (300, 6144), (300, 6145), (1500, 130), (3100, 40), (700, 1000)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_backward(tokens, n, dtype):
     backward(tokens, n, dtype, dtype)
