@@ -13,6 +13,7 @@
 // then has four neighbouring j of one i.  fp32 goes through the 32-bit instruction.  Sums are fp32; each C is rounded once, after the epilogue.
 // Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "operators.hpp"
 
@@ -83,10 +84,9 @@ struct Product {
     int64_t lda, ldb;  // from a row to the next, or from one k to the next
     int64_t rows, columns, depth;
     Epilogue to;
-    uint32_t tiles_i, tiles_j;
-    uint32_t whole, parts;  // the first `whole` tiles go through the epilogue; the contraction of the others is cut into parts
+    uint32_t tiles_i, tiles_j, parts;  // more than one: the contraction of every tile is cut
     int64_t depth_of_part;
-    float* part;            // [tiles - whole][parts][rows of a tile][columns of a tile]
+    float* part;  // [tiles][parts][rows of a tile][columns of a tile]
 };
 
 // Four neighbouring j of row i, `left` of them in the matrix.
@@ -101,8 +101,8 @@ __device__ __forceinline__ void finish(const Epilogue& to, int64_t i, int64_t j,
     store_some<T, 4>(static_cast<T*>(to.out) + i * to.ldo + j, z, left);
 }
 
-// Where chunk c of a row lies: eight neighbouring rows, and eight rows four apart, have the same chunk in different places.
-__device__ __forceinline__ unsigned place(unsigned row, unsigned c) { return row * 8 + (c ^ (row & 7) ^ (row >> 3 & 3)); }
+// Where chunk c of a row lies: eight neighbouring rows, and eight rows four or eight apart, have the same chunk in different places.
+__device__ __forceinline__ unsigned place(unsigned row, unsigned c) { return row * 8 + (c ^ (row & 7) ^ (row >> 3 & 7)); }
 
 // Sixteen bytes of k of 32 rows on either side: lanes 0 - 31 have the lower chunk, 32 - 63 the next one.
 template <class T>
@@ -121,31 +121,31 @@ __device__ __forceinline__ F16 multiply(Chunk a, Chunk b, F16 c) {
 
 // One operand's way from memory to LDS: kRows rows of 128 bytes of k, kAhead tiles of them on their way in registers.  Of rows past the matrix any others are
 // read in their place (their results are dropped); k past the end is 0 on both sides.
-template <class T, int kRows, int kThreads, bool kTurn, int kAhead>
+template <class T, int kRows, int kThreads, bool kTurn, int kAhead, int kLine = 4>
 struct Stage {
     static constexpr int E = 16 / sizeof(T), kDepth = 8 * E;
-    static constexpr int kPieces = kTurn ? kRows * 2 : kRows * 8, kCount = (kPieces + kThreads - 1) / kThreads;  // turned: 4 rows by a chunk
+    static constexpr int kPieces = kTurn ? kRows / kLine * 8 : kRows * 8, kCount = (kPieces + kThreads - 1) / kThreads;  // turned: kLine rows by a chunk
     const T* at[kCount];
-    uint32_t to[kCount][kTurn ? 4 : 1];  // chunks of LDS
+    uint32_t to[kCount][kTurn ? kLine : 1];  // chunks of LDS
     Chunk held[kAhead][kTurn ? 1 : kCount];
-    Vec<T, 4> lines[kAhead][kTurn ? kCount : 1][kTurn ? E : 1];
+    Vec<T, kLine> lines[kAhead][kTurn ? kCount : 1][kTurn ? E : 1];
 
-    static __device__ __forceinline__ unsigned piece(int n) { return threadIdx.x + n * kThreads; }
+    static __device__ __forceinline__ unsigned piece(int n) { return threadIdx.x % kThreads + n * kThreads; }
     static __device__ __forceinline__ bool busy(int n) { return kPieces % kThreads == 0 || piece(n) < (unsigned)kPieces; }
-    static __device__ __forceinline__ unsigned row(int n) { return kTurn ? piece(n) % (kRows / 4) * 4 : piece(n) / 8; }
-    static __device__ __forceinline__ unsigned chunk(int n) { return kTurn ? piece(n) / (kRows / 4) : piece(n) % 8; }
+    static __device__ __forceinline__ unsigned row(int n) { return kTurn ? piece(n) % (kRows / kLine) * kLine : piece(n) / 8; }
+    static __device__ __forceinline__ unsigned chunk(int n) { return kTurn ? piece(n) / (kRows / kLine) : piece(n) % 8; }
 
-    // Turned, four rows are read at once: the last four instead of any that pass the end, where the tile has four.
-    static __device__ __forceinline__ bool inside(int64_t row0, int64_t rows) { return !kTurn || rows - row0 >= 4; }
+    // Turned, kLine rows are read at once: the last ones instead of any that pass the end, where the tile has as many.
+    static __device__ __forceinline__ bool inside(int64_t row0, int64_t rows) { return !kTurn || rows - row0 >= kLine; }
     __device__ __forceinline__ void start(const void* base, int64_t ld, int64_t row0, int64_t rows, int64_t k0) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             const int64_t k = k0 + chunk(n) * E, most = rows - row0;
             if constexpr (kTurn) {
-                const int i = inside(row0, rows) && row(n) + 4 > most ? (int)most - 4 : (int)row(n);
+                const int i = inside(row0, rows) && row(n) + kLine > most ? (int)most - kLine : (int)row(n);
                 at[n] = static_cast<const T*>(base) + k * ld + row0 + i;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) to[n][r] = place(i + r, chunk(n));
+                for (int r = 0; r < kLine; ++r) to[n][r] = place(i + r, chunk(n));
             } else {
                 at[n] = static_cast<const T*>(base) + (row0 + (row(n) < most ? row(n) : most - 1)) * ld + k;
                 to[n][0] = place(row(n), chunk(n));
@@ -159,21 +159,21 @@ struct Stage {
             if (!busy(n)) continue;
             if constexpr (kTurn) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) lines[slot][n][q] = load<T, 4>(at[n] + q * ld);
+                for (int q = 0; q < E; ++q) lines[slot][n][q] = load<T, kLine>(at[n] + q * ld);
             } else {
                 held[slot][n] = __builtin_bit_cast(Chunk, (load<T, E>(at[n])));
             }
         }
     }
-    // The same where `remain` of k are left, and (turned) fewer than four rows may be.
+    // The same where `remain` of k are left, and (turned) fewer than kLine rows may be.
     __device__ __forceinline__ void load_some(int slot, int64_t ld, int64_t remain, int64_t row0, int64_t rows) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             if (!busy(n)) continue;
-            const int64_t k = remain - chunk(n) * E, most = inside(row0, rows) ? 4 : rows - row0 - row(n);
+            const int64_t k = remain - chunk(n) * E, most = inside(row0, rows) ? kLine : rows - row0 - row(n);
             if constexpr (kTurn) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) lines[slot][n][q] = load_own<T, 4>(at[n] + q * ld, q < k ? most : 0);
+                for (int q = 0; q < E; ++q) lines[slot][n][q] = load_own<T, kLine>(at[n] + q * ld, q < k ? most : 0);
             } else {
                 held[slot][n] = __builtin_bit_cast(Chunk, (load_own<T, E>(at[n], k)));
             }
@@ -189,7 +189,7 @@ struct Stage {
             if (!busy(n)) continue;
             if constexpr (kTurn) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < kLine; ++r) {
                     Vec<T, E> line;
 #pragma unroll
                     for (int q = 0; q < E; ++q) line[q] = lines[slot][n][q][r];
@@ -199,6 +199,73 @@ struct Stage {
                 room[to[n][0]] = held[slot][n];
             }
         }
+    }
+};
+
+// Both operands' way.  Where both are turned and the halves of the workgroup can take one each, a thread has eight rows of one of them and not four of both: 16 bytes
+// of a line and not 8, in half as many requests (dW of 4096 tokens, 4096 -> 9216 bf16: 370 -> 343 us).
+template <class T, int kI, int kJ, int kThreads, int kAhead, bool kTurnA, bool kTurnB>
+struct Operands {
+    using A = Stage<T, kI, kThreads, kTurnA, kAhead>;
+    using B = Stage<T, kJ, kThreads, kTurnB, kAhead>;
+    A a;
+    B b;
+    __device__ __forceinline__ bool inside(const Product& p, int64_t i0, int64_t j0) const { return A::inside(i0, p.rows) && B::inside(j0, p.columns); }
+    __device__ __forceinline__ void start(const Product& p, int64_t i0, int64_t j0, int64_t k0) {
+        a.start(p.a, p.lda, i0, p.rows, k0);
+        b.start(p.b, p.ldb, j0, p.columns, k0);
+    }
+    __device__ __forceinline__ void load_whole(int slot, const Product& p) {
+        a.load_whole(slot, p.lda);
+        b.load_whole(slot, p.ldb);
+    }
+    __device__ __forceinline__ void load_some(int slot, const Product& p, int64_t remain, int64_t i0, int64_t j0) {
+        a.load_some(slot, p.lda, remain, i0, p.rows);
+        b.load_some(slot, p.ldb, remain, j0, p.columns);
+    }
+    __device__ __forceinline__ void advance(const Product& p) {
+        a.advance(p.lda);
+        b.advance(p.ldb);
+    }
+    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const {
+        a.to_lds(slot, room);
+        b.to_lds(slot, room + kI * 8);
+    }
+    // One of the two steps in which a tile is exchanged.
+    __device__ __forceinline__ void exchange(unsigned step, int slot, Chunk* room, const Product& p, bool more) {
+        if (step == 0) {
+            a.to_lds(slot, room);
+            if (more) a.advance(p.lda);
+            a.load_whole(slot, p.lda);
+        } else {
+            b.to_lds(slot, room + kI * 8);
+            if (more) b.advance(p.ldb);
+            b.load_whole(slot, p.ldb);
+        }
+    }
+};
+template <class T, int kSide, int kThreads, int kAhead>
+struct Halves {
+    using S = Stage<T, kSide, kThreads / 2, true, kAhead, 8>;
+    S s;
+    int64_t ld;
+    __device__ __forceinline__ static bool second() { return __builtin_amdgcn_readfirstlane(threadIdx.x / (kThreads / 2)); }
+    __device__ __forceinline__ bool inside(const Product& p, int64_t i0, int64_t j0) const { return S::inside(i0, p.rows) && S::inside(j0, p.columns); }
+    __device__ __forceinline__ void start(const Product& p, int64_t i0, int64_t j0, int64_t k0) {
+        ld = second() ? p.ldb : p.lda;
+        s.start(second() ? p.b : p.a, ld, second() ? j0 : i0, second() ? p.columns : p.rows, k0);
+    }
+    __device__ __forceinline__ void load_whole(int slot, const Product&) { s.load_whole(slot, ld); }
+    __device__ __forceinline__ void load_some(int slot, const Product& p, int64_t remain, int64_t i0, int64_t j0) {
+        s.load_some(slot, ld, remain, second() ? j0 : i0, second() ? p.columns : p.rows);
+    }
+    __device__ __forceinline__ void advance(const Product&) { s.advance(ld); }
+    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const { s.to_lds(slot, room + (second() ? kSide * 8 : 0)); }
+    __device__ __forceinline__ void exchange(unsigned step, int slot, Chunk* room, const Product&, bool more) {
+        if (step != 0) return;
+        s.to_lds(slot, room + (second() ? kSide * 8 : 0));
+        if (more) s.advance(ld);
+        s.load_whole(slot, ld);
     }
 };
 
@@ -221,35 +288,33 @@ template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead, bool kT
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
-    using StageA = Stage<T, kI, kThreads, kTurnA, kAhead>;
-    using StageB = Stage<T, kJ, kThreads, kTurnB, kAhead>;
-    constexpr int kDepth = StageA::kDepth;
+    constexpr int kDepth = 128 / sizeof(T);
+    using Way = std::conditional_t<kTurnA && kTurnB && sizeof(T) == 2 && kI == kJ && kI / 8 * 8 % (kThreads / 2) == 0, Halves<T, kI, kThreads, kAhead>,
+                                   Operands<T, kI, kJ, kThreads, kAhead, kTurnA, kTurnB>>;
     __shared__ Chunk room[2][(kI + kJ) * 8];
     static_assert(sizeof(room) >= sizeof(float) * kWavesI * kWavesJ * 32 * kPitch, "");
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wave_i = wave / kWavesJ, wave_j = wave % kWavesJ;
-    const bool cut = blockIdx.x >= p.whole;
-    const unsigned piece = cut ? blockIdx.x - p.whole : 0;
+    const bool cut = p.parts > 1;
+    const unsigned piece = blockIdx.x;
     unsigned ti, tj;
-    tile_of(cut ? p.whole + piece / p.parts : on_dies(blockIdx.x, p.whole), p.tiles_i, p.tiles_j, &ti, &tj);
+    tile_of(cut ? piece / p.parts : on_dies(piece, p.tiles_i * p.tiles_j), p.tiles_i, p.tiles_j, &ti, &tj);
     const int64_t i0 = (int64_t)ti * kI, j0 = (int64_t)tj * kJ, k0 = cut ? piece % p.parts * p.depth_of_part : 0;
     int64_t remain = cut && p.depth - k0 > p.depth_of_part ? p.depth_of_part : p.depth - k0;
-    StageA a;
-    StageB b;
-    a.start(p.a, p.lda, i0, p.rows, k0);
-    b.start(p.b, p.ldb, j0, p.columns, k0);
+    Way way;
+    way.start(p, i0, j0, k0);
     F16 sums[kTilesI][kTilesJ];
 #pragma unroll
     for (int x = 0; x < kTilesI; ++x)
 #pragma unroll
         for (int y = 0; y < kTilesJ; ++y) sums[x][y] = 0.f;
-    const unsigned at_lane = place(lane & 31, lane >> 5);  // chunk 2 . step + (lane >> 5): the permutation is an exclusive or
+    // chunk 2 . step + (lane >> 5) of row lane & 31 of an even or odd 32 rows: the permutation is an exclusive or
+    const unsigned at_lane = place(lane & 31, lane >> 5);
     Chunk x[2][kTilesI], y[2][kTilesJ];
     const auto operands = [&](const Chunk* half, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
-        const Chunk* from = half + (at_lane ^ 2 * step);
 #pragma unroll
-        for (int k = 0; k < kTilesI; ++k) u[k] = from[(wave_i * kWideI + k * 32) * 8];
+        for (int k = 0; k < kTilesI; ++k) u[k] = half[(wave_i * kWideI + k * 32) * 8 + (at_lane ^ 2 * step ^ (wave_i * kTilesI + k) % 2 * 4)];
 #pragma unroll
-        for (int k = 0; k < kTilesJ; ++k) v[k] = from[(kI + wave_j * kWideJ + k * 32) * 8];
+        for (int k = 0; k < kTilesJ; ++k) v[k] = half[(kI + wave_j * kWideJ + k * 32) * 8 + (at_lane ^ 2 * step ^ (wave_j * kTilesJ + k) % 2 * 4)];
     };
     const auto products = [&](const Chunk(&u)[kTilesI], const Chunk(&v)[kTilesJ]) {
 #pragma unroll
@@ -260,17 +325,14 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     // Whole tiles.  While tile k is multiplied out of one half of LDS, tile k + 1 goes from registers into the other half and the kAhead after it are on their
     // way from memory; past the last one the last is read again, for nobody.
     unsigned turn = 0;
-    const int64_t whole = StageA::inside(i0, p.rows) && StageB::inside(j0, p.columns) && remain > 0 ? remain / kDepth : 0;
+    const int64_t whole = way.inside(p, i0, j0) && remain > 0 ? remain / kDepth : 0;
     if (whole) {
-        a.load_whole(0, p.lda);
-        b.load_whole(0, p.ldb);
-        a.to_lds(0, room[0]);
-        b.to_lds(0, room[0] + kI * 8);
+        way.load_whole(0, p);
+        way.to_lds(0, room[0]);
 #pragma unroll
         for (int ahead = 0; ahead < kAhead; ++ahead) {
-            if (ahead + 1 < whole) a.advance(p.lda), b.advance(p.ldb);
-            a.load_whole(ahead, p.lda);
-            b.load_whole(ahead, p.ldb);
+            if (ahead + 1 < whole) way.advance(p);
+            way.load_whole(ahead, p);
         }
         lds_barrier();
         operands(room[0], 0, x[0], y[0]);
@@ -287,15 +349,7 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
                         lds_barrier();
                         operands(room[turn ^ 1], 0, x[0], y[0]);
                     }
-                    if (step == 0) {
-                        a.to_lds(slot, room[turn ^ 1]);
-                        if (more) a.advance(p.lda);
-                        a.load_whole(slot, p.lda);
-                    } else if (step == 1) {
-                        b.to_lds(slot, room[turn ^ 1] + kI * 8);
-                        if (more) b.advance(p.ldb);
-                        b.load_whole(slot, p.ldb);
-                    }
+                    if (step < 2) way.exchange(step, slot, room[turn ^ 1], p, more);
                     __builtin_amdgcn_sched_barrier(0);  // the compiler would move requests down to where their answers are needed
                     products(x[step & 1], y[step & 1]);
                     __builtin_amdgcn_sched_barrier(0);
@@ -305,15 +359,12 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
         }
         lds_barrier();
         remain -= whole * kDepth;
-        a.advance(p.lda);
-        b.advance(p.ldb);
+        way.advance(p);
     }
-    // What is left: a part of a tile, or all of them where rows end inside a turned operand.
+    // What is left: a part of a tile, or all of them where a turned operand has fewer rows than are read at once.
     while (remain > 0) {
-        a.load_some(0, p.lda, remain, i0, p.rows);
-        b.load_some(0, p.ldb, remain, j0, p.columns);
-        a.to_lds(0, room[turn]);
-        b.to_lds(0, room[turn] + kI * 8);
+        way.load_some(0, p, remain, i0, j0);
+        way.to_lds(0, room[turn]);
         lds_barrier();
 #pragma unroll
         for (unsigned step = 0; step < 4; ++step) {
@@ -321,8 +372,7 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
             products(x[0], y[0]);
         }
         remain -= kDepth;
-        a.advance(p.lda);
-        b.advance(p.ldb);
+        way.advance(p);
         turn ^= 1;
     }
     __syncthreads();
@@ -353,11 +403,11 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     }
 }
 
-// The parts of the tiles that were cut, added up in their order, then the epilogue: four neighbouring numbers of C a thread.  Workgroup (b, t): 1024 numbers of tile t.
+// The parts added up in their order, then the epilogue: four neighbouring numbers of C a thread.  Workgroup (b, t): 1024 numbers of tile t.
 template <class T, int kI, int kJ>
 __global__ __launch_bounds__(256) void parts_kernel(Product p) {
     unsigned ti, tj;
-    tile_of(p.whole + blockIdx.y, p.tiles_i, p.tiles_j, &ti, &tj);
+    tile_of(blockIdx.y, p.tiles_i, p.tiles_j, &ti, &tj);
     const unsigned at = blockIdx.x * 1024 + threadIdx.x * 4;
     const int64_t i = (int64_t)ti * kI + at / kJ, j = (int64_t)tj * kJ + at % kJ;
     if (i >= p.rows || j >= p.columns) return;
@@ -368,16 +418,18 @@ __global__ __launch_bounds__(256) void parts_kernel(Product p) {
     finish<T>(p.to, i, j, z, p.columns - j);
 }
 
-// How a product is cut: tiles of a size, the last of them in parts along the contraction.
+// How a product is cut: tiles of a size, the contraction in parts; or its first rows or columns so that their tiles fill the chip some whole times, and the rest by itself.
 struct Plan {
     int side = 0;
-    int64_t tiles = 0, whole = 0, parts = 1;
+    int64_t parts = 1;
+    int64_t first = 0;  // rows or columns of C before the rest; 0: there is none
+    bool rows = false;
     double time = 0;  // microseconds, estimated
 };
 constexpr int64_t kComputeUnits = 256;
 
 template <class T>
-Plan plan_of(int64_t rows, int64_t columns, int64_t depth) {
+Plan plan_of(int64_t rows, int64_t columns, int64_t depth, bool may_cut) {
     constexpr int64_t kDepth = 128 / sizeof(T);
     // Per k, in nanoseconds: what `at_once` workgroups on a compute unit take at least (a step's way through LDS and its barrier, whatever it multiplies), and what each
     // adds once they share the matrix cores.  Measured with 2048 and 4096 tokens of 4096 -> 4096 (16 bits), 999 of 2048 -> 4608 (fp32).
@@ -387,27 +439,29 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth) {
     };
     constexpr Size wide[] = {{256, 1, 21.0, 30.7}, {128, 2, 10.3, 9.7}, {64, 4, 6.9, 3.4}}, exact[] = {{128, 2, 60.0, 62.0}, {64, 4, 18.0, 17.0}};
     const int64_t steps = (depth + kDepth - 1) / kDepth;
+    const auto rounds = [&](const Size& size, int64_t workgroups, double k) {
+        const int64_t most = (workgroups + kComputeUnits - 1) / kComputeUnits;
+        const bool few = workgroups <= kComputeUnits / 2;
+        return k * 1e-3 * std::max((double)((most + size.at_once - 1) / size.at_once) * size.alone, most * (size.at_once == 1 && few ? size.alone : size.each));
+    };
     Plan best;
-    const auto consider = [&](const Size& size, int64_t tiles, int64_t whole, int64_t parts) {
-        const auto rounds = [&](int64_t workgroups, double k) {
-            const int64_t most = (workgroups + kComputeUnits - 1) / kComputeUnits;
-            const bool one = workgroups <= kComputeUnits / 2;
-            return k * 1e-3 * std::max((double)((most + size.at_once - 1) / size.at_once) * size.alone, most * (size.at_once == 1 && one ? size.alone : size.each));
-        };
-        double time = 6.0 + (whole ? rounds(whole, (double)depth) : 0.0);
-        if (tiles > whole) {
-            const int64_t of_part = (steps + parts - 1) / parts;
-            time += rounds((tiles - whole) * parts, (double)(of_part * kDepth));
-            if (parts > 1) time += 5.0 + (double)((tiles - whole) * parts) * size.side * size.side * 8 / 2.5e6;  // written and read again, at 2.5 TB/s in bursts
-        }
-        if (!best.side || time < best.time) best = {size.side, tiles, whole, parts, time};
+    const auto consider = [&](const Plan& p) {
+        if (!best.side || p.time < best.time) best = p;
     };
     const auto of = [&](const Size& size) {
-        const int64_t tiles = ((rows + size.side - 1) / size.side) * ((columns + size.side - 1) / size.side);
-        consider(size, tiles, tiles, 1);
-        const int64_t room = kComputeUnits * size.at_once, whole = tiles / room * room, left = tiles - whole;
-        if (left == 0) return;
-        for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * left <= room; ++parts) consider(size, tiles, whole, parts);
+        const int64_t tiles_i = (rows + size.side - 1) / size.side, tiles_j = (columns + size.side - 1) / size.side, tiles = tiles_i * tiles_j, room = kComputeUnits * size.at_once;
+        consider({size.side, 1, 0, false, 6.0 + rounds(size, tiles, (double)depth)});
+        for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * tiles <= room; ++parts)  // written and read again, at 2.5 TB/s in bursts
+            consider({size.side, parts, 0, false,
+                      11.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 2.5e6});
+        if (!may_cut || tiles <= room || tiles > 16 * room) return;
+        for (const bool by_rows : {false, true}) {
+            const int64_t across = by_rows ? tiles_j : tiles_i, lines = tiles / room * room / across;  // whole lines of tiles
+            if (lines < 1 || lines >= (by_rows ? tiles_i : tiles_j)) continue;
+            const int64_t first = lines * size.side;
+            const Plan rest = plan_of<T>(by_rows ? rows - first : rows, by_rows ? columns : columns - first, depth, false);
+            consider({size.side, 1, first, by_rows, 6.0 + rounds(size, lines * across, (double)depth) + rest.time});
+        }
     };
     if constexpr (sizeof(T) == 2) {
         for (const Size& size : wide) of(size);
@@ -418,33 +472,51 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth) {
 }
 
 template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead>
-int launch_tiles(Product p, const Plan& plan, bool turn_a, bool turn_b, hipStream_t s) {
+int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t s) {
     constexpr int64_t kDepth = 128 / sizeof(T);
     p.tiles_i = (uint32_t)((p.rows + kI - 1) / kI), p.tiles_j = (uint32_t)((p.columns + kJ - 1) / kJ);
-    const int64_t steps = (p.depth + kDepth - 1) / kDepth, of_part = std::max<int64_t>(1, (steps + plan.parts - 1) / plan.parts), left = plan.tiles - plan.whole;
-    p.whole = (uint32_t)plan.whole;
+    const int64_t steps = (p.depth + kDepth - 1) / kDepth, of_part = std::max<int64_t>(1, (steps + parts - 1) / parts);
     p.parts = (uint32_t)std::max<int64_t>(1, (steps + of_part - 1) / of_part);  // none without a step
     p.depth_of_part = of_part * kDepth;
-    Temporary t((size_t)left * p.parts * kI * kJ * 4, s);
+    const unsigned tiles = p.tiles_i * p.tiles_j;
+    Temporary t(p.parts > 1 ? (size_t)tiles * p.parts * kI * kJ * 4 : 0, s);
     if (t.error) return t.error;
     p.part = t.floats();
-    const unsigned grid = (unsigned)(plan.whole + left * p.parts);
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, false><<<grid, kThreads, 0, s>>>(p);
-    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, true><<<grid, kThreads, 0, s>>>(p);
-    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, true, true><<<grid, kThreads, 0, s>>>(p);
+    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, true, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
     if (int e = (int)hipGetLastError()) return e;
-    if (left) parts_kernel<T, kI, kJ><<<dim3(kI * kJ / 1024, (unsigned)left), 256, 0, s>>>(p);
+    if (p.parts > 1) parts_kernel<T, kI, kJ><<<dim3(kI * kJ / 1024, tiles), 256, 0, s>>>(p);
     return (int)hipGetLastError();
 }
 
 template <class T>
-int launch_product(const Product& p, bool turn_a, bool turn_b, hipStream_t s) {
-    const Plan plan = plan_of<T>(p.rows, p.columns, p.depth);
-    if (plan.side == 64) return launch_tiles<T, 64, 64, 2, 2, 1>(p, plan, turn_a, turn_b, s);
-    if (plan.side == 128) return launch_tiles<T, 128, 128, 2, 2, 1>(p, plan, turn_a, turn_b, s);
-    if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 1>(p, plan, turn_a, turn_b, s);
+int launch_planned(const Product& p, const Plan& plan, bool turn_a, bool turn_b, hipStream_t s) {
+    if (plan.side == 64) return launch_tiles<T, 64, 64, 2, 2, 1>(p, plan.parts, turn_a, turn_b, s);
+    if (plan.side == 128) return launch_tiles<T, 128, 128, 2, 2, 1>(p, plan.parts, turn_a, turn_b, s);
+    if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 1>(p, plan.parts, turn_a, turn_b, s);
     return (int)hipErrorInvalidValue;
+}
+int size_of(int32_t type) { return type == CER_TYPE_F32 ? 4 : 2; }
+
+template <class T>
+int launch_product(const Product& p, bool turn_a, bool turn_b, hipStream_t s) {
+    const Plan plan = plan_of<T>(p.rows, p.columns, p.depth, true);
+    if (!plan.first) return launch_planned<T>(p, plan, turn_a, turn_b, s);
+    Product head = p, rest = p;
+    const auto past = [](auto* at, int64_t bytes) { return at ? (std::remove_pointer_t<decltype(at)>*)((uintptr_t)at + bytes) : at; };
+    const int64_t item = sizeof(T);
+    (plan.rows ? head.rows : head.columns) = plan.first;
+    (plan.rows ? rest.rows : rest.columns) -= plan.first;
+    if (plan.rows) rest.a = past(p.a, plan.first * (turn_a ? 1 : p.lda) * item);
+    else rest.b = past(p.b, plan.first * (turn_b ? 1 : p.ldb) * item);
+    if (p.to.bias_rows == plan.rows) rest.to.bias = past(p.to.bias, plan.first * size_of(p.to.bias_type));
+    rest.to.residual = past(p.to.residual, plan.first * (plan.rows ? p.to.ldr : 1) * item);
+    rest.to.pre = past(p.to.pre, plan.first * (plan.rows ? p.to.ldp : 1) * item);
+    rest.to.out = past(p.to.out, plan.first * (plan.rows ? p.to.ldo : 1) * item);
+    if (int e = launch_planned<T>(head, plan, turn_a, turn_b, s)) return e;
+    return launch_planned<T>(rest, plan_of<T>(rest.rows, rest.columns, rest.depth, false), turn_a, turn_b, s);
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------------
