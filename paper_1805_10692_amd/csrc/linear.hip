@@ -101,8 +101,9 @@ __device__ __forceinline__ void finish(const Epilogue& to, int64_t i, int64_t j,
     store_some<T, 4>(static_cast<T*>(to.out) + i * to.ldo + j, z, left);
 }
 
-// Where chunk c of a row lies: eight neighbouring rows, and eight rows four or eight apart, have the same chunk in different places.
-__device__ __forceinline__ unsigned place(unsigned row, unsigned c) { return row * 8 + (c ^ (row & 7) ^ (row >> 3 & 7)); }
+// Where chunk c of a row lies: eight neighbouring rows, and eight rows four (kFar: or eight) apart, have the same chunk in different places.
+template <bool kFar>
+__device__ __forceinline__ unsigned place(unsigned row, unsigned c) { return row * 8 + (c ^ (row & 7) ^ (row >> 3 & (kFar ? 7 : 3))); }
 
 // Sixteen bytes of k of 32 rows on either side: lanes 0 - 31 have the lower chunk, 32 - 63 the next one.
 template <class T>
@@ -121,7 +122,7 @@ __device__ __forceinline__ F16 multiply(Chunk a, Chunk b, F16 c) {
 
 // One operand's way from memory to LDS: kRows rows of 128 bytes of k, kAhead tiles of them on their way in registers.  Of rows past the matrix any others are
 // read in their place (their results are dropped); k past the end is 0 on both sides.
-template <class T, int kRows, int kThreads, bool kTurn, int kAhead, int kLine = 4>
+template <class T, int kRows, int kThreads, bool kTurn, int kAhead, bool kFar, int kLine = 4>
 struct Stage {
     static constexpr int E = 16 / sizeof(T), kDepth = 8 * E;
     static constexpr int kPieces = kTurn ? kRows / kLine * 8 : kRows * 8, kCount = (kPieces + kThreads - 1) / kThreads;  // turned: kLine rows by a chunk
@@ -145,10 +146,10 @@ struct Stage {
                 const int i = inside(row0, rows) && row(n) + kLine > most ? (int)most - kLine : (int)row(n);
                 at[n] = static_cast<const T*>(base) + k * ld + row0 + i;
 #pragma unroll
-                for (int r = 0; r < kLine; ++r) to[n][r] = place(i + r, chunk(n));
+                for (int r = 0; r < kLine; ++r) to[n][r] = place<kFar>(i + r, chunk(n));
             } else {
                 at[n] = static_cast<const T*>(base) + (row0 + (row(n) < most ? row(n) : most - 1)) * ld + k;
-                to[n][0] = place(row(n), chunk(n));
+                to[n][0] = place<kFar>(row(n), chunk(n));
             }
         }
     }
@@ -204,10 +205,10 @@ struct Stage {
 
 // Both operands' way.  Where both are turned and the halves of the workgroup can take one each, a thread has eight rows of one of them and not four of both: 16 bytes
 // of a line and not 8, in half as many requests (dW of 4096 tokens, 4096 -> 9216 bf16: 370 -> 343 us).
-template <class T, int kI, int kJ, int kThreads, int kAhead, bool kTurnA, bool kTurnB>
+template <class T, int kI, int kJ, int kThreads, int kAhead, bool kTurnA, bool kTurnB, bool kFar>
 struct Operands {
-    using A = Stage<T, kI, kThreads, kTurnA, kAhead>;
-    using B = Stage<T, kJ, kThreads, kTurnB, kAhead>;
+    using A = Stage<T, kI, kThreads, kTurnA, kAhead, kFar>;
+    using B = Stage<T, kJ, kThreads, kTurnB, kAhead, kFar>;
     A a;
     B b;
     __device__ __forceinline__ bool inside(const Product& p, int64_t i0, int64_t j0) const { return A::inside(i0, p.rows) && B::inside(j0, p.columns); }
@@ -246,7 +247,7 @@ struct Operands {
 };
 template <class T, int kSide, int kThreads, int kAhead>
 struct Halves {
-    using S = Stage<T, kSide, kThreads / 2, true, kAhead, 8>;
+    using S = Stage<T, kSide, kThreads / 2, true, kAhead, true, 8>;
     S s;
     int64_t ld;
     __device__ __forceinline__ static bool second() { return __builtin_amdgcn_readfirstlane(threadIdx.x / (kThreads / 2)); }
@@ -289,8 +290,9 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
     constexpr int kDepth = 128 / sizeof(T);
-    using Way = std::conditional_t<kTurnA && kTurnB && sizeof(T) == 2 && kI == kJ && kI / 8 * 8 % (kThreads / 2) == 0, Halves<T, kI, kThreads, kAhead>,
-                                   Operands<T, kI, kJ, kThreads, kAhead, kTurnA, kTurnB>>;
+    constexpr bool kHalves = kTurnA && kTurnB && sizeof(T) == 2 && kI == kJ && kI % (kThreads / 2) == 0;
+    constexpr bool kFar = kHalves || kI == 256;  // eight rows a thread want it; elsewhere it costs registers (dX of 512 tokens 39 -> 45 us), or none that are missed (4096: 305 -> 290)
+    using Way = std::conditional_t<kHalves, Halves<T, kI, kThreads, kAhead>, Operands<T, kI, kJ, kThreads, kAhead, kTurnA, kTurnB, kFar>>;
     __shared__ Chunk room[2][(kI + kJ) * 8];
     static_assert(sizeof(room) >= sizeof(float) * kWavesI * kWavesJ * 32 * kPitch, "");
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wave_i = wave / kWavesJ, wave_j = wave % kWavesJ;
@@ -308,13 +310,13 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
 #pragma unroll
         for (int y = 0; y < kTilesJ; ++y) sums[x][y] = 0.f;
     // chunk 2 . step + (lane >> 5) of row lane & 31 of an even or odd 32 rows: the permutation is an exclusive or
-    const unsigned at_lane = place(lane & 31, lane >> 5);
+    const unsigned at_lane = place<kFar>(lane & 31, lane >> 5);
     Chunk x[2][kTilesI], y[2][kTilesJ];
     const auto operands = [&](const Chunk* half, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
 #pragma unroll
-        for (int k = 0; k < kTilesI; ++k) u[k] = half[(wave_i * kWideI + k * 32) * 8 + (at_lane ^ 2 * step ^ (wave_i * kTilesI + k) % 2 * 4)];
+        for (int k = 0; k < kTilesI; ++k) u[k] = half[(wave_i * kWideI + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_i * kTilesI + k) % 2 * 4 : 0))];
 #pragma unroll
-        for (int k = 0; k < kTilesJ; ++k) v[k] = half[(kI + wave_j * kWideJ + k * 32) * 8 + (at_lane ^ 2 * step ^ (wave_j * kTilesJ + k) % 2 * 4)];
+        for (int k = 0; k < kTilesJ; ++k) v[k] = half[(kI + wave_j * kWideJ + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_j * kTilesJ + k) % 2 * 4 : 0))];
     };
     const auto products = [&](const Chunk(&u)[kTilesI], const Chunk(&v)[kTilesJ]) {
 #pragma unroll
