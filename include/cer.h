@@ -608,7 +608,8 @@ int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float*
  *   pre   what linear_matmul wrote (relu: its Y does as well, without a residual); NULL for CER_ACTIVATION_NONE
  *   dY, X, pre, base, dX: of W's type and all in the same order; X only for dW.  dW: W's type, rows contiguous, lddw >= in.
  *
- * Temporaries: dZ with an activation; sums of parts where the product has few outputs (forward: up to 64 . tokens . out floats, 13 MB in all at most).
+ * The order of a sum depends on the sizes (a token's results may differ in their last bits between batches), on nothing else.
+ * Temporaries: dZ with an activation; up to 1024 . out floats for dbias; sums of parts where a product has few outputs (67 MB at most).
  */
 enum { CER_ACTIVATION_NONE = 0, CER_ACTIVATION_RELU = 1, CER_ACTIVATION_GELU = 2, CER_ACTIVATION_GELU_TANH = 3, CER_ACTIVATION_SILU = 4 };
 int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* X, const cer_tokens_t* Y,
