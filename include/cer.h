@@ -589,9 +589,15 @@ int grad_norm(const cer_gradient_t* grads, int64_t count, float* norm, void* str
 int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float* norm, void* stream);
 
 /*
- * Operators of a block around projections.  Matrices, types, orders, streams, graphs and errors as above; CER_E_TOO_LARGE: tokens over 2^28
+ * Operators of a block around projections.  Matrices, types, orders, streams and errors as above; CER_E_TOO_LARGE: tokens over 2^28
  * (linear: 2^24), features over 2^22 (block_norm: 32768), tokens . features or in . out over 2^40.
+ *
+ * workspace: device memory for a call's temporaries, 16-byte aligned, of linear_workspace_bytes() or block_workspace_bytes() bytes (which suffice for every call of
+ * those sizes, type and order; block: with columns != 0 for F, Y or dY in columns), or NULL: a stream-ordered temporary.  With it a call only launches kernels; calls that
+ * may run at once need one each.  A call that is recorded into a HIP graph has to bring it where it needs any (else CER_E_HIP).
  */
+int64_t linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t type, int32_t order, int32_t backward);
+int64_t block_workspace_bytes(int64_t tokens, int64_t n, int32_t type, int32_t columns, int32_t backward);
 
 /*
  * linear_matmul -- the product with a dense matrix that is not compressed, and what follows it:
@@ -613,10 +619,11 @@ int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float*
  */
 enum { CER_ACTIVATION_NONE = 0, CER_ACTIVATION_RELU = 1, CER_ACTIVATION_GELU = 2, CER_ACTIVATION_GELU_TANH = 3, CER_ACTIVATION_SILU = 4 };
 int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* X, const cer_tokens_t* Y,
-                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* stream);
+                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* workspace,
+                  int64_t workspace_bytes, void* stream);
 int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* dY, const cer_tokens_t* X,
                     int32_t activation, const cer_tokens_t* pre, const cer_tokens_t* base, const cer_tokens_t* dX, void* dW, int64_t lddw, float* dbias,
-                    void* stream);
+                    void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * block_norm -- where a block's output joins the residual stream:
@@ -641,11 +648,12 @@ int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, in
  */
 int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t* H, const cer_tokens_t* Y, int64_t tokens, int64_t n, const cer_tokens_t* gate,
                const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
-               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* stream);
+               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* workspace, int64_t workspace_bytes, void* stream);
 int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_tokens_t* F, const float* rstd_pre, const float* rstd_post,
                         const cer_tokens_t* dX, const cer_tokens_t* dF, int64_t tokens, int64_t n, const cer_tokens_t* gate, const void* gate_vector,
                         int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
-                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* stream);
+                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* workspace,
+                        int64_t workspace_bytes, void* stream);
 
 /*
  * dropout_add -- Y_ti = residual_ti (NULL: 0) + (keep_ti ? X_ti . 65536 / (65536 - d) : 0), d = p . 65536 rounded to nearest even, 0 <= p <= 1 (d = 65536: nothing is

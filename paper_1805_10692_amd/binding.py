@@ -48,7 +48,7 @@ EXPORTS = [
 OPERATOR_EXPORTS = ["rms_norm", "rms_norm_backward", "adapter_workspace_bytes", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip"]
 
 # operators of a block around projections
-BLOCK_EXPORTS = ["linear_matmul", "linear_backward", "block_norm", "block_norm_backward", "dropout_add"]
+BLOCK_EXPORTS = ["linear_workspace_bytes", "block_workspace_bytes", "linear_matmul", "linear_backward", "block_norm", "block_norm_backward", "dropout_add"]
 
 CER_FORMAT_CER, CER_FORMAT_CSER = 0, 1
 
@@ -198,6 +198,9 @@ def lib() -> ctypes.CDLL:
         L.cer_last_hip_error.argtypes = []
         L.adapter_workspace_bytes.restype = i64
         L.adapter_workspace_bytes.argtypes = [i64] * 4
+        L.linear_workspace_bytes.restype = L.block_workspace_bytes.restype = i64
+        L.linear_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.block_workspace_bytes.argtypes = [i64, i64, i32, i32, i32]
         _cerpy.bind(*(ctypes.cast(getattr(L, f), vp).value
                       for f in ("cer_matmul", "cser_matmul", "cer_matmul_noalloc", "csr_matmul")))
         _lib = L
@@ -246,14 +249,16 @@ else:
 #   adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)
 #   grad_norm(grads, norm, stream=None)
 #   grad_clip(grads, max_norm, norm, outs=None, stream=None)
-# and those of a block around projections (activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'; gate: (n,) or (tokens, n); key: int64, (2,)):
-#   linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, stream=None)
-#   linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, stream=None)
-#   block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, stream=None)
+# and those of a block around projections (activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'; gate: (n,) or (tokens, n); key: int64, (2,); workspace: float32,
+# linear_workspace_bytes() or block_workspace_bytes() / 4 numbers, needed while recorded into a graph):
+#   linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, workspace=None, stream=None)
+#   linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, workspace=None, stream=None)
+#   block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, workspace=None,
+#              stream=None)
 #   block_norm_backward(dY, H, F, rstd_pre, dX, dF, rstd_post=None, gate=None, post_weight=None, pre_weight=None, scale=1.0, dsum=None, dgate=None,
-#                       dpost_weight=None, dpre_weight=None, stream=None)
+#                       dpost_weight=None, dpre_weight=None, workspace=None, stream=None)
 #   dropout_add(X, Y, key, p, residual=None, call=0, stream=None)
-_OPERATORS = ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip", *BLOCK_EXPORTS)
+_OPERATORS = ("rms_norm", "rms_norm_backward", "adapter_matmul", "adapter_backward", "grad_norm", "grad_clip", *BLOCK_EXPORTS[2:])
 
 
 def __getattr__(name: str):
@@ -501,6 +506,26 @@ def adapter_workspace_bytes(tokens: int, rank: int, features_in: int, features_o
     v = lib().adapter_workspace_bytes(tokens, rank, features_in, features_out)
     if v < 0:
         raise CerError(int(v), "adapter_workspace_bytes")
+    return int(v)
+
+
+def _type_code(dtype) -> int:
+    return {"float32": 0, "bfloat16": 1, "float16": 2}.get(str(dtype).replace("torch.", ""), -1)
+
+
+def linear_workspace_bytes(tokens: int, features_in: int, features_out: int, dtype, columns: bool = False, backward: bool = False) -> int:
+    """Size of the workspace with which linear_matmul (backward: linear_backward) allocates nothing."""
+    v = lib().linear_workspace_bytes(tokens, features_in, features_out, _type_code(dtype), int(columns), int(backward))
+    if v < 0:
+        raise CerError(int(v), "linear_workspace_bytes")
+    return int(v)
+
+
+def block_workspace_bytes(tokens: int, n: int, dtype, columns: bool = False, backward: bool = False) -> int:
+    """Size of the workspace with which block_norm (backward: block_norm_backward) allocates nothing; dtype: of the residual stream, columns: F, Y or dY are in columns."""
+    v = lib().block_workspace_bytes(tokens, n, _type_code(dtype), int(columns), int(backward))
+    if v < 0:
+        raise CerError(int(v), "block_workspace_bytes")
     return int(v)
 
 

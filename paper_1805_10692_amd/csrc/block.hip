@@ -186,14 +186,15 @@ int block_rows(const BlockArgs& a, hipStream_t s) {
 template <class TX>
 int block_of(const BlockCall& c, BlockArgs a, hipStream_t s) {
     const bool f_columns = c.f.order == CER_ORDER_COLUMNS, y_columns = c.y.order == CER_ORDER_COLUMNS;
-    const size_t room = (size_t)c.tokens * c.n * 4;
-    Temporary f(f_columns ? room : 0, s), y(y_columns ? room : 0, s);
-    if (f.error || y.error) return f.error ? f.error : y.error;
+    const size_t bytes = (size_t)c.tokens * c.n * 4;
+    Room room(c.workspace, block_room(c), s);
+    if (room.error) return room.error;
+    float *f = room.take(f_columns ? bytes : 0), *y = room.take(y_columns ? bytes : 0);
     if (f_columns) {
-        a.f = f.p, a.ldf = c.n;
-        if (int e = turn({{{static_cast<const float*>(c.f.data), f.floats(), c.f.ld, c.n}, {}}, c.n, c.tokens}, 1, s)) return e;
+        a.f = f, a.ldf = c.n;
+        if (int e = turn({{{static_cast<const float*>(c.f.data), f, c.f.ld, c.n}, {}}, c.n, c.tokens}, 1, s)) return e;
     }
-    if (y_columns) a.y = y.p, a.ldy = c.n;
+    if (y_columns) a.y = y, a.ldy = c.n;
     int e;
     if constexpr (sizeof(TX) == 4) {
         e = block_rows<float, float, float>(a, s);
@@ -203,7 +204,7 @@ int block_of(const BlockCall& c, BlockArgs a, hipStream_t s) {
                    : wide_y ? block_rows<TX, TX, float>(a, s) : block_rows<TX, TX, TX>(a, s);
     }
     if (e || !y_columns) return e;
-    return turn({{{y.floats(), static_cast<float*>(c.y.data), c.n, c.y.ld}, {}}, c.tokens, c.n}, 1, s);
+    return turn({{{y, static_cast<float*>(c.y.data), c.n, c.y.ld}, {}}, c.tokens, c.n}, 1, s);
 }
 
 // ---- backward -------------------------------------------------------------------------------------------------------------------
@@ -479,20 +480,38 @@ __global__ __launch_bounds__(1024) void block_back_totals_kernel(Totals w, uint3
 }
 
 constexpr unsigned kFewThreads = 768;  // up to here a thread has 168 registers
+// How a backward call goes about its tokens, and its temporaries.
+struct BackShape {
+    Threads w;
+    bool inside, sums[2];
+    unsigned groups, parts;
+    int64_t tokens_of_part;
+    size_t turned, room, means;
+    BackShape(const BlockBackwardCall& c) : w(c.n, c.h.type == CER_TYPE_F32 ? 4 : 8) {
+        // 1024 threads with eight features each spill: 2048 x 8192 bf16 80 us here, 72 in strips; with four or eight of fp32 they do not, or hardly (2000 x 7680: 94 us, 110).
+        inside = w.threads <= kFewThreads ? w.chunks == 1 : c.h.type == CER_TYPE_F32 && c.n <= 8192;
+        sums[0] = c.dpre_weight != nullptr, sums[1] = c.dpost_weight || c.dgate_vector;
+        groups = inside && w.threads <= kFewThreads ? (unsigned)std::max<int64_t>(1, std::min<int64_t>(kFewThreads / w.threads, (c.tokens + 255) / 256)) : 1;
+        tokens_of_part = std::max<int64_t>(1, (c.tokens + 63) / 64);
+        parts = (unsigned)(inside ? std::min<int64_t>((c.tokens + groups - 1) / groups, 256) : (c.tokens + tokens_of_part - 1) / tokens_of_part);
+        turned = (size_t)c.tokens * c.n * 4;
+        room = (size_t)(sums[0] + sums[1]) * parts * c.n * 4;
+        means = inside ? 0 : (size_t)c.tokens * 8;
+    }
+    static bool columns(const cer_tokens_t& m) { return m.data && m.order == CER_ORDER_COLUMNS; }
+    int64_t bytes(const BlockBackwardCall& c) const {
+        return (int64_t)(Room::rounded(turned) * ((columns(c.dy) ? 1 : 0) + (columns(c.f) ? 2 : 0)) + Room::rounded(room) + Room::rounded(means));
+    }
+};
 template <class TX, class TF, class TD>
-int block_back_rows(BlockBackArgs a, Totals totals, hipStream_t s) {
+int block_back_rows(BlockBackArgs a, Totals totals, const BackShape& shape, Room& temporaries, hipStream_t s) {
     constexpr int V = 16 / sizeof(TX);
-    const Threads w(a.n, V);
-    // 1024 threads with eight features each spill: 2048 x 8192 bf16 80 us here, 72 in strips; with four or eight of fp32 they do not, or hardly (2000 x 7680: 94 us, 110).
-    const bool inside = w.threads <= kFewThreads ? w.chunks == 1 : V == 4 && a.n <= 8192, sums[2] = {totals.pre != nullptr, totals.post || totals.gate};
-    const unsigned groups = inside && w.threads <= kFewThreads ? (unsigned)std::min<int64_t>(kFewThreads / w.threads, (a.tokens + 255) / 256) : 1;
-    const int64_t tokens_of_part = (a.tokens + 63) / 64;
-    const unsigned parts = (unsigned)(inside ? std::min<int64_t>((a.tokens + groups - 1) / groups, 256) : (a.tokens + tokens_of_part - 1) / tokens_of_part);
-    Temporary room((size_t)(sums[0] + sums[1]) * parts * a.n * 4, s), means(inside ? 0 : (size_t)a.tokens * 8, s);
-    if (room.error || means.error) return room.error ? room.error : means.error;
-    for (int k = 0, at = 0; k < 2; ++k) totals.part[k] = a.part[k] = sums[k] ? room.floats() + (size_t)at++ * parts * a.n : nullptr;
-    a.means = means.floats();
-    if (inside) {
+    const Threads& w = shape.w;
+    const unsigned groups = shape.groups, parts = shape.parts;
+    float* room = temporaries.take(shape.room);
+    for (int k = 0, at = 0; k < 2; ++k) totals.part[k] = a.part[k] = shape.sums[k] ? room + (size_t)at++ * parts * a.n : nullptr;
+    a.means = temporaries.take(shape.means);
+    if (shape.inside) {
         const dim3 block(w.threads, groups);
         const auto bytes = [&](int chunks) { return (size_t)V * 4 * w.threads * std::max<size_t>(2 * chunks, groups > 1 ? groups : 0); };
         if (w.threads <= kFewThreads && w.chunks == 1) block_back_rows_kernel<TX, TF, TD, 1, kFewThreads><<<parts, block, bytes(1), s>>>(a);
@@ -505,10 +524,10 @@ int block_back_rows(BlockBackArgs a, Totals totals, hipStream_t s) {
     } else {
         block_back_means_kernel<TX, TF, TD><<<(unsigned)std::min<int64_t>(a.tokens, 1 << 20), 512, 0, s>>>(a);
         if (int e = (int)hipGetLastError()) return e;
-        block_back_strips_kernel<TX, TF, TD><<<dim3((unsigned)((a.n + 64 * V - 1) / (64 * V)), parts), 256, 0, s>>>(a, tokens_of_part);
+        block_back_strips_kernel<TX, TF, TD><<<dim3((unsigned)((a.n + 64 * V - 1) / (64 * V)), parts), 256, 0, s>>>(a, shape.tokens_of_part);
     }
     if (int e = (int)hipGetLastError()) return e;
-    if (!sums[0] && !sums[1]) return 0;
+    if (!shape.sums[0] && !shape.sums[1]) return 0;
     block_back_totals_kernel<<<dim3((unsigned)((a.n + 63) / 64), 2), 1024, 0, s>>>(totals, parts, a.n);
     return (int)hipGetLastError();
 }
@@ -516,34 +535,39 @@ int block_back_rows(BlockBackArgs a, Totals totals, hipStream_t s) {
 template <class TX>
 int block_back_of(const BlockBackwardCall& c, BlockBackArgs a, const Totals& outs, hipStream_t s) {
     const bool dy_columns = c.dy.order == CER_ORDER_COLUMNS, f_columns = c.f.order == CER_ORDER_COLUMNS;
-    const size_t room = (size_t)c.tokens * c.n * 4;
-    Temporary dy(dy_columns ? room : 0, s), f(f_columns ? room : 0, s), df(f_columns ? room : 0, s);
-    if (dy.error || f.error || df.error) return dy.error ? dy.error : f.error ? f.error : df.error;
+    const BackShape shape(c);
+    Room room(c.workspace, shape.bytes(c), s);
+    if (room.error) return room.error;
+    float *dy = room.take(dy_columns ? shape.turned : 0), *f = room.take(f_columns ? shape.turned : 0), *df = room.take(f_columns ? shape.turned : 0);
     Turns w{{}, c.n, c.tokens};
     unsigned many = 0;
     if (dy_columns) {
-        a.dy = dy.p, a.lddy = c.n;
-        w.each[many++] = {static_cast<const float*>(c.dy.data), dy.floats(), c.dy.ld, c.n};
+        a.dy = dy, a.lddy = c.n;
+        w.each[many++] = {static_cast<const float*>(c.dy.data), dy, c.dy.ld, c.n};
     }
     if (f_columns) {
-        a.f = f.p, a.df = df.p, a.ldf = a.lddf = c.n;
-        w.each[many++] = {static_cast<const float*>(c.f.data), f.floats(), c.f.ld, c.n};
+        a.f = f, a.df = df, a.ldf = a.lddf = c.n;
+        w.each[many++] = {static_cast<const float*>(c.f.data), f, c.f.ld, c.n};
     }
     if (many)
         if (int e = turn(w, many, s)) return e;
     int e;
     if constexpr (sizeof(TX) == 4) {
-        e = block_back_rows<float, float, float>(a, outs, s);
+        e = block_back_rows<float, float, float>(a, outs, shape, room, s);
     } else {
         const bool wide_f = c.f.type == CER_TYPE_F32, wide_dy = c.dy.type == CER_TYPE_F32;
-        e = wide_f ? wide_dy ? block_back_rows<TX, float, float>(a, outs, s) : block_back_rows<TX, float, TX>(a, outs, s)
-                   : wide_dy ? block_back_rows<TX, TX, float>(a, outs, s) : block_back_rows<TX, TX, TX>(a, outs, s);
+        e = wide_f ? wide_dy ? block_back_rows<TX, float, float>(a, outs, shape, room, s) : block_back_rows<TX, float, TX>(a, outs, shape, room, s)
+                   : wide_dy ? block_back_rows<TX, TX, float>(a, outs, shape, room, s) : block_back_rows<TX, TX, TX>(a, outs, shape, room, s);
     }
     if (e || !f_columns) return e;
-    return turn({{{df.floats(), static_cast<float*>(c.df.data), c.n, c.df.ld}, {}}, c.tokens, c.n}, 1, s);
+    return turn({{{df, static_cast<float*>(c.df.data), c.n, c.df.ld}, {}}, c.tokens, c.n}, 1, s);
 }
 }  // namespace
 
+int64_t block_room(const BlockCall& c) {
+    return (int64_t)Room::rounded((size_t)c.tokens * c.n * 4) * ((c.f.order == CER_ORDER_COLUMNS) + (c.y.order == CER_ORDER_COLUMNS));
+}
+int64_t block_backward_room(const BlockBackwardCall& c) { return c.tokens ? BackShape(c).bytes(c) : 0; }
 int launch_block_norm(const BlockCall& c, hipStream_t s) {
     BlockArgs a{};
     a.x = c.x.data, a.f = c.f.data, a.gate = c.gate.data, a.h = c.h.data, a.y = c.y.data;

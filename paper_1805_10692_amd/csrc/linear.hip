@@ -480,17 +480,34 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth, int turned, bool may_
     return best;
 }
 
+// Steps of the contraction to a part, and parts: none without a step.
+template <class T>
+void parts_of(int64_t depth, int64_t parts, int64_t* depth_of_part, uint32_t* many) {
+    constexpr int64_t kDepth = 128 / sizeof(T);
+    const int64_t steps = (depth + kDepth - 1) / kDepth, of_part = std::max<int64_t>(1, (steps + parts - 1) / parts);
+    *many = (uint32_t)std::max<int64_t>(1, (steps + of_part - 1) / of_part);
+    *depth_of_part = of_part * kDepth;
+}
+template <class T>
+size_t parts_bytes(const Plan& plan, int64_t rows, int64_t columns, int64_t depth) {
+    int64_t of_part;
+    uint32_t parts;
+    parts_of<T>(depth, plan.parts, &of_part, &parts);
+    return parts > 1 ? (size_t)((rows + plan.side - 1) / plan.side * ((columns + plan.side - 1) / plan.side)) * parts * plan.side * plan.side * 4 : 0;
+}
+template <class T>
+size_t product_bytes(int64_t rows, int64_t columns, int64_t depth, int turned) {
+    const Plan plan = plan_of<T>(rows, columns, depth, turned, true);
+    if (!plan.first) return parts_bytes<T>(plan, rows, columns, depth);
+    (plan.rows ? rows : columns) -= plan.first;
+    return parts_bytes<T>(plan_of<T>(rows, columns, depth, turned, false), rows, columns, depth);
+}
+
 template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead>
 int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t s) {
-    constexpr int64_t kDepth = 128 / sizeof(T);
     p.tiles_i = (uint32_t)((p.rows + kI - 1) / kI), p.tiles_j = (uint32_t)((p.columns + kJ - 1) / kJ);
-    const int64_t steps = (p.depth + kDepth - 1) / kDepth, of_part = std::max<int64_t>(1, (steps + parts - 1) / parts);
-    p.parts = (uint32_t)std::max<int64_t>(1, (steps + of_part - 1) / of_part);  // none without a step
-    p.depth_of_part = of_part * kDepth;
+    parts_of<T>(p.depth, parts, &p.depth_of_part, &p.parts);
     const unsigned tiles = p.tiles_i * p.tiles_j;
-    Temporary t(p.parts > 1 ? (size_t)tiles * p.parts * kI * kJ * 4 : 0, s);
-    if (t.error) return t.error;
-    p.part = t.floats();
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
     if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
     else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
@@ -725,6 +742,12 @@ __global__ __launch_bounds__(1024) void bias_totals_kernel(const float* part, ui
 }
 
 template <class T>
+int64_t linear_bytes(const LinearCall& c) {
+    const bool columns = c.x.order == CER_ORDER_COLUMNS;
+    if (!c.tokens || few_tokens(c.tokens, c.in, c.out, sizeof(T))) return 0;
+    return (int64_t)Room::rounded(product_bytes<T>(columns ? c.out : c.tokens, columns ? c.tokens : c.out, c.in, columns));
+}
+template <class T>
 int linear_of(const LinearCall& c, hipStream_t s) {
     const bool columns = c.x.order == CER_ORDER_COLUMNS;
     const Epilogue to{c.bias, c.bias_type, columns, c.activation, c.residual.data, c.pre.data, c.y.data, c.residual.ld, c.pre.ld, c.y.ld};
@@ -739,43 +762,63 @@ int linear_of(const LinearCall& c, hipStream_t s) {
     p.b = columns ? c.x.data : c.w, p.ldb = columns ? c.x.ld : c.ldw;
     p.rows = columns ? c.out : c.tokens, p.columns = columns ? c.tokens : c.out, p.depth = c.in;
     p.to = to;
+    Room room(c.workspace, linear_bytes<T>(c), s);
+    if (room.error) return room.error;
+    p.part = room.take((size_t)linear_bytes<T>(c));
     return launch_product<T>(p, false, columns, s);
 }
 
-constexpr int64_t kBriefTokens = 512;
+// What a backward call needs and how it goes about the gradient of z.
+template <class T>
+struct BackwardShape {
+    static constexpr int V = 16 / sizeof(T);
+    bool columns, act, brief;
+    int64_t lanes, blocks, tokens_of_part, parts;
+    size_t dz, sums, product;
+    // Rows: about a thousand workgroups of whole lines.  A few hundred tokens: all of them in one of 64 bytes' features, which needs no second launch (257 x 2049 fp32 10.7 us for 13.4).
+    explicit BackwardShape(const LinearBackwardCall& c) : columns(c.dy.order == CER_ORDER_COLUMNS), act(c.activation != CER_ACTIVATION_NONE), brief(!columns && c.tokens <= 512) {
+        lanes = brief ? 4 : 64, blocks = (c.out + lanes * V - 1) / (lanes * V);
+        const int64_t most = brief ? 1 : std::max<int64_t>(1, std::min<int64_t>(1024 / std::min<int64_t>(blocks, 1024), (c.tokens + 15) / 16));
+        tokens_of_part = std::max<int64_t>(1, (c.tokens + most - 1) / most), parts = (c.tokens + tokens_of_part - 1) / tokens_of_part;
+        dz = act && (c.dx.data || c.dw) ? (size_t)c.tokens * c.out * sizeof(T) : 0;
+        sums = c.dbias && parts > 1 && !columns ? (size_t)parts * c.out * 4 : 0;
+        product = 0;
+        if (c.dx.data && c.tokens) product = product_bytes<T>(columns ? c.in : c.tokens, columns ? c.tokens : c.in, c.out, columns ? 2 : 1);
+        if (c.dw) product = std::max(product, product_bytes<T>(c.out, c.in, c.tokens, columns ? 0 : 2));
+    }
+    int64_t bytes() const { return (int64_t)(Room::rounded(dz) + Room::rounded(sums) + Room::rounded(product)); }
+};
 template <class T>
 int linear_backward_of(const LinearBackwardCall& c, hipStream_t s) {
-    constexpr int V = 16 / sizeof(T);
-    const bool columns = c.dy.order == CER_ORDER_COLUMNS, act = c.activation != CER_ACTIVATION_NONE, product = c.dx.data || c.dw;
+    const BackwardShape<T> shape(c);
+    const bool columns = shape.columns, act = shape.act;
     const int64_t across = columns ? c.tokens : c.out;
-    // Rows: about a thousand workgroups of whole lines.  A few hundred tokens: all of them in one of 64 bytes' features, which needs no second launch (257 x 2049 fp32 10.7 us for 13.4).
-    const bool brief = !columns && c.tokens <= kBriefTokens;
-    const int64_t lanes = brief ? 4 : 64, blocks = (c.out + lanes * V - 1) / (lanes * V);
-    const int64_t most = brief ? 1 : std::max<int64_t>(1, std::min<int64_t>(1024 / std::min<int64_t>(blocks, 1024), (c.tokens + 15) / 16));
-    const int64_t tokens_of_part = std::max<int64_t>(1, (c.tokens + most - 1) / most), parts = (c.tokens + tokens_of_part - 1) / tokens_of_part;
-    Temporary dz(act && product ? (size_t)c.tokens * c.out * sizeof(T) : 0, s), sums(c.dbias && parts > 1 && !columns ? (size_t)parts * c.out * 4 : 0, s);
-    if (dz.error || sums.error) return dz.error ? dz.error : sums.error;
-    if (c.tokens && (dz.p || c.dbias)) {
-        SlopeArgs a{c.dy.data, act ? c.pre.data : nullptr, dz.p, c.dy.ld, c.pre.ld, across, c.tokens, c.out, c.activation, sums.p ? sums.floats() : c.dbias, tokens_of_part};
+    Room room(c.workspace, shape.bytes(), s);
+    if (room.error) return room.error;
+    void* dz = room.take(shape.dz);
+    float *sums = room.take(shape.sums), *part = room.take(shape.product);
+    if (c.tokens && (dz || c.dbias)) {
+        SlopeArgs a{c.dy.data, act ? c.pre.data : nullptr, dz, c.dy.ld, c.pre.ld, across, c.tokens, c.out, c.activation, sums ? sums : c.dbias, shape.tokens_of_part};
         if constexpr (sizeof(T) == 4) {
             if (columns) slope_columns_kernel<<<(unsigned)c.out, 256, 0, s>>>(a);
         }
-        const dim3 grid((unsigned)blocks, (unsigned)parts);
-        if (brief) slope_rows_kernel<T, 4><<<grid, 256, 0, s>>>(a);
+        const dim3 grid((unsigned)shape.blocks, (unsigned)shape.parts);
+        if (shape.brief) slope_rows_kernel<T, 4><<<grid, 256, 0, s>>>(a);
         else if (!columns) slope_rows_kernel<T, 64><<<grid, 256, 0, s>>>(a);
         if (int e = (int)hipGetLastError()) return e;
     }
-    if (c.dbias && (sums.p || !c.tokens)) {
-        bias_totals_kernel<<<(unsigned)((c.out + 63) / 64), 1024, 0, s>>>(sums.floats(), c.tokens ? (uint32_t)parts : 0, c.out, c.dbias);
+    if (c.dbias && (sums || !c.tokens)) {
+        bias_totals_kernel<<<(unsigned)((c.out + 63) / 64), 1024, 0, s>>>(sums, c.tokens ? (uint32_t)shape.parts : 0, c.out, c.dbias);
         if (int e = (int)hipGetLastError()) return e;
     }
-    const void* z = act ? dz.p : c.dy.data;
+    const void* z = act ? dz : c.dy.data;
     const int64_t ldz = act ? across : c.dy.ld;
     if (c.dx.data && c.tokens) {
         Product p{};
         p.a = columns ? c.w : z, p.lda = columns ? c.ldw : ldz;
         p.b = columns ? z : c.w, p.ldb = columns ? ldz : c.ldw;
         p.rows = columns ? c.in : c.tokens, p.columns = columns ? c.tokens : c.in, p.depth = c.out;
+        p.part = part;
         p.to.residual = c.base.data, p.to.ldr = c.base.ld, p.to.out = c.dx.data, p.to.ldo = c.dx.ld;
         if (int e = launch_product<T>(p, columns, true, s)) return e;
     }
@@ -783,6 +826,7 @@ int linear_backward_of(const LinearBackwardCall& c, hipStream_t s) {
         Product p{};
         p.a = z, p.lda = ldz, p.b = c.x.data, p.ldb = c.x.ld;
         p.rows = c.out, p.columns = c.in, p.depth = c.tokens;
+        p.part = part;
         p.to.out = c.dw, p.to.ldo = c.lddw;
         if (int e = launch_product<T>(p, !columns, !columns, s)) return e;
     }
@@ -790,6 +834,12 @@ int linear_backward_of(const LinearBackwardCall& c, hipStream_t s) {
 }
 }  // namespace
 
+int64_t linear_room(const LinearCall& c) {
+    return c.type == CER_TYPE_BF16 ? linear_bytes<__bf16>(c) : c.type == CER_TYPE_F16 ? linear_bytes<_Float16>(c) : linear_bytes<float>(c);
+}
+int64_t linear_backward_room(const LinearBackwardCall& c) {
+    return c.type == CER_TYPE_BF16 ? BackwardShape<__bf16>(c).bytes() : c.type == CER_TYPE_F16 ? BackwardShape<_Float16>(c).bytes() : BackwardShape<float>(c).bytes();
+}
 int launch_linear(const LinearCall& c, hipStream_t s) {
     if (c.type == CER_TYPE_BF16) return linear_of<__bf16>(c, s);
     if (c.type == CER_TYPE_F16) return linear_of<_Float16>(c, s);

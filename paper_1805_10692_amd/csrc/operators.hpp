@@ -73,7 +73,9 @@ struct BlockCall {
     float scale, eps;
     bool post;
     float *rstd_post, *rstd_pre;
+    void* workspace;
 };
+int64_t block_room(const BlockCall& c);  // bytes of temporaries, here and below
 int launch_block_norm(const BlockCall& c, hipStream_t s);
 
 struct BlockBackwardCall {
@@ -86,7 +88,9 @@ struct BlockBackwardCall {
     int32_t post_weight_type, pre_weight_type;
     float scale;
     float *dgate_vector, *dpost_weight, *dpre_weight;
+    void* workspace;
 };
+int64_t block_backward_room(const BlockBackwardCall& c);
 int launch_block_norm_backward(const BlockBackwardCall& c, hipStream_t s);
 
 struct DropoutCall {
@@ -106,7 +110,9 @@ struct LinearCall {
     cer_tokens_t x, residual, y, pre;
     const void* bias;
     int32_t bias_type, activation;
+    void* workspace;
 };
+int64_t linear_room(const LinearCall& c);
 int launch_linear(const LinearCall& c, hipStream_t s);
 
 struct LinearBackwardCall {
@@ -119,7 +125,9 @@ struct LinearBackwardCall {
     void* dw;
     int64_t lddw;
     float* dbias;
+    void* workspace;
 };
+int64_t linear_backward_room(const LinearBackwardCall& c);
 int launch_linear_backward(const LinearBackwardCall& c, hipStream_t s);
 
 // A temporary for the length of a call, ordered on the stream.
@@ -133,6 +141,27 @@ struct Temporary {
     float* floats() const { return static_cast<float*>(p); }
     void* p = nullptr;
     hipStream_t stream;
+    int error = 0;
+};
+
+// All temporaries of a call in one: the caller's workspace, or one of the call's own.  A call that is being recorded has to bring its workspace.
+struct Room {
+    static size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+    Room(void* workspace, int64_t bytes, hipStream_t s) : own(workspace || !bytes || recorded(s) ? 0 : (size_t)bytes, s), at(static_cast<char*>(workspace ? workspace : own.p)) {
+        error = own.error ? own.error : bytes && !at ? (int)hipErrorStreamCaptureUnsupported : 0;
+    }
+    static bool recorded(hipStream_t s) {
+        hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+        return s && (hipStreamIsCapturing(s, &st) != hipSuccess || st != hipStreamCaptureStatusNone);
+    }
+    float* take(size_t bytes) {  // 256-byte aligned, as the workspace is
+        if (!bytes) return nullptr;
+        char* p = at;
+        at += rounded(bytes);
+        return reinterpret_cast<float*>(p);
+    }
+    Temporary own;
+    char* at;
     int error = 0;
 };
 

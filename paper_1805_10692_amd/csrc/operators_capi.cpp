@@ -60,6 +60,7 @@ bool apart(const void* out, std::initializer_list<const cer_tokens_t*> others) {
     return !out || std::none_of(others.begin(), others.end(), [&](const cer_tokens_t* m) { return there(m) && m->data == out; });
 }
 bool vector(const void* p, int type) { return !p || (number_type(type) && reinterpret_cast<uintptr_t>(p) % bytes_of(type) == 0); }
+bool room_enough(const void* workspace, int64_t have, int64_t need) { return !workspace || (have >= need && reinterpret_cast<uintptr_t>(workspace) % 16 == 0); }
 
 int check_linear(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, int32_t activation) {
     if (!W || !number_type(type) || tokens < 0 || in < 1 || out < 1 || ldw < 0) return CER_E_INVALID;
@@ -161,8 +162,28 @@ int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float*
 }
 
 
+int64_t linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t type, int32_t order, int32_t backward) {
+    if (tokens < 0 || in < 1 || out < 1 || !number_type(type) || (order != CER_ORDER_ROWS && !(order == CER_ORDER_COLUMNS && type == CER_TYPE_F32))) return CER_E_INVALID;
+    if (int e = check_linear(&type, in, type, tokens, in, out, CER_ACTIVATION_NONE)) return e == CER_E_TOO_LARGE ? e : CER_E_INVALID;
+    void* some = &type;  // everything is there
+    const cer_tokens_t m{some, 0, type, order};
+    if (!backward) return linear_room({some, in, type, tokens, in, out, m, m, m, m, some, type, CER_ACTIVATION_SILU, nullptr});
+    float all = 0;
+    return linear_backward_room({some, in, type, tokens, in, out, m, m, m, m, m, CER_ACTIVATION_SILU, some, in, &all, nullptr});
+}
+
+int64_t block_workspace_bytes(int64_t tokens, int64_t n, int32_t type, int32_t columns, int32_t backward) {
+    if (!number_type(type)) return CER_E_INVALID;
+    if (int e = check_block(tokens, n, nullptr, 0, nullptr, 0, nullptr, 0, 1.f)) return e;
+    float all = 0;
+    const cer_tokens_t stream{&all, 0, type, CER_ORDER_ROWS}, branch{&all, 0, columns ? CER_TYPE_F32 : type, columns ? CER_ORDER_COLUMNS : CER_ORDER_ROWS}, none{nullptr, 0, 0, 0};
+    if (!backward) return block_room({stream, branch, stream, branch, none, tokens, n, nullptr, 0, nullptr, nullptr, 0, 0, 1.f, 0.f, true, nullptr, nullptr, nullptr});
+    return block_backward_room({branch, stream, branch, none, none, stream, branch, none, tokens, n, &all, &all, &all, 0, nullptr, nullptr, 0, 0, 1.f, &all, &all, &all, nullptr});
+}
+
 int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* X, const cer_tokens_t* Y,
-                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* stream) {
+                  const void* bias, int32_t bias_type, const cer_tokens_t* residual, int32_t activation, const cer_tokens_t* pre, void* workspace,
+                  int64_t workspace_bytes, void* stream) {
     if (int e = check_linear(W, ldw, type, tokens, in, out, activation)) return e;
     if (!vector(bias, bias_type)) return CER_E_INVALID;
     if (tokens == 0) return CER_OK;
@@ -170,13 +191,14 @@ int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int6
     if (!none_or_like(residual, X, tokens, out, false) || !none_or_like(pre, X, tokens, out, true)) return CER_E_INVALID;
     if (there(residual) && !same_or_apart(residual, Y)) return CER_E_INVALID;
     if (Y->data == W || !apart(Y->data, {X, pre}) || (there(pre) && (pre->data == W || !apart(pre->data, {X, residual})))) return CER_E_INVALID;
-    LinearCall c{W, ldw, type, tokens, in, out, *X, or_none(residual), *Y, or_none(pre), bias, bias_type, activation};
+    LinearCall c{W, ldw, type, tokens, in, out, *X, or_none(residual), *Y, or_none(pre), bias, bias_type, activation, workspace};
+    if (!room_enough(workspace, workspace_bytes, linear_room(c))) return CER_E_INVALID;
     return result(launch_linear(c, static_cast<hipStream_t>(stream)));
 }
 
 int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, const cer_tokens_t* dY, const cer_tokens_t* X,
                     int32_t activation, const cer_tokens_t* pre, const cer_tokens_t* base, const cer_tokens_t* dX, void* dW, int64_t lddw, float* dbias,
-                    void* stream) {
+                    void* workspace, int64_t workspace_bytes, void* stream) {
     if (int e = check_linear(W, ldw, type, tokens, in, out, activation)) return e;
     if (dW && (lddw < in || (out > 1 && lddw > std::numeric_limits<int64_t>::max() / 8 / out) || reinterpret_cast<uintptr_t>(dW) % bytes_of(type) || dW == W)) return CER_E_INVALID;
     if (reinterpret_cast<uintptr_t>(dbias) % 4) return CER_E_INVALID;
@@ -190,13 +212,14 @@ int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, in
         if (!apart(dW, {dY, X, pre, base}) || !apart(dbias, {dY, X, pre, base, dX})) return CER_E_INVALID;
     }
     const cer_tokens_t none{nullptr, 0, 0, 0};
-    LinearBackwardCall c{W, ldw, type, tokens, in, out, or_none(dY), or_none(X), activation != CER_ACTIVATION_NONE ? or_none(pre) : none, or_none(base), or_none(dX), activation, dW, lddw, dbias};
+    LinearBackwardCall c{W, ldw, type, tokens, in, out, or_none(dY), or_none(X), activation != CER_ACTIVATION_NONE ? or_none(pre) : none, or_none(base), or_none(dX), activation, dW, lddw, dbias, workspace};
+    if (!room_enough(workspace, workspace_bytes, linear_backward_room(c))) return CER_E_INVALID;
     return result(launch_linear_backward(c, static_cast<hipStream_t>(stream)));
 }
 
 int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t* H, const cer_tokens_t* Y, int64_t tokens, int64_t n, const cer_tokens_t* gate,
                const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
-               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* stream) {
+               float eps, int32_t post, float* rstd_post, float* rstd_pre, void* workspace, int64_t workspace_bytes, void* stream) {
     if (int e = check_block(tokens, n, gate_vector, gate_type, post_weight, post_type, pre_weight, pre_type, scale)) return e;
     if (!(eps >= 0.f) || std::isinf(eps) || (!post && (post_weight || rstd_post)) || (gate_vector && there(gate))) return CER_E_INVALID;
     if (tokens == 0) return CER_OK;
@@ -206,14 +229,16 @@ int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t*
     if (F->data == Y->data && (!same_or_apart(F, Y) || F->order != CER_ORDER_ROWS)) return CER_E_INVALID;
     if (!none_or_like(gate, X, tokens, n, false)) return CER_E_INVALID;
     if (!apart(H->data, {F, Y, gate}) || !apart(Y->data, {X, gate})) return CER_E_INVALID;
-    BlockCall c{*X, *F, *H, *Y, or_none(gate), tokens, n, gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, eps, post != 0, rstd_post, rstd_pre};
+    BlockCall c{*X, *F, *H, *Y, or_none(gate), tokens, n, gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, eps, post != 0, rstd_post, rstd_pre, workspace};
+    if (!room_enough(workspace, workspace_bytes, block_room(c))) return CER_E_INVALID;
     return result(launch_block_norm(c, static_cast<hipStream_t>(stream)));
 }
 
 int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer_tokens_t* F, const float* rstd_pre, const float* rstd_post,
                         const cer_tokens_t* dX, const cer_tokens_t* dF, int64_t tokens, int64_t n, const cer_tokens_t* gate, const void* gate_vector,
                         int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,
-                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* stream) {
+                        const cer_tokens_t* dsum, const cer_tokens_t* dgate, float* dgate_vector, float* dpost_weight, float* dpre_weight, void* workspace,
+                        int64_t workspace_bytes, void* stream) {
     if (int e = check_block(tokens, n, gate_vector, gate_type, post_weight, post_type, pre_weight, pre_type, scale)) return e;
     if (gate_vector && there(gate)) return CER_E_INVALID;
     if (dgate_vector && !gate_vector) return CER_E_INVALID;
@@ -228,7 +253,8 @@ int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer
         if (there(dgate) && !apart(dgate->data, {dY, H, F, gate, dsum})) return CER_E_INVALID;
     }
     BlockBackwardCall c{or_none(dY), or_none(H), or_none(F), or_none(gate), or_none(dsum), or_none(dX), or_none(dF), or_none(dgate), tokens, n, rstd_post, rstd_pre,
-                        gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, dgate_vector, dpost_weight, dpre_weight};
+                        gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, dgate_vector, dpost_weight, dpre_weight, workspace};
+    if (!room_enough(workspace, workspace_bytes, block_backward_room(c))) return CER_E_INVALID;
     return result(launch_block_norm_backward(c, static_cast<hipStream_t>(stream)));
 }
 

@@ -435,6 +435,12 @@ bool number_of(PyObject* o, double otherwise, double* v) {
     *v = o ? PyFloat_AsDouble(o) : otherwise;
     return *v != -1.0 || !PyErr_Occurred();
 }
+// Any number of fp32 numbers, or nothing.
+struct Workspace {
+    void* at = nullptr;
+    int64_t numbers = 0;
+    bool of(PyObject* o, Device& dev) { return !o || flat_of(o, "workspace", dev, CER_TYPE_F32, -1, &at, nullptr, &numbers); }
+};
 // Matrices that a call wants in one order: a single token's or feature's is both, so that those of them that have a choice follow one that has none.
 template <int kMany>
 void one_order(cer_tokens_t* const (&m)[kMany], const int64_t (&features)[kMany], int64_t tokens) {
@@ -452,8 +458,8 @@ void one_order(cer_tokens_t* const (&m)[kMany], const int64_t (&features)[kMany]
 }
 
 PyObject* py_linear_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
-    static const char* const names[] = {"W", "X", "Y", "bias", "residual", "activation", "pre", "stream"};
-    enum { W, X, Y, kBias, kResidual, kActivation, kPre, kStream, kCount };
+    static const char* const names[] = {"W", "X", "Y", "bias", "residual", "activation", "pre", "workspace", "stream"};
+    enum { W, X, Y, kBias, kResidual, kActivation, kPre, kWorkspace, kStream, kCount };
     static const Signature f = {"linear_matmul", 3, kCount, names};
     PyObject* a[kCount];
     if (!take(f, args, nargs, kwnames, a)) return nullptr;
@@ -470,13 +476,14 @@ PyObject* py_linear_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, P
     one_order<4>({&x, &y, &r, &pre}, {in, out, out, out}, tokens);
     void* bias = nullptr;
     if (a[kBias] && !flat_of(a[kBias], "bias", dev, -1, out, &bias, &bias_type)) return nullptr;
-    if (!activation_of(a[kActivation], &kind) || !dev.stream(a[kStream], &stream)) return nullptr;
-    return call(g_fn.linear, f.name, w, ldw, type, tokens, in, out, &x, &y, static_cast<const void*>(bias), bias_type, &r, kind, &pre, stream);
+    Workspace work;
+    if (!activation_of(a[kActivation], &kind) || !work.of(a[kWorkspace], dev) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.linear, f.name, w, ldw, type, tokens, in, out, &x, &y, static_cast<const void*>(bias), bias_type, &r, kind, &pre, work.at, work.numbers * 4, stream);
 }
 
 PyObject* py_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
-    static const char* const names[] = {"W", "dY", "X", "activation", "pre", "base", "dX", "dW", "dbias", "stream"};
-    enum { W, kDY, X, kActivation, kPre, kBase, kDX, kDW, kDBias, kStream, kCount };
+    static const char* const names[] = {"W", "dY", "X", "activation", "pre", "base", "dX", "dW", "dbias", "workspace", "stream"};
+    enum { W, kDY, X, kActivation, kPre, kBase, kDX, kDW, kDBias, kWorkspace, kStream, kCount };
     static const Signature f = {"linear_backward", 2, kCount, names};
     PyObject* a[kCount];
     if (!take(f, args, nargs, kwnames, a)) return nullptr;
@@ -496,8 +503,10 @@ PyObject* py_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs,
     if (a[kDW] && !weights_of(a[kDW], "dW", dev, &dw, &lddw, &type, &out, &in)) return nullptr;
     void* dbias = nullptr;
     if (a[kDBias] && !flat_of(a[kDBias], "dbias", dev, CER_TYPE_F32, out, &dbias)) return nullptr;
-    if (!activation_of(a[kActivation], &kind) || !dev.stream(a[kStream], &stream)) return nullptr;
-    return call(g_fn.linear_backward, f.name, w, ldw, type, tokens, in, out, &dy, &x, kind, &pre, &base, &dx, const_cast<void*>(dw), lddw, static_cast<float*>(dbias), stream);
+    Workspace work;
+    if (!activation_of(a[kActivation], &kind) || !work.of(a[kWorkspace], dev) || !dev.stream(a[kStream], &stream)) return nullptr;
+    return call(g_fn.linear_backward, f.name, w, ldw, type, tokens, in, out, &dy, &x, kind, &pre, &base, &dx, const_cast<void*>(dw), lddw, static_cast<float*>(dbias), work.at,
+                work.numbers * 4, stream);
 }
 
 // gate: (n,) of any type, or (tokens, n)
@@ -518,8 +527,8 @@ struct Gate {
 };
 
 PyObject* py_block_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
-    static const char* const names[] = {"X", "F", "H", "Y", "gate", "post_weight", "pre_weight", "scale", "eps", "post", "rstd_post", "rstd_pre", "stream"};
-    enum { X, F, H, Y, kGate, kPostWeight, kPreWeight, kScale, kEps, kPost, kRstdPost, kRstdPre, kStream, kCount };
+    static const char* const names[] = {"X", "F", "H", "Y", "gate", "post_weight", "pre_weight", "scale", "eps", "post", "rstd_post", "rstd_pre", "workspace", "stream"};
+    enum { X, F, H, Y, kGate, kPostWeight, kPreWeight, kScale, kEps, kPost, kRstdPost, kRstdPre, kWorkspace, kStream, kCount };
     static const Signature f = {"block_norm", 4, kCount, names};
     PyObject* a[kCount];
     if (!take(f, args, nargs, kwnames, a)) return nullptr;
@@ -542,14 +551,17 @@ PyObject* py_block_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
     double scale, eps;
     if (!number_of(a[kScale], 1.0, &scale) || !number_of(a[kEps], 1e-6, &eps)) return nullptr;
     const int post = a[kPost] ? PyObject_IsTrue(a[kPost]) : 1;
-    if (post < 0 || !dev.stream(a[kStream], &stream)) return nullptr;
+    Workspace work;
+    if (post < 0 || !work.of(a[kWorkspace], dev) || !dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.block, f.name, &x, &o, &h, &y, tokens, n, &gate.each, static_cast<const void*>(gate.vector), gate.type, static_cast<const void*>(post_weight), post_type,
-                static_cast<const void*>(pre_weight), pre_type, (float)scale, (float)eps, post, static_cast<float*>(rstd_post), static_cast<float*>(rstd_pre), stream);
+                static_cast<const void*>(pre_weight), pre_type, (float)scale, (float)eps, post, static_cast<float*>(rstd_post), static_cast<float*>(rstd_pre), work.at,
+                work.numbers * 4, stream);
 }
 
 PyObject* py_block_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
-    static const char* const names[] = {"dY", "H", "F", "rstd_pre", "dX", "dF", "rstd_post", "gate", "post_weight", "pre_weight", "scale", "dsum", "dgate", "dpost_weight", "dpre_weight", "stream"};
-    enum { kDY, H, F, kRstdPre, kDX, kDF, kRstdPost, kGate, kPostWeight, kPreWeight, kScale, kDSum, kDGate, kDPostWeight, kDPreWeight, kStream, kCount };
+    static const char* const names[] = {"dY", "H", "F", "rstd_pre", "dX", "dF", "rstd_post", "gate", "post_weight", "pre_weight", "scale", "dsum", "dgate", "dpost_weight", "dpre_weight",
+                                        "workspace", "stream"};
+    enum { kDY, H, F, kRstdPre, kDX, kDF, kRstdPost, kGate, kPostWeight, kPreWeight, kScale, kDSum, kDGate, kDPostWeight, kDPreWeight, kWorkspace, kStream, kCount };
     static const Signature f = {"block_norm_backward", 6, kCount, names};
     PyObject* a[kCount];
     if (!take(f, args, nargs, kwnames, a)) return nullptr;
@@ -574,10 +586,11 @@ PyObject* py_block_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t na
     if (a[kDPostWeight] && !flat_of(a[kDPostWeight], "dpost_weight", dev, CER_TYPE_F32, n, &dpost)) return nullptr;
     if (a[kDPreWeight] && !flat_of(a[kDPreWeight], "dpre_weight", dev, CER_TYPE_F32, n, &dpre)) return nullptr;
     double scale;
-    if (!number_of(a[kScale], 1.0, &scale) || !dev.stream(a[kStream], &stream)) return nullptr;
+    Workspace work;
+    if (!number_of(a[kScale], 1.0, &scale) || !work.of(a[kWorkspace], dev) || !dev.stream(a[kStream], &stream)) return nullptr;
     return call(g_fn.block_backward, f.name, &dy, &h, &o, static_cast<const float*>(rstd_pre), static_cast<const float*>(rstd_post), &dx, &df, tokens, n, &gate.each,
                 static_cast<const void*>(gate.vector), gate.type, static_cast<const void*>(post_weight), post_type, static_cast<const void*>(pre_weight), pre_type, (float)scale, &dsum,
-                &dgate.each, static_cast<float*>(dgate.vector), static_cast<float*>(dpost), static_cast<float*>(dpre), stream);
+                &dgate.each, static_cast<float*>(dgate.vector), static_cast<float*>(dpost), static_cast<float*>(dpre), work.at, work.numbers * 4, stream);
 }
 
 PyObject* py_dropout_add(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
@@ -646,14 +659,15 @@ PyMethodDef g_methods[] = {
                  "adapter_backward(A, B, index, dY, X, hidden, scales=None, ranks=None, base=None, dX=None, dA=None, dB=None, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_norm", py_grad_norm, "grad_norm(grads, norm, stream=None)\n--\n\n"),
     CER_OPERATOR("grad_clip", py_grad_clip, "grad_clip(grads, max_norm, norm, outs=None, stream=None)\n--\n\n"),
-    CER_OPERATOR("linear_matmul", py_linear_matmul, "linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, stream=None)\n--\n\n"),
+    CER_OPERATOR("linear_matmul", py_linear_matmul, "linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, workspace=None, stream=None)\n--\n\n"),
     CER_OPERATOR("linear_backward", py_linear_backward,
-                 "linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, stream=None)\n--\n\n"),
+                 "linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, workspace=None, stream=None)\n--\n\n"),
     CER_OPERATOR("block_norm", py_block_norm,
-                 "block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, stream=None)\n--\n\n"),
+                 "block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, workspace=None, "
+                 "stream=None)\n--\n\n"),
     CER_OPERATOR("block_norm_backward", py_block_norm_backward,
                  "block_norm_backward(dY, H, F, rstd_pre, dX, dF, rstd_post=None, gate=None, post_weight=None, pre_weight=None, scale=1.0, dsum=None, dgate=None, "
-                 "dpost_weight=None, dpre_weight=None, stream=None)\n--\n\n"),
+                 "dpost_weight=None, dpre_weight=None, workspace=None, stream=None)\n--\n\n"),
     CER_OPERATOR("dropout_add", py_dropout_add, "dropout_add(X, Y, key, p, residual=None, call=0, stream=None)\n--\n\n"),
     {"setup", setup, METH_O, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},

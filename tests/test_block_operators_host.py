@@ -27,9 +27,9 @@ def test_declared_and_exported():
 
 
 @pytest.mark.parametrize("call,names", [
-    (B.linear_matmul, "W X Y bias residual activation pre stream"), (B.linear_backward, "W dY X activation pre base dX dW dbias stream"),
-    (B.block_norm, "X F H Y gate post_weight pre_weight scale eps post rstd_post rstd_pre stream"),
-    (B.block_norm_backward, "dY H F rstd_pre dX dF rstd_post gate post_weight pre_weight scale dsum dgate dpost_weight dpre_weight stream"),
+    (B.linear_matmul, "W X Y bias residual activation pre workspace stream"), (B.linear_backward, "W dY X activation pre base dX dW dbias workspace stream"),
+    (B.block_norm, "X F H Y gate post_weight pre_weight scale eps post rstd_post rstd_pre workspace stream"),
+    (B.block_norm_backward, "dY H F rstd_pre dX dF rstd_post gate post_weight pre_weight scale dsum dgate dpost_weight dpre_weight workspace stream"),
     (B.dropout_add, "X Y key p residual call stream")])
 def test_signatures(call, names):
     assert list(inspect.signature(call).parameters) == names.split()
@@ -49,8 +49,9 @@ def test_host_tensors_are_refused():
             call()
 
 
-def linear(W=AT, ldw=8, type=F32, n_tokens=4, n=8, m=6, x=tokens(at=2 * AT), y=tokens(at=3 * AT), bias=0, bias_type=F32, r=None, act=0, pre=None):
-    return B.lib().linear_matmul(P(W), I64(ldw), I32(type), I64(n_tokens), I64(n), I64(m), ref(x), ref(y), P(bias), I32(bias_type), ref(r), I32(act), ref(pre), None)
+def linear(W=AT, ldw=8, type=F32, n_tokens=4, n=8, m=6, x=tokens(at=2 * AT), y=tokens(at=3 * AT), bias=0, bias_type=F32, r=None, act=0, pre=None, work=0,
+           room=0):
+    return B.lib().linear_matmul(P(W), I64(ldw), I32(type), I64(n_tokens), I64(n), I64(m), ref(x), ref(y), P(bias), I32(bias_type), ref(r), I32(act), ref(pre), P(work), I64(room), None)
 
 
 def test_linear_refusals():
@@ -66,8 +67,10 @@ def test_linear_refusals():
         assert linear(**bad) == B.CER_E_TOO_LARGE, bad
 
 
-def linear_back(W=AT, ldw=8, type=F32, n_tokens=4, n=8, m=6, dy=tokens(at=2 * AT), x=tokens(at=3 * AT), act=0, pre=None, base=None, dx=tokens(at=4 * AT), dw=5 * AT, lddw=8, db=6 * AT):
-    return B.lib().linear_backward(P(W), I64(ldw), I32(type), I64(n_tokens), I64(n), I64(m), ref(dy), ref(x), I32(act), ref(pre), ref(base), ref(dx), P(dw), I64(lddw), P(db), None)
+def linear_back(W=AT, ldw=8, type=F32, n_tokens=4, n=8, m=6, dy=tokens(at=2 * AT), x=tokens(at=3 * AT), act=0, pre=None, base=None, dx=tokens(at=4 * AT), dw=5 * AT, lddw=8, db=6 * AT, work=0,
+                room=0):
+    return B.lib().linear_backward(P(W), I64(ldw), I32(type), I64(n_tokens), I64(n), I64(m), ref(dy), ref(x), I32(act), ref(pre), ref(base), ref(dx), P(dw), I64(lddw), P(db), P(work), I64(room),
+                                   None)
 
 
 def test_linear_backward_refusals():
@@ -82,9 +85,9 @@ def test_linear_backward_refusals():
 
 
 def block(x=tokens(), f=tokens(at=2 * AT), h=tokens(at=3 * AT), y=tokens(at=4 * AT), n_tokens=4, n=8, gate=None, vector=0, gate_type=F32, post_w=0, post_t=F32, pre_w=0, pre_t=F32, scale=1.0,
-          eps=1e-6, post=1, rstd_post=0, rstd_pre=0):
+          eps=1e-6, post=1, rstd_post=0, rstd_pre=0, work=0, room=0):
     return B.lib().block_norm(ref(x), ref(f), ref(h), ref(y), I64(n_tokens), I64(n), ref(gate), P(vector), I32(gate_type), P(post_w), I32(post_t), P(pre_w), I32(pre_t), F(scale), F(eps),
-                              I32(post), P(rstd_post), P(rstd_pre), None)
+                              I32(post), P(rstd_post), P(rstd_pre), P(work), I64(room), None)
 
 
 def test_block_refusals():
@@ -103,9 +106,9 @@ def test_block_refusals():
 
 
 def block_back(dy=tokens(), h=tokens(at=2 * AT), f=tokens(at=3 * AT), rstd_pre=AT, rstd_post=AT, dx=tokens(at=4 * AT), df=tokens(at=5 * AT), n_tokens=4, n=8, gate=None, vector=0, gate_type=F32,
-               post_w=0, post_t=F32, pre_w=0, pre_t=F32, scale=1.0, dsum=None, dgate=None, dvector=0, dpost=0, dpre=0):
+               post_w=0, post_t=F32, pre_w=0, pre_t=F32, scale=1.0, dsum=None, dgate=None, dvector=0, dpost=0, dpre=0, work=0, room=0):
     return B.lib().block_norm_backward(ref(dy), ref(h), ref(f), P(rstd_pre), P(rstd_post), ref(dx), ref(df), I64(n_tokens), I64(n), ref(gate), P(vector), I32(gate_type), P(post_w), I32(post_t),
-                                       P(pre_w), I32(pre_t), F(scale), ref(dsum), ref(dgate), P(dvector), P(dpost), P(dpre), None)
+                                       P(pre_w), I32(pre_t), F(scale), ref(dsum), ref(dgate), P(dvector), P(dpost), P(dpre), P(work), I64(room), None)
 
 
 def test_block_backward_refusals():
@@ -130,3 +133,27 @@ def test_dropout_refusals():
         assert call(**bad) == B.CER_E_INVALID, bad
     for bad in ({"n": (1 << 22) + 1}, {"n_tokens": (1 << 28) + 1}, {"n_tokens": 1 << 28, "n": 4097}):
         assert call(**bad) == B.CER_E_TOO_LARGE, bad
+
+
+def test_workspaces():
+    f32, bf16 = torch.float32, torch.bfloat16
+    assert B.linear_workspace_bytes(1, 4096, 4096, bf16) == 0 and B.linear_workspace_bytes(0, 8, 8, f32) == 0
+    need = B.linear_workspace_bytes(64, 9216, 4096, bf16)
+    assert need > 0 and need % 256 == 0
+    x, y = tokens(BF16, ld=9216, at=2 * AT), tokens(BF16, ld=4096, at=3 * AT)
+    sizes = dict(type=BF16, n_tokens=64, n=9216, m=4096, ldw=9216, x=x, y=y)
+    for work, room in ((AT, need - 1), (AT + 4, need), (AT, 0)):
+        assert linear(work=work, room=room, **sizes) == B.CER_E_INVALID
+    back = B.linear_workspace_bytes(300, 1000, 2000, f32, backward=True)
+    assert back >= 300 * 2000 * 4
+    wide = dict(n_tokens=300, n=1000, m=2000, ldw=1000, lddw=1000, dy=tokens(ld=2000, at=2 * AT), x=tokens(ld=1000, at=3 * AT), act=4, pre=tokens(ld=2000, at=7 * AT), dx=tokens(ld=1000, at=4 * AT))
+    assert linear_back(work=AT, room=300 * 2000 * 4 - 256, **wide) == B.CER_E_INVALID
+    assert B.block_workspace_bytes(100, 64, bf16) == 0 and B.block_workspace_bytes(100, 64, bf16, columns=True) == 2 * 100 * 64 * 4
+    assert B.block_workspace_bytes(100, 64, bf16, backward=True) > 0
+    assert block(f=tokens(order=COLUMNS, at=2 * AT), work=AT, room=127) == B.CER_E_INVALID
+    assert block_back(dpre=AT, work=AT, room=31) == B.CER_E_INVALID
+    for bad in (lambda: B.linear_workspace_bytes(-1, 8, 8, f32), lambda: B.linear_workspace_bytes(4, 0, 8, f32), lambda: B.linear_workspace_bytes(4, 8, 8, torch.int32),
+                lambda: B.linear_workspace_bytes(4, 8, 8, bf16, columns=True), lambda: B.block_workspace_bytes(4, 0, f32), lambda: B.block_workspace_bytes(4, 40000, f32),
+                lambda: B.block_workspace_bytes(4, 8, torch.float8_e4m3fn)):
+        with pytest.raises(B.CerError):
+            bad()
