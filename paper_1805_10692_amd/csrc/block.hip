@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void block_back_rows_kernel(BlockBackArgs
     __shared__ float room[2][kThreads / 64][48];
     F *with_pre = reinterpret_cast<F*>(lds), *with_gate = with_pre + kChunks * blockDim.x;
     const auto feature = [&](int c) { return ((int64_t)c * blockDim.x + threadIdx.x) * V; };
-    const unsigned group = threadIdx.y, groups = blockDim.y;
+    const unsigned group = __builtin_amdgcn_readfirstlane(threadIdx.y), groups = blockDim.y;  // the same for a whole wave: addresses of a token are scalar
     const auto token = [&](int64_t first) { return first + group < a.tokens ? first + group : a.tokens - 1; };  // a group without one repeats the last
     BackInputs<TX, TF, TD> in[kChunks];
     float next_r, next_q;

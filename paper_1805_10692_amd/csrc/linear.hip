@@ -495,12 +495,21 @@ size_t parts_bytes(const Plan& plan, int64_t rows, int64_t columns, int64_t dept
     parts_of<T>(depth, plan.parts, &of_part, &parts);
     return parts > 1 ? (size_t)((rows + plan.side - 1) / plan.side * ((columns + plan.side - 1) / plan.side)) * parts * plan.side * plan.side * 4 : 0;
 }
+// The plan of a product, that of its rest where there is one, and the bytes of their parts (they follow one another).
+struct Course {
+    Plan head, rest;
+    size_t bytes = 0;
+};
 template <class T>
-size_t product_bytes(int64_t rows, int64_t columns, int64_t depth, int turned) {
-    const Plan plan = plan_of<T>(rows, columns, depth, turned, true);
-    if (!plan.first) return parts_bytes<T>(plan, rows, columns, depth);
-    (plan.rows ? rows : columns) -= plan.first;
-    return parts_bytes<T>(plan_of<T>(rows, columns, depth, turned, false), rows, columns, depth);
+Course course_of(int64_t rows, int64_t columns, int64_t depth, int turned) {
+    Course c;
+    c.head = plan_of<T>(rows, columns, depth, turned, true);
+    if (c.head.first) {
+        (c.head.rows ? rows : columns) -= c.head.first;
+        c.rest = plan_of<T>(rows, columns, depth, turned, false);
+    }
+    c.bytes = parts_bytes<T>(c.head.first ? c.rest : c.head, rows, columns, depth);
+    return c;
 }
 
 template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead>
@@ -527,9 +536,8 @@ int launch_planned(const Product& p, const Plan& plan, bool turn_a, bool turn_b,
 int size_of(int32_t type) { return type == CER_TYPE_F32 ? 4 : 2; }
 
 template <class T>
-int launch_product(const Product& p, bool turn_a, bool turn_b, hipStream_t s) {
-    const int turned = turn_a + turn_b;
-    const Plan plan = plan_of<T>(p.rows, p.columns, p.depth, turned, true);
+int launch_product(const Product& p, const Course& course, bool turn_a, bool turn_b, hipStream_t s) {
+    const Plan& plan = course.head;
     if (!plan.first) return launch_planned<T>(p, plan, turn_a, turn_b, s);
     Product head = p, rest = p;
     const auto past = [](auto* at, int64_t bytes) { return at ? (std::remove_pointer_t<decltype(at)>*)((uintptr_t)at + bytes) : at; };
@@ -543,7 +551,7 @@ int launch_product(const Product& p, bool turn_a, bool turn_b, hipStream_t s) {
     rest.to.pre = past(p.to.pre, plan.first * (plan.rows ? p.to.ldp : 1) * item);
     rest.to.out = past(p.to.out, plan.first * (plan.rows ? p.to.ldo : 1) * item);
     if (int e = launch_planned<T>(head, plan, turn_a, turn_b, s)) return e;
-    return launch_planned<T>(rest, plan_of<T>(rest.rows, rest.columns, rest.depth, turned, false), turn_a, turn_b, s);
+    return launch_planned<T>(rest, course.rest, turn_a, turn_b, s);
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------------
@@ -742,10 +750,13 @@ __global__ __launch_bounds__(1024) void bias_totals_kernel(const float* part, ui
 }
 
 template <class T>
-int64_t linear_bytes(const LinearCall& c) {
+Course linear_course(const LinearCall& c) {
     const bool columns = c.x.order == CER_ORDER_COLUMNS;
-    if (!c.tokens || few_tokens(c.tokens, c.in, c.out, sizeof(T))) return 0;
-    return (int64_t)Room::rounded(product_bytes<T>(columns ? c.out : c.tokens, columns ? c.tokens : c.out, c.in, columns));
+    return course_of<T>(columns ? c.out : c.tokens, columns ? c.tokens : c.out, c.in, columns);
+}
+template <class T>
+int64_t linear_bytes(const LinearCall& c) {
+    return !c.tokens || few_tokens(c.tokens, c.in, c.out, sizeof(T)) ? 0 : (int64_t)Room::rounded(linear_course<T>(c).bytes);
 }
 template <class T>
 int linear_of(const LinearCall& c, hipStream_t s) {
@@ -762,10 +773,11 @@ int linear_of(const LinearCall& c, hipStream_t s) {
     p.b = columns ? c.x.data : c.w, p.ldb = columns ? c.x.ld : c.ldw;
     p.rows = columns ? c.out : c.tokens, p.columns = columns ? c.tokens : c.out, p.depth = c.in;
     p.to = to;
-    Room room(c.workspace, linear_bytes<T>(c), s);
+    const Course course = linear_course<T>(c);
+    Room room(c.workspace, (int64_t)course.bytes, s);
     if (room.error) return room.error;
-    p.part = room.take((size_t)linear_bytes<T>(c));
-    return launch_product<T>(p, false, columns, s);
+    p.part = room.take(course.bytes);
+    return launch_product<T>(p, course, false, columns, s);
 }
 
 // What a backward call needs and how it goes about the gradient of z.
@@ -775,6 +787,7 @@ struct BackwardShape {
     bool columns, act, brief;
     int64_t lanes, blocks, tokens_of_part, parts;
     size_t dz, sums, product;
+    Course to_x, to_w;
     // Rows: about a thousand workgroups of whole lines.  A few hundred tokens: all of them in one of 64 bytes' features, which needs no second launch (257 x 2049 fp32 10.7 us for 13.4).
     explicit BackwardShape(const LinearBackwardCall& c) : columns(c.dy.order == CER_ORDER_COLUMNS), act(c.activation != CER_ACTIVATION_NONE), brief(!columns && c.tokens <= 512) {
         lanes = brief ? 4 : 64, blocks = (c.out + lanes * V - 1) / (lanes * V);
@@ -782,9 +795,9 @@ struct BackwardShape {
         tokens_of_part = std::max<int64_t>(1, (c.tokens + most - 1) / most), parts = (c.tokens + tokens_of_part - 1) / tokens_of_part;
         dz = act && (c.dx.data || c.dw) ? (size_t)c.tokens * c.out * sizeof(T) : 0;
         sums = c.dbias && parts > 1 && !columns ? (size_t)parts * c.out * 4 : 0;
-        product = 0;
-        if (c.dx.data && c.tokens) product = product_bytes<T>(columns ? c.in : c.tokens, columns ? c.tokens : c.in, c.out, columns ? 2 : 1);
-        if (c.dw) product = std::max(product, product_bytes<T>(c.out, c.in, c.tokens, columns ? 0 : 2));
+        if (c.dx.data && c.tokens) to_x = course_of<T>(columns ? c.in : c.tokens, columns ? c.tokens : c.in, c.out, columns ? 2 : 1);
+        if (c.dw) to_w = course_of<T>(c.out, c.in, c.tokens, columns ? 0 : 2);
+        product = std::max(to_x.bytes, to_w.bytes);
     }
     int64_t bytes() const { return (int64_t)(Room::rounded(dz) + Room::rounded(sums) + Room::rounded(product)); }
 };
@@ -820,7 +833,7 @@ int linear_backward_of(const LinearBackwardCall& c, hipStream_t s) {
         p.rows = columns ? c.in : c.tokens, p.columns = columns ? c.tokens : c.in, p.depth = c.out;
         p.part = part;
         p.to.residual = c.base.data, p.to.ldr = c.base.ld, p.to.out = c.dx.data, p.to.ldo = c.dx.ld;
-        if (int e = launch_product<T>(p, columns, true, s)) return e;
+        if (int e = launch_product<T>(p, shape.to_x, columns, true, s)) return e;
     }
     if (c.dw) {
         Product p{};
@@ -828,7 +841,7 @@ int linear_backward_of(const LinearBackwardCall& c, hipStream_t s) {
         p.rows = c.out, p.columns = c.in, p.depth = c.tokens;
         p.part = part;
         p.to.out = c.dw, p.to.ldo = c.lddw;
-        if (int e = launch_product<T>(p, !columns, !columns, s)) return e;
+        if (int e = launch_product<T>(p, shape.to_w, !columns, !columns, s)) return e;
     }
     return 0;
 }

@@ -60,7 +60,7 @@ bool apart(const void* out, std::initializer_list<const cer_tokens_t*> others) {
     return !out || std::none_of(others.begin(), others.end(), [&](const cer_tokens_t* m) { return there(m) && m->data == out; });
 }
 bool vector(const void* p, int type) { return !p || (number_type(type) && reinterpret_cast<uintptr_t>(p) % bytes_of(type) == 0); }
-bool room_enough(const void* workspace, int64_t have, int64_t need) { return !workspace || (have >= need && reinterpret_cast<uintptr_t>(workspace) % 16 == 0); }
+bool room_enough(const void* workspace, int64_t have, int64_t need) { return have >= need && reinterpret_cast<uintptr_t>(workspace) % 16 == 0; }
 
 int check_linear(const void* W, int64_t ldw, int32_t type, int64_t tokens, int64_t in, int64_t out, int32_t activation) {
     if (!W || !number_type(type) || tokens < 0 || in < 1 || out < 1 || ldw < 0) return CER_E_INVALID;
@@ -192,7 +192,7 @@ int linear_matmul(const void* W, int64_t ldw, int32_t type, int64_t tokens, int6
     if (there(residual) && !same_or_apart(residual, Y)) return CER_E_INVALID;
     if (Y->data == W || !apart(Y->data, {X, pre}) || (there(pre) && (pre->data == W || !apart(pre->data, {X, residual})))) return CER_E_INVALID;
     LinearCall c{W, ldw, type, tokens, in, out, *X, or_none(residual), *Y, or_none(pre), bias, bias_type, activation, workspace};
-    if (!room_enough(workspace, workspace_bytes, linear_room(c))) return CER_E_INVALID;
+    if (workspace && !room_enough(workspace, workspace_bytes, linear_room(c))) return CER_E_INVALID;
     return result(launch_linear(c, static_cast<hipStream_t>(stream)));
 }
 
@@ -213,7 +213,7 @@ int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, in
     }
     const cer_tokens_t none{nullptr, 0, 0, 0};
     LinearBackwardCall c{W, ldw, type, tokens, in, out, or_none(dY), or_none(X), activation != CER_ACTIVATION_NONE ? or_none(pre) : none, or_none(base), or_none(dX), activation, dW, lddw, dbias, workspace};
-    if (!room_enough(workspace, workspace_bytes, linear_backward_room(c))) return CER_E_INVALID;
+    if (workspace && !room_enough(workspace, workspace_bytes, linear_backward_room(c))) return CER_E_INVALID;
     return result(launch_linear_backward(c, static_cast<hipStream_t>(stream)));
 }
 
@@ -230,7 +230,7 @@ int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t*
     if (!none_or_like(gate, X, tokens, n, false)) return CER_E_INVALID;
     if (!apart(H->data, {F, Y, gate}) || !apart(Y->data, {X, gate})) return CER_E_INVALID;
     BlockCall c{*X, *F, *H, *Y, or_none(gate), tokens, n, gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, eps, post != 0, rstd_post, rstd_pre, workspace};
-    if (!room_enough(workspace, workspace_bytes, block_room(c))) return CER_E_INVALID;
+    if (workspace && !room_enough(workspace, workspace_bytes, block_room(c))) return CER_E_INVALID;
     return result(launch_block_norm(c, static_cast<hipStream_t>(stream)));
 }
 
@@ -254,7 +254,7 @@ int block_norm_backward(const cer_tokens_t* dY, const cer_tokens_t* H, const cer
     }
     BlockBackwardCall c{or_none(dY), or_none(H), or_none(F), or_none(gate), or_none(dsum), or_none(dX), or_none(dF), or_none(dgate), tokens, n, rstd_post, rstd_pre,
                         gate_vector, gate_type, post_weight, pre_weight, post_type, pre_type, scale, dgate_vector, dpost_weight, dpre_weight, workspace};
-    if (!room_enough(workspace, workspace_bytes, block_backward_room(c))) return CER_E_INVALID;
+    if (workspace && !room_enough(workspace, workspace_bytes, block_backward_room(c))) return CER_E_INVALID;
     return result(launch_block_norm_backward(c, static_cast<hipStream_t>(stream)));
 }
 

@@ -96,6 +96,27 @@ def test_a_recorded_call_without_its_workspace_is_refused(name):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("first,second", [("parts", "parts' gradient"), ("block's gradient", "wide block's gradient"), ("block's gradient, columns", "tiles' gradient")])
+def test_two_streams_with_a_workspace_each(first, second):
+    both, want = [made(first), made(second)], []
+    for call, _, outputs in both:
+        call()
+        torch.cuda.synchronize()
+        want.append([y.clone() for y in outputs])
+        for y in outputs:
+            y.fill_(-1.0)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (call, _, _), s in zip(both, streams):
+            with torch.cuda.stream(s):
+                call()
+    torch.cuda.synchronize()
+    for (_, _, outputs), exact in zip(both, want):
+        for a, b in zip(outputs, exact):
+            assert torch.equal(a, b)
+
+
 FAULTED = "calls that allocate their temporaries, recorded or on two streams at once, were among those of a run that ended with a GPU fault whose cause was not found"
 
 
