@@ -8,10 +8,14 @@
 //
 // A workgroup forms a tile of C.  128 bytes of k (64 numbers of 16 bits, 32 of fp32) of all its rows go from memory through registers into LDS while
 // the tile before is multiplied: by element-aligned loads, so that any leading dimension works, and an operand whose k lies a line apart is turned in
-// registers on the way (8 x 4 numbers a thread).  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
+// registers on the way.  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
 // stores and the operand loads of 32 rows touch every bank evenly.  The matrix instruction takes B's rows as its first operand: a lane
 // then has four neighbouring j of one i.  fp32 goes through the 32-bit instruction.  Sums are fp32; each C is rounded once, after the epilogue.
-// Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order.
+// Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order (`plan_of`).
+//
+// What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 126 us, 1090 TFLOP/s; without its loads 123, without
+// stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's clock falls under them).  A large library product reaches 1123 on this card.
+// fp32: 105 - 111 TFLOP/s of 154.  4096 tokens, 4096 -> 9216 bf16, forward 332 us (2.25 rounds), dX 291, dW 312, dz 56.
 #include <algorithm>
 #include <type_traits>
 
@@ -121,18 +125,18 @@ __device__ __forceinline__ F16 multiply(Chunk a, Chunk b, F16 c) {
     }
 }
 
-// One operand's way from memory to LDS: kRows rows of 128 bytes of k, kAhead tiles of them on their way in registers.  Of rows past the matrix any others are
+// One operand's way from memory to LDS: kRows rows of 128 bytes of k, a tile of them on its way in registers.  Of rows past the matrix any others are
 // read in their place (their results are dropped); k past the end is 0 on both sides.
-template <class T, int kRows, int kThreads, bool kTurn, int kAhead, bool kFar, int kLine>
+template <class T, int kRows, int kThreads, bool kTurn, bool kFar, int kLine>
 struct Stage {
     static constexpr int E = 16 / sizeof(T), kDepth = 8 * E;
     static constexpr int kPieces = kTurn ? kRows / kLine * 8 : kRows * 8, kCount = kPieces / kThreads;  // turned: kLine rows by a chunk
     const T* at[kCount];
     uint32_t to[kCount][kTurn ? kLine : 1];  // chunks of LDS
-    Chunk held[kAhead][kTurn ? 1 : kCount];
+    Chunk held[kTurn ? 1 : kCount];
     static constexpr int kWords = kLine * (int)sizeof(T) / 4;
     using Line = Vec<uint32_t, kWords>;
-    Line lines[kAhead][kTurn ? kCount : 1][kTurn ? E : 1];
+    Line lines[kTurn ? kCount : 1][kTurn ? E : 1];
 
     static __device__ __forceinline__ unsigned piece(int n) { return threadIdx.x % kThreads + n * kThreads; }
     static_assert(kPieces % kThreads == 0, "every thread has as much");
@@ -158,27 +162,27 @@ struct Stage {
         }
     }
     // The kDepth of k at hand, all of them in the matrix.
-    __device__ __forceinline__ void load_whole(int slot, int64_t ld) {
+    __device__ __forceinline__ void load_whole(int64_t ld) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             if constexpr (kTurn) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) lines[slot][n][q] = __builtin_bit_cast(Line, (load<T, kLine>(at[n] + q * ld)));
+                for (int q = 0; q < E; ++q) lines[n][q] = __builtin_bit_cast(Line, (load<T, kLine>(at[n] + q * ld)));
             } else {
-                held[slot][n] = __builtin_bit_cast(Chunk, (load<T, E>(at[n])));
+                held[n] = __builtin_bit_cast(Chunk, (load<T, E>(at[n])));
             }
         }
     }
     // The same where `remain` of k are left, and (turned) fewer than kLine rows may be.
-    __device__ __forceinline__ void load_some(int slot, int64_t ld, int64_t remain, int64_t row0, int64_t rows) {
+    __device__ __forceinline__ void load_some(int64_t ld, int64_t remain, int64_t row0, int64_t rows) {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             const int64_t k = remain - chunk(n) * E, most = inside(rows) ? kLine : rows - row0 - row(n);
             if constexpr (kTurn) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) lines[slot][n][q] = __builtin_bit_cast(Line, (load_own<T, kLine>(at[n] + q * ld, q < k ? most : 0)));
+                for (int q = 0; q < E; ++q) lines[n][q] = __builtin_bit_cast(Line, (load_own<T, kLine>(at[n] + q * ld, q < k ? most : 0)));
             } else {
-                held[slot][n] = __builtin_bit_cast(Chunk, (load_own<T, E>(at[n], k)));
+                held[n] = __builtin_bit_cast(Chunk, (load_own<T, E>(at[n], k)));
             }
         }
     }
@@ -186,7 +190,7 @@ struct Stage {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) at[n] += kDepth * (kTurn ? ld : 1);
     }
-    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const {
+    __device__ __forceinline__ void to_lds(Chunk* room) const {
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
             if constexpr (kTurn) {
@@ -195,13 +199,13 @@ struct Stage {
                     Chunk line;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        if constexpr (sizeof(T) == 4) line[w] = lines[slot][n][w][r];
-                        else line[w] = __builtin_amdgcn_perm(lines[slot][n][(2 * w + 1) % E][r / 2], lines[slot][n][2 * w % E][r / 2], r % 2 ? 0x07060302u : 0x05040100u);
+                        if constexpr (sizeof(T) == 4) line[w] = lines[n][w][r];
+                        else line[w] = __builtin_amdgcn_perm(lines[n][(2 * w + 1) % E][r / 2], lines[n][2 * w % E][r / 2], r % 2 ? 0x07060302u : 0x05040100u);
                     }
                     room[to[n][r]] = line;
                 }
             } else {
-                room[to[n][0]] = held[slot][n];
+                room[to[n][0]] = held[n];
             }
         }
     }
@@ -209,10 +213,10 @@ struct Stage {
 
 // Both operands' way.  Where both are turned a half of the workgroup takes one each: a thread has eight rows of one of them and not four of both, 16 bytes
 // of a line and not 8, in half as many requests (dW of 4096 tokens, 4096 -> 9216 bf16: 370 -> 343 us).
-template <class T, int kI, int kJ, int kThreads, int kAhead, bool kTurnA, bool kTurnB, bool kFar>
+template <class T, int kI, int kJ, int kThreads, bool kTurnA, bool kTurnB, bool kFar>
 struct Operands {
-    using A = Stage<T, kI, kThreads, kTurnA, kAhead, kFar, kI * 8 / kThreads>;
-    using B = Stage<T, kJ, kThreads, kTurnB, kAhead, kFar, kJ * 8 / kThreads>;
+    using A = Stage<T, kI, kThreads, kTurnA, kFar, kI * 8 / kThreads>;
+    using B = Stage<T, kJ, kThreads, kTurnB, kFar, kJ * 8 / kThreads>;
     A a;
     B b;
     __device__ __forceinline__ bool inside(const Product& p) const { return A::inside(p.rows) && B::inside(p.columns); }
@@ -220,38 +224,38 @@ struct Operands {
         a.start(p.a, p.lda, i0, p.rows, k0);
         b.start(p.b, p.ldb, j0, p.columns, k0);
     }
-    __device__ __forceinline__ void load_whole(int slot, const Product& p) {
-        a.load_whole(slot, p.lda);
-        b.load_whole(slot, p.ldb);
+    __device__ __forceinline__ void load_whole(const Product& p) {
+        a.load_whole(p.lda);
+        b.load_whole(p.ldb);
     }
-    __device__ __forceinline__ void load_some(int slot, const Product& p, int64_t remain, int64_t i0, int64_t j0) {
-        a.load_some(slot, p.lda, remain, i0, p.rows);
-        b.load_some(slot, p.ldb, remain, j0, p.columns);
+    __device__ __forceinline__ void load_some(const Product& p, int64_t remain, int64_t i0, int64_t j0) {
+        a.load_some(p.lda, remain, i0, p.rows);
+        b.load_some(p.ldb, remain, j0, p.columns);
     }
     __device__ __forceinline__ void advance(const Product& p) {
         a.advance(p.lda);
         b.advance(p.ldb);
     }
-    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const {
-        a.to_lds(slot, room);
-        b.to_lds(slot, room + kI * 8);
+    __device__ __forceinline__ void to_lds(Chunk* room) const {
+        a.to_lds(room);
+        b.to_lds(room + kI * 8);
     }
     // One of the two steps in which a tile is exchanged.
-    __device__ __forceinline__ void exchange(unsigned step, int slot, Chunk* room, const Product& p, bool more) {
+    __device__ __forceinline__ void exchange(unsigned step, Chunk* room, const Product& p, bool more) {
         if (step == 0) {
-            a.to_lds(slot, room);
+            a.to_lds(room);
             if (more) a.advance(p.lda);
-            a.load_whole(slot, p.lda);
+            a.load_whole(p.lda);
         } else {
-            b.to_lds(slot, room + kI * 8);
+            b.to_lds(room + kI * 8);
             if (more) b.advance(p.ldb);
-            b.load_whole(slot, p.ldb);
+            b.load_whole(p.ldb);
         }
     }
 };
-template <class T, int kSide, int kThreads, int kAhead>
+template <class T, int kSide, int kThreads>
 struct Halves {
-    using S = Stage<T, kSide, kThreads / 2, true, kAhead, true, kSide * 16 / kThreads>;
+    using S = Stage<T, kSide, kThreads / 2, true, true, kSide * 16 / kThreads>;
     S s;
     int64_t ld;
     __device__ __forceinline__ static bool second() { return __builtin_amdgcn_readfirstlane(threadIdx.x / (kThreads / 2)); }
@@ -260,17 +264,17 @@ struct Halves {
         ld = second() ? p.ldb : p.lda;
         s.start(second() ? p.b : p.a, ld, second() ? j0 : i0, second() ? p.columns : p.rows, k0);
     }
-    __device__ __forceinline__ void load_whole(int slot, const Product&) { s.load_whole(slot, ld); }
-    __device__ __forceinline__ void load_some(int slot, const Product& p, int64_t remain, int64_t i0, int64_t j0) {
-        s.load_some(slot, ld, remain, second() ? j0 : i0, second() ? p.columns : p.rows);
+    __device__ __forceinline__ void load_whole(const Product&) { s.load_whole(ld); }
+    __device__ __forceinline__ void load_some(const Product& p, int64_t remain, int64_t i0, int64_t j0) {
+        s.load_some(ld, remain, second() ? j0 : i0, second() ? p.columns : p.rows);
     }
     __device__ __forceinline__ void advance(const Product&) { s.advance(ld); }
-    __device__ __forceinline__ void to_lds(int slot, Chunk* room) const { s.to_lds(slot, room + (second() ? kSide * 8 : 0)); }
-    __device__ __forceinline__ void exchange(unsigned step, int slot, Chunk* room, const Product&, bool more) {
+    __device__ __forceinline__ void to_lds(Chunk* room) const { s.to_lds(room + (second() ? kSide * 8 : 0)); }
+    __device__ __forceinline__ void exchange(unsigned step, Chunk* room, const Product&, bool more) {
         if (step != 0) return;
-        s.to_lds(slot, room + (second() ? kSide * 8 : 0));
+        s.to_lds(room + (second() ? kSide * 8 : 0));
         if (more) s.advance(ld);
-        s.load_whole(slot, ld);
+        s.load_whole(ld);
     }
 };
 
@@ -289,14 +293,14 @@ __device__ __forceinline__ void tile_of(unsigned at, unsigned tiles_i, unsigned 
 // A barrier for LDS alone: __syncthreads would also wait for the loads from memory that are on their way for the tile after next.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead, bool kTurnA, bool kTurnB>
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB>
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
     constexpr int kDepth = 128 / sizeof(T);
     constexpr bool kHalves = kTurnA && kTurnB && kI == kJ;
     constexpr bool kFar = kHalves || kI == 256;  // eight rows a thread want it; elsewhere it costs registers (dX of 512 tokens 39 -> 45 us), or none that are missed (4096: 305 -> 290)
-    using Way = std::conditional_t<kHalves, Halves<T, kI, kThreads, kAhead>, Operands<T, kI, kJ, kThreads, kAhead, kTurnA, kTurnB, kFar>>;
+    using Way = std::conditional_t<kHalves, Halves<T, kI, kThreads>, Operands<T, kI, kJ, kThreads, kTurnA, kTurnB, kFar>>;
     __shared__ Chunk room[2][(kI + kJ) * 8];
     static_assert(sizeof(room) >= sizeof(float) * kWavesI * kWavesJ * 32 * kPitch, "");
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wave_i = wave / kWavesJ, wave_j = wave % kWavesJ;
@@ -328,39 +332,31 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
 #pragma unroll
             for (int j = 0; j < kTilesJ; ++j) sums[i][j] = multiply<T>(v[j], u[i], sums[i][j]);
     };
-    // Whole tiles.  While tile k is multiplied out of one half of LDS, tile k + 1 goes from registers into the other half and the kAhead after it are on their
-    // way from memory; past the last one the last is read again, for nobody.
+    // Whole tiles.  While tile k is multiplied out of one half of LDS, tile k + 1 goes from registers into the other half and tile k + 2 is on its way from
+    // memory; past the last one the last is read again, for nobody.  (Two or four tiles on their way gained nothing.)
     unsigned turn = 0;
     const int64_t whole = way.inside(p) && remain > 0 ? remain / kDepth : 0;
     if (whole) {
-        way.load_whole(0, p);
-        way.to_lds(0, room[0]);
-#pragma unroll
-        for (int ahead = 0; ahead < kAhead; ++ahead) {
-            if (ahead + 1 < whole) way.advance(p);
-            way.load_whole(ahead, p);
-        }
+        way.load_whole(p);
+        way.to_lds(room[0]);
+        if (whole > 1) way.advance(p);
+        way.load_whole(p);
         lds_barrier();
         operands(room[0], 0, x[0], y[0]);
-        for (int64_t k0 = 0; k0 < whole; k0 += kAhead) {
+        for (int64_t k = 0; k < whole; ++k, turn ^= 1) {
+            const bool more = k + 2 < whole;
 #pragma unroll
-            for (int slot = 0; slot < kAhead; ++slot) {
-                if (k0 + slot >= whole) break;
-                const bool more = k0 + slot + kAhead + 1 < whole;
-#pragma unroll
-                for (unsigned step = 0; step < 4; ++step) {
-                    if (step < 3) {
-                        operands(room[turn], step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
-                    } else {  // every operand of this tile is in registers: the next tile's first ones come while the last products run
-                        lds_barrier();
-                        operands(room[turn ^ 1], 0, x[0], y[0]);
-                    }
-                    if (step < 2) way.exchange(step, slot, room[turn ^ 1], p, more);
-                    __builtin_amdgcn_sched_barrier(0);  // the compiler would move requests down to where their answers are needed
-                    products(x[step & 1], y[step & 1]);
-                    __builtin_amdgcn_sched_barrier(0);
+            for (unsigned step = 0; step < 4; ++step) {
+                if (step < 3) {
+                    operands(room[turn], step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
+                } else {  // every operand of this tile is in registers: the next tile's first ones come while the last products run
+                    lds_barrier();
+                    operands(room[turn ^ 1], 0, x[0], y[0]);
                 }
-                turn ^= 1;
+                if (step < 2) way.exchange(step, room[turn ^ 1], p, more);
+                __builtin_amdgcn_sched_barrier(0);  // the compiler would move requests down to where their answers are needed
+                products(x[step & 1], y[step & 1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         lds_barrier();
@@ -369,8 +365,8 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     }
     // What is left: a part of a tile, or all of them where a turned operand has fewer rows than are read at once.
     while (remain > 0) {
-        way.load_some(0, p, remain, i0, j0);
-        way.to_lds(0, room[turn]);
+        way.load_some(p, remain, i0, j0);
+        way.to_lds(room[turn]);
         lds_barrier();
 #pragma unroll
         for (unsigned step = 0; step < 4; ++step) {
@@ -512,15 +508,15 @@ Course course_of(int64_t rows, int64_t columns, int64_t depth, int turned) {
     return c;
 }
 
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, int kAhead>
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ>
 int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t s) {
     p.tiles_i = (uint32_t)((p.rows + kI - 1) / kI), p.tiles_j = (uint32_t)((p.columns + kJ - 1) / kJ);
     parts_of<T>(p.depth, parts, &p.depth_of_part, &p.parts);
     const unsigned tiles = p.tiles_i * p.tiles_j;
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, kAhead, true, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, true, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
     if (int e = (int)hipGetLastError()) return e;
     if (p.parts > 1) parts_kernel<T, kI, kJ><<<dim3(kI * kJ / 1024, tiles), 256, 0, s>>>(p);
     return (int)hipGetLastError();
@@ -528,9 +524,9 @@ int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t
 
 template <class T>
 int launch_planned(const Product& p, const Plan& plan, bool turn_a, bool turn_b, hipStream_t s) {
-    if (plan.side == 64) return launch_tiles<T, 64, 64, 2, 2, 1>(p, plan.parts, turn_a, turn_b, s);
-    if (plan.side == 128) return launch_tiles<T, 128, 128, 2, 2, 1>(p, plan.parts, turn_a, turn_b, s);
-    if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4, 1>(p, plan.parts, turn_a, turn_b, s);
+    if (plan.side == 64) return launch_tiles<T, 64, 64, 2, 2>(p, plan.parts, turn_a, turn_b, s);
+    if (plan.side == 128) return launch_tiles<T, 128, 128, 2, 2>(p, plan.parts, turn_a, turn_b, s);
+    if constexpr (sizeof(T) == 2) return launch_tiles<T, 256, 256, 2, 4>(p, plan.parts, turn_a, turn_b, s);
     return (int)hipErrorInvalidValue;
 }
 int size_of(int32_t type) { return type == CER_TYPE_F32 ? 4 : 2; }
