@@ -15,7 +15,7 @@
 //
 // What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 126 us, 1090 TFLOP/s; without its loads 123, without
 // stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's clock falls under them).  A large library product reaches 1123 on this card.
-// fp32: 105 - 111 TFLOP/s of 154.  4096 tokens, 4096 -> 9216 bf16, forward 332 us (2.25 rounds), dX 291, dW 312, dz 56.
+// fp32: 105 - 111 TFLOP/s of 154.  4096 tokens, 4096 -> 9216 bf16, forward 308 us (2.25 rounds), dX 284, dW 311, dz 56.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,15 +48,31 @@ __device__ __forceinline__ float normal_share(float z) { return 0.5f * erfcf(-kH
 __device__ __forceinline__ float tanh_argument(float z) { return 2.f * kTanhFactor * z * fmaf(kTanhCube * z, z, 1.f); }
 // z . share; a share of 0 has its limit for an infinite z.
 __device__ __forceinline__ float part_of(float z, float share) { return share == 0.f ? 0.f : z * share; }
+// z / (1 + 2^-t)
+__device__ __forceinline__ float share_of(float z, float t) { return part_of(z, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-t))); }
+constexpr float kLog2E = 1.4426950408889634f;
 
-__device__ __forceinline__ float activate(float z, int kind) {
+__device__ __forceinline__ Vec<float, 4> activate(Vec<float, 4> z, int kind) {  // one branch for four
     switch (kind) {
-        case CER_ACTIVATION_RELU: return z < 0.f ? 0.f : z;  // NaN stays
-        case CER_ACTIVATION_GELU: return part_of(z, normal_share(z));
-        case CER_ACTIVATION_GELU_TANH: return part_of(z, Logistic(tanh_argument(z)).q);
-        case CER_ACTIVATION_SILU: return part_of(z, Logistic(z).q);
-        default: return z;
+        case CER_ACTIVATION_RELU:
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[q] = z[q] < 0.f ? 0.f : z[q];  // NaN stays
+            break;
+        case CER_ACTIVATION_GELU:
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[q] = part_of(z[q], normal_share(z[q]));
+            break;
+        case CER_ACTIVATION_GELU_TANH:
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[q] = share_of(z[q], z[q] * fmaf(2.f * kTanhFactor * kLog2E * kTanhCube * z[q], z[q], 2.f * kTanhFactor * kLog2E));
+            break;
+        case CER_ACTIVATION_SILU:
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[q] = share_of(z[q], z[q] * kLog2E);
+            break;
+        default: break;
     }
+    return z;
 }
 __device__ __forceinline__ float slope(float z, int kind) {
     switch (kind) {
@@ -94,14 +110,15 @@ struct Product {
     float* part;  // [tiles][parts][rows of a tile][columns of a tile]
 };
 
-// Four neighbouring j of row i, `left` of them in the matrix.
+// Four neighbouring j of row i, `left` of them in the matrix; `bias` along j, where it goes that way.
+__device__ __forceinline__ Vec<float, 4> bias_along(const Epilogue& to, int64_t j, int64_t left) {
+    return to.bias && !to.bias_rows ? load_some_of<4>(to.bias, to.bias_type, j, left) : Vec<float, 4>(0.f);
+}
 template <class T>
-__device__ __forceinline__ void finish(const Epilogue& to, int64_t i, int64_t j, Vec<float, 4> z, int64_t left) {
-    if (to.bias) z += to.bias_rows ? Vec<float, 4>(load_some_of<1>(to.bias, to.bias_type, i, 1)[0]) : load_some_of<4>(to.bias, to.bias_type, j, left);
+__device__ __forceinline__ void finish(const Epilogue& to, int64_t i, int64_t j, Vec<float, 4> z, Vec<float, 4> bias, int64_t left) {
+    if (to.bias) z += to.bias_rows ? Vec<float, 4>(load_some_of<1>(to.bias, to.bias_type, i, 1)[0]) : bias;
     if (to.pre) store_some<T, 4>(static_cast<T*>(to.pre) + i * to.ldp + j, z, left);
-    if (to.activation)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) z[q] = activate(z[q], to.activation);
+    z = activate(z, to.activation);
     if (to.residual) z += load_some<T, 4>(static_cast<const T*>(to.residual) + i * to.ldr + j, left);
     store_some<T, 4>(static_cast<T*>(to.out) + i * to.ldo + j, z, left);
 }
@@ -378,8 +395,12 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
         turn ^= 1;
     }
     __syncthreads();
-    // 32 rows of each wave at a time through LDS, so that neighbouring lanes have neighbouring numbers of a row
+    // 32 rows of each wave at a time through LDS, so that neighbouring lanes have neighbouring numbers of a row.  Nothing is multiplied meanwhile: what the epilogue computes for
+    // a number counts (with two roundings in full and a branch for each number, 4096 tokens, 4096 -> 9216 with gelu_tanh and Z kept took 332 us; now 308).
     float* own = reinterpret_cast<float*>(room) + wave * 32 * kPitch;
+    constexpr int kAbreast = kWideJ / 4;
+    const int64_t j = j0 + wave_j * kWideJ + lane % kAbreast * 4;
+    const Vec<float, 4> bias = cut ? Vec<float, 4>(0.f) : bias_along(p.to, j, p.columns - j);
 #pragma unroll
     for (int x = 0; x < kTilesI; ++x) {
         if (x) __syncthreads();
@@ -390,8 +411,6 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
                 *reinterpret_cast<Vec<float, 4>*>(own + (lane & 31) * kPitch + y * 32 + q * 8 + (lane >> 5) * 4) =
                     Vec<float, 4>{sums[x][y][4 * q], sums[x][y][4 * q + 1], sums[x][y][4 * q + 2], sums[x][y][4 * q + 3]};
         __syncthreads();
-        constexpr int kAbreast = kWideJ / 4;
-        const int64_t j = j0 + wave_j * kWideJ + lane % kAbreast * 4;
 #pragma unroll 1
         for (int row = lane / kAbreast; row < 32; row += 64 / kAbreast) {
             const int64_t i = i0 + wave_i * kWideI + x * 32 + row;
@@ -400,7 +419,7 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
                 store<float, 4>(p.part + ((int64_t)piece * kI + (i - i0)) * kJ + (j - j0), z);
                 continue;
             }
-            if (i < p.rows && j < p.columns) finish<T>(p.to, i, j, z, p.columns - j);
+            if (i < p.rows && j < p.columns) finish<T>(p.to, i, j, z, bias, p.columns - j);
         }
     }
 }
@@ -417,7 +436,7 @@ __global__ __launch_bounds__(256) void parts_kernel(Product p) {
     Vec<float, 4> z = 0.f;
 #pragma unroll 8
     for (uint32_t k = 0; k < p.parts; ++k) z += load<float, 4>(from + (int64_t)k * (kI * kJ));
-    finish<T>(p.to, i, j, z, p.columns - j);
+    finish<T>(p.to, i, j, z, bias_along(p.to, j, p.columns - j), p.columns - j);
 }
 
 // How a product is cut: tiles of a size, the contraction in parts; or its first rows or columns so that their tiles fill the chip some whole times, and the rest by itself.
@@ -639,9 +658,9 @@ __global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
     if constexpr (kColumns) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            if (j + q < a.out) finish<T>(a.to, j + q, t, F4(z[q]), 1);
+            if (j + q < a.out) finish<T>(a.to, j + q, t, F4(z[q]), F4(0.f), 1);
     } else {
-        finish<T>(a.to, t, j, z, a.out - j);
+        finish<T>(a.to, t, j, z, bias_along(a.to, j, a.out - j), a.out - j);
     }
 }
 // Two tiles of 16 tokens only where W is short: there the other kernel's two launches take longer (32 tokens, 640 -> 640 bf16: 6.8 against 11.1 us; 9216 -> 4096 33 against 22).
