@@ -225,3 +225,32 @@ def test_gradients_against_differences():
                 moved[which].view(-1)[at] += sign * step
                 both.append(run(*moved)[-1])
             assert abs((both[0] - both[1]) / (2 * step) - float(got.view(-1)[at])) <= slack
+
+
+@pytest.mark.parametrize("vector", [BF16, F16])
+@pytest.mark.parametrize("n", [70, 9000])
+def test_types_of_weights_and_gate(vector, n):
+    x, f, dy = numbers(61, 5, n, dtype=BF16), numbers(62, 5, n), numbers(63, 5, n)
+    g, a, b = numbers(64, n, dtype=vector), numbers(65, n, dtype=vector), numbers(66, n, dtype=vector)
+    r = torch.ones(5, device="cuda")
+
+    def run(g, a, b):
+        h, y, dx, df = torch.empty_like(x), torch.empty_like(f), torch.empty_like(x), torch.empty_like(f)
+        sums = [torch.empty(n, device="cuda") for _ in range(3)]
+        B.block_norm(x, f, h, y, gate=g, post_weight=a, pre_weight=b)
+        B.block_norm_backward(dy, h, f, r, dx, df, rstd_post=r, gate=g, post_weight=a, pre_weight=b, dgate=sums[0], dpost_weight=sums[1], dpre_weight=sums[2])
+        return [h, y, dx, df] + sums
+    for got, want in zip(run(g, a, b), run(g.float(), a.float(), b.float())):
+        assert torch.equal(got, want)
+
+
+def test_arguments_are_checked():
+    x, f, v, t = numbers(1, 3, 8), numbers(2, 3, 8), numbers(3, 8), numbers(4, 3)
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    for bad in (lambda: B.block_norm(x, f, h, y, gate=numbers(5, 7)), lambda: B.block_norm(x, f, h, y, gate=numbers(5, 2, 8)), lambda: B.block_norm(x, f[:2], h, y),
+                lambda: B.block_norm(x, f, h, y, post_weight=v[:4]), lambda: B.block_norm(x, f, h, y, post=False, post_weight=v), lambda: B.block_norm(x, f, h, y, rstd_pre=v),
+                lambda: B.block_norm(x, f, h, y, gate=numbers(5, 3, 8, dtype=BF16)), lambda: B.block_norm(x, f, f, y),
+                lambda: B.block_norm_backward(f, x, f, t, h, y, gate=v, dgate=numbers(6, 3, 8)), lambda: B.block_norm_backward(f, x, f, t, h, y, gate=v, dgate=v.to(BF16)),
+                lambda: B.block_norm_backward(f, x, f, t, h, y, dpost_weight=v), lambda: B.block_norm_backward(f, x, f, t, x, y)):
+        with pytest.raises((ValueError, B.CerError)):
+            bad()

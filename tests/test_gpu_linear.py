@@ -227,3 +227,39 @@ def test_gradients_against_differences(name):
                 both.append(loss(*moved))
             slack = float(dy.abs().sum()) * (4 * h * h / 6 * max(1.0, float(W.abs().max()), float(x.abs().max())) ** 3 + 4 * 2.0 ** -20 / h)
             assert abs((both[0] - both[1]) / (2 * h) - float(got.view(-1)[at])) <= slack
+
+
+@pytest.mark.parametrize("tokens", [50, 1200])
+@pytest.mark.parametrize("dtype,columns", [(BF16, False), (F32, False), (F32, True)])
+def test_gradients_that_are_not_wanted(tokens, dtype, columns):
+    n, m = 90, 130
+    W, x = numbers(81, m, n, dtype=dtype), numbers(82, tokens, n, dtype=dtype, columns=columns)
+    dy, z = numbers(83, tokens, m, dtype=dtype, columns=columns), numbers(84, tokens, m, dtype=dtype, columns=columns)
+    every = {"dX": torch.empty_like(x), "dW": torch.empty_like(W), "dbias": torch.empty(m, device="cuda")}
+    for name, pre in (("silu", z), ("none", None)):
+        B.linear_backward(W, dy, X=x, activation=name, pre=pre, **every)
+        for k, want in every.items():
+            one = torch.empty_like(want)
+            B.linear_backward(W, dy, X=x if k == "dW" else None, activation=name, pre=pre, **{k: one})
+            assert torch.equal(one, want), (name, k)
+    B.linear_backward(W, dy)  # nothing is wanted
+
+
+@pytest.mark.parametrize("bias_type", [BF16, F16])
+@pytest.mark.parametrize("tokens,columns", [(3, False), (100, False), (3, True), (100, True)])
+def test_types_of_the_bias(tokens, columns, bias_type):
+    W, x, b = numbers(91, 70, 40), numbers(92, tokens, 40, columns=columns), numbers(93, 70, dtype=bias_type)
+    y, want = numbers(94, tokens, 70, columns=columns), numbers(95, tokens, 70, columns=columns)
+    B.linear_matmul(W, x, y, bias=b)
+    B.linear_matmul(W, x, want, bias=b.float())
+    assert torch.equal(y, want)
+
+
+def test_arguments_are_checked():
+    W, x, y = numbers(1, 6, 4), numbers(2, 3, 4), numbers(3, 3, 6)
+    for bad in (lambda: B.linear_matmul(W, x, x), lambda: B.linear_matmul(W, y, y), lambda: B.linear_matmul(W.to(BF16), x, y), lambda: B.linear_matmul(W, x, y, bias=numbers(4, 5)),
+                lambda: B.linear_matmul(W, x, y, activation="tanh"), lambda: B.linear_matmul(W, x, y, activation=1), lambda: B.linear_matmul(W.t(), y, x), lambda: B.linear_matmul(W[0], x, y),
+                lambda: B.linear_matmul(W, x, y, workspace=torch.empty(4, dtype=BF16, device="cuda")), lambda: B.linear_backward(W, y, X=x, dW=numbers(5, 4, 6)),
+                lambda: B.linear_backward(W, y, X=x, dbias=numbers(6, 6, dtype=BF16)), lambda: B.linear_backward(W, y, dW=W.clone()), lambda: B.linear_backward(W, y, activation="relu", dX=x)):
+        with pytest.raises((ValueError, B.CerError)):
+            bad()
