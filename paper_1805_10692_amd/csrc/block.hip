@@ -393,7 +393,6 @@ __global__ __launch_bounds__(kThreads) void block_back_rows_kernel(BlockBackArgs
 template <class TX, class TF, class TD>
 __global__ __launch_bounds__(512) void block_back_means_kernel(BlockBackArgs a) {
     constexpr int V = 16 / sizeof(TX);
-    using F = Vec<float, V>;
     __shared__ float room[2][48];
     unsigned turn = 0;
     for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x, turn ^= 1) {
