@@ -6,16 +6,17 @@
 //     dW (out x in)       A = dz,    B = X         A with i, B with j side by side (k: tokens)
 // and for activations in columns the same with the operands' places and orders exchanged, so that C's rows are always contiguous.
 //
-// A workgroup forms a tile of C.  128 bytes of k (64 numbers of 16 bits, 32 of fp32) of all its rows go from memory through registers into LDS while
-// the tile before is multiplied: by element-aligned loads, so that any leading dimension works, and an operand whose k lies a line apart is turned in
-// registers on the way.  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
+// A workgroup forms a tile of C.  128 bytes of k (64 numbers of 16 bits, 32 of fp32) of all its rows go from memory into LDS while the tiles before
+// are multiplied: straight there where k is side by side on both sides and rows begin on 16 bytes; else through registers, by element-aligned loads, so
+// that any leading dimension works, and an operand whose k lies a line apart is turned on the way.  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
 // stores and the operand loads of 32 rows touch every bank evenly.  The matrix instruction takes B's rows as its first operand: a lane
 // then has four neighbouring j of one i.  fp32 goes through the 32-bit instruction.  Sums are fp32; each C is rounded once, after the epilogue.
 // Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order (`plan_of`).
 //
-// What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 126 us, 1090 TFLOP/s; without its loads 123, without
-// stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's clock falls under them).  A large library product reaches 1123 on this card.
-// fp32: 105 - 111 TFLOP/s of 154.  4096 tokens, 4096 -> 9216 bf16, forward 308 us (2.25 rounds), dX 284, dW 311, dz 56.
+// What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 119 us, 1155 TFLOP/s (a large library product reaches
+// 1123 on this card); through registers 126, of which without loads 123, without stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's
+// clock falls under them).  fp32: 2048 x 4096 -> 4096 476 us, 144 TFLOP/s of 154; through registers 105 - 135.  4096 tokens, 4096 -> 9216 bf16, forward 308 - 317 us (2.25 rounds, and the
+// epilogue of each by itself), dX 284, dW 311, dz 56.
 #include <algorithm>
 #include <type_traits>
 
@@ -310,7 +311,20 @@ __device__ __forceinline__ void tile_of(unsigned at, unsigned tiles_i, unsigned 
 // A barrier for LDS alone: __syncthreads would also wait for the loads from memory that are on their way for the tile after next.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB>
+// 16 bytes a lane from memory, `at` bytes behind `from`, into LDS from `to` on, lane after lane; `from` and `to` are the same for the whole wave.  Nothing waits for
+// it but arrived_barrier.  (As a buffer's load: after the flat form the compiler lets every product wait for all operands that are being read; 512 tokens of 4096 -> 4096 28.1 -> 29.7 us.)
+__device__ __forceinline__ void to_lds_directly(const void* from, uint32_t at, Chunk* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, -1, 0x00020000), (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+}
+// All but the last kLater requests of the wave have arrived, and all waves are here.
+template <int kLater>
+__device__ __forceinline__ void arrived_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
+}
+
+// kStages: 0: two tiles in LDS, and the way there through registers.  Else so many tiles in LDS, all but one of them on their way straight from memory: no registers, no stores
+// to LDS among the reads of it, and more than one tile under way where a compute unit has a single workgroup, which else waits for memory at each step.
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0>
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
@@ -318,7 +332,7 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     constexpr bool kHalves = kTurnA && kTurnB && kI == kJ;
     constexpr bool kFar = kHalves || kI == 256;  // eight rows a thread want it; elsewhere it costs registers (dX of 512 tokens 39 -> 45 us), or none that are missed (4096: 305 -> 290)
     using Way = std::conditional_t<kHalves, Halves<T, kI, kThreads>, Operands<T, kI, kJ, kThreads, kTurnA, kTurnB, kFar>>;
-    __shared__ Chunk room[2][(kI + kJ) * 8];
+    __shared__ Chunk room[kStages ? kStages : 2][(kI + kJ) * 8];
     static_assert(sizeof(room) >= sizeof(float) * kWavesI * kWavesJ * 32 * kPitch, "");
     const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wave_i = wave / kWavesJ, wave_j = wave % kWavesJ;
     const bool cut = p.parts > 1;
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     const int64_t i0 = (int64_t)ti * kI, j0 = (int64_t)tj * kJ, k0 = cut ? piece % p.parts * p.depth_of_part : 0;
     int64_t remain = cut && p.depth - k0 > p.depth_of_part ? p.depth_of_part : p.depth - k0;
     Way way;
-    way.start(p, i0, j0, k0);
+    if (!kStages) way.start(p, i0, j0, k0);
     F16 sums[kTilesI][kTilesJ];
 #pragma unroll
     for (int x = 0; x < kTilesI; ++x)
@@ -353,7 +367,55 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     // memory; past the last one the last is read again, for nobody.  (Two or four tiles on their way gained nothing.)
     unsigned turn = 0;
     const int64_t whole = way.inside(p) && remain > 0 ? remain / kDepth : 0;
-    if (whole) {
+    if constexpr (kStages > 0) {
+        // A wave fills 64 neighbouring slots at a time.  Slot s of a tile has row s / 8 of A, then of B, and of its chunks the one that `place` puts there; the lane asks for that one.
+        constexpr int kOf = (kI + kJ) * 8 / kThreads, kOfA = kI * 8 / kThreads, E = 16 / sizeof(T);
+        const T *from_a = static_cast<const T*>(p.a) + i0 * p.lda + k0, *from_b = static_cast<const T*>(p.b) + j0 * p.ldb + k0;
+        uint32_t at[kOf];
+#pragma unroll
+        for (int n = 0; n < kOf; ++n) {
+            const unsigned slot = threadIdx.x + (n < kOfA ? n : n - kOfA) * kThreads, row = slot / 8, c = place<kFar>(row, slot % 8) % 8;  // the permutation is its own inverse
+            const int64_t most = n < kOfA ? p.rows - i0 : p.columns - j0;
+            at[n] = ((uint32_t)(row < most ? row : most - 1) * (uint32_t)(n < kOfA ? p.lda : p.ldb) + c * E) * sizeof(T);
+        }
+        Chunk* const base = &room[0][0] + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
+        const auto request = [&](unsigned stage, int64_t step) {  // a tile, and `step` on to the next
+#pragma unroll
+            for (int n = 0; n < kOf; ++n) {
+                to_lds_directly(n < kOfA ? from_a : from_b, at[n], base + (stage * (kI + kJ) * 8 + n * kThreads));
+            }
+            from_a += step;
+            from_b += step;
+        };
+        if (whole) {
+            for (unsigned stage = 0; stage + 1 < kStages; ++stage) request(stage, stage + 1 < whole ? kDepth : 0);
+            arrived_barrier<kOf*(kStages - 2)>();
+            operands(room[0], 0, x[0], y[0]);
+            unsigned next = kStages - 1;  // the stage to fill: all waves are past the barrier behind their reads of it
+            for (int64_t k = 0; k < whole; ++k) {
+                const unsigned following = turn + 1 == kStages ? 0 : turn + 1;
+#pragma unroll
+                for (unsigned step = 0; step < 4; ++step) {
+                    if (step < 3) {
+                        operands(room[turn], step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
+                    } else {
+                        arrived_barrier<kOf*(kStages - 2)>();
+                        operands(room[following], 0, x[0], y[0]);
+                    }
+                    if (step == 0) request(next, k + kStages < whole ? kDepth : 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    products(x[step & 1], y[step & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                next = turn;
+                turn = following;
+            }
+            arrived_barrier<0>();
+            turn = 0;
+            remain -= whole * kDepth;
+        }
+        way.start(p, i0, j0, k0 + whole * kDepth);
+    } else if (whole) {
         way.load_whole(p);
         way.to_lds(room[0]);
         if (whole > 1) way.advance(p);
@@ -453,15 +515,15 @@ template <class T>
 Plan plan_of(int64_t rows, int64_t columns, int64_t depth, int turned, bool may_cut) {
     constexpr int64_t kDepth = 128 / sizeof(T);
     // Per k, in nanoseconds: what `at_once` workgroups on a compute unit take at least (a step's way through LDS and its barrier, whatever it multiplies), and what each
-    // adds once they share the matrix cores; by how many operands are turned.  Measured with 512 - 4096 tokens of 4096 -> 4096 and 9216 (16 bits), 999 of 2048 -> 4608 (fp32).
+    // adds once they share the matrix cores; by how many operands are turned.  Measured with 64 - 4096 tokens of 4096 -> 4096 and 9216 (16 bits), 256 - 1024 of 2048 and 4096 (fp32).
     struct Size {
         int side, at_once;
         double alone, each;
     };
-    constexpr Size wide[3][3] = {{{256, 1, 21.0, 30.7}, {128, 2, 10.3, 9.7}, {64, 4, 6.9, 3.4}},
+    constexpr Size wide[3][3] = {{{256, 1, 21.7, 26.4}, {128, 2, 8.0, 7.8}, {64, 3, 2.8, 2.75}},
                                  {{256, 1, 22.0, 31.5}, {128, 2, 10.8, 10.5}, {64, 4, 6.5, 3.9}},
                                  {{256, 1, 24.0, 32.0}, {128, 2, 12.0, 11.0}, {64, 4, 7.0, 5.2}}};
-    constexpr Size exact[3][2] = {{{128, 2, 60.0, 62.0}, {64, 4, 18.0, 17.0}}, {{128, 2, 62.0, 64.0}, {64, 4, 19.0, 18.0}}, {{128, 2, 64.0, 66.0}, {64, 4, 20.0, 19.0}}};
+    constexpr Size exact[3][2] = {{{128, 2, 61.0, 62.0}, {64, 3, 18.0, 15.5}}, {{128, 2, 62.0, 64.0}, {64, 4, 19.0, 18.0}}, {{128, 2, 64.0, 66.0}, {64, 4, 20.0, 19.0}}};
     const int64_t steps = (depth + kDepth - 1) / kDepth;
     const auto rounds = [&](const Size& size, int64_t workgroups, double k) {
         const int64_t most = (workgroups + kComputeUnits - 1) / kComputeUnits;
@@ -475,9 +537,9 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth, int turned, bool may_
     const auto of = [&](const Size& size) {
         const int64_t tiles_i = (rows + size.side - 1) / size.side, tiles_j = (columns + size.side - 1) / size.side, tiles = tiles_i * tiles_j, room = kComputeUnits * size.at_once;
         consider({size.side, 1, 0, false, 6.0 + rounds(size, tiles, (double)depth)});
-        for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * tiles <= room; ++parts)  // written and read again, at 2.5 TB/s in bursts
+        for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * tiles <= room; ++parts)  // written and read again, at 5 TB/s
             consider({size.side, parts, 0, false,
-                      13.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 2.5e6});
+                      9.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 5e6});
         if (!may_cut || tiles <= room || tiles > 16 * room) return;
         for (const bool by_rows : {false, true}) {
             const int64_t across = by_rows ? tiles_j : tiles_i, lines = tiles / room * room / across;  // whole lines of tiles
@@ -533,7 +595,14 @@ int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t
     parts_of<T>(p.depth, parts, &p.depth_of_part, &p.parts);
     const unsigned tiles = p.tiles_i * p.tiles_j;
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    const bool aligned = ((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)(p.lda * sizeof(T)) | (uintptr_t)(p.ldb * sizeof(T))) % 16 == 0;
+    const bool direct = aligned && p.lda < (INT64_C(1) << 21) && p.ldb < (INT64_C(1) << 21);  // a tile's offsets have 32 bits
+    // One more tile under way where a compute unit has one workgroup (256 tokens of 4096 -> 4096 bf16, 64 x 64: 3 tiles in LDS 20.5 us, 4 17.6, 6 17.9; 1024 tokens, 128 x 128:
+    // 2 55, 3 43, 4 43.5); where it has several, their number counts for more (512 tokens: 27.1, 28.3, 33.8; 2048 tokens: 68, 84, 84).
+    constexpr int kStages = kI == 64 ? 3 : 2, kMore = kI == 256 ? kStages : kStages + 1;
+    if (direct && !turn_b && tiles * p.parts > kComputeUnits) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false, kStages><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else if (direct && !turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false, kMore><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    else if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
     else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
     else product_kernel<T, kI, kJ, kWavesI, kWavesJ, true, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
     if (int e = (int)hipGetLastError()) return e;

@@ -245,6 +245,41 @@ def test_gradients_that_are_not_wanted(tokens, dtype, columns):
     B.linear_backward(W, dy)  # nothing is wanted
 
 
+def at_offset(x, offset):
+    room = torch.full((x.numel() + offset,), float("nan"), dtype=x.dtype, device="cuda")
+    to = room[offset:].view(x.shape)
+    to.copy_(x)
+    return to
+
+
+# One step of 128 bytes of the contraction, fewer and more of them than are under way, with and without a rest; one workgroup to a compute unit and several; each tile.
+@pytest.mark.parametrize("tokens,n,m", [(70, 64, 80), (70, 128, 80), (70, 192, 66), (70, 320, 66), (65, 456, 70), (1000, 64, 1030), (1000, 200, 1030), (1030, 512, 4100), (2050, 264, 4100), (4097, 192, 4700)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_where_the_operands_lie_changes_nothing(tokens, n, m, dtype):
+    """Rows on 16 bytes and rows that are not go different ways into LDS: the same sums in the same order."""
+    W, x = numbers(1, m, n, dtype=dtype), numbers(2, tokens, n, dtype=dtype)
+    got = [torch.empty((tokens, m), dtype=dtype, device="cuda") for _ in range(3)]
+    B.linear_matmul(W, x, got[0])
+    B.linear_matmul(at_offset(W, 1), x, got[1])
+    B.linear_matmul(W, at_offset(x, 3), got[2])
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    want = x.double() @ W.double().t().contiguous()
+    near(got[0], want, (n + 8) * 2.0 ** -23 * (x.double().abs() @ W.double().abs().t().contiguous()) + SMALLEST[dtype], HALF[dtype])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("ld", [(1 << 21) - 8, 1 << 21, (1 << 21) + 8])
+def test_rows_far_apart(ld, dtype):
+    tokens, n, m = 200, 264, 136
+    W, x = numbers(1, m, n, dtype=dtype), numbers(2, tokens, n, dtype=dtype)
+    room = torch.empty((tokens, ld), dtype=dtype, device="cuda")
+    room[:, :n].copy_(x)
+    want, got = (torch.empty((tokens, m), dtype=dtype, device="cuda") for _ in range(2))
+    B.linear_matmul(W, x, want)
+    B.linear_matmul(W, room[:, :n], got)
+    assert torch.equal(want, got)
+
+
 @pytest.mark.parametrize("bias_type", [BF16, F16])
 @pytest.mark.parametrize("tokens,columns", [(3, False), (100, False), (3, True), (100, True)])
 def test_types_of_the_bias(tokens, columns, bias_type):
