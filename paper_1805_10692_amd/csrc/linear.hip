@@ -7,16 +7,16 @@
 // and for activations in columns the same with the operands' places and orders exchanged, so that C's rows are always contiguous.
 //
 // A workgroup forms a tile of C.  128 bytes of k (64 numbers of 16 bits, 32 of fp32) of all its rows go from memory into LDS while the tiles before
-// are multiplied: straight there where k is side by side on both sides and rows begin on 16 bytes; else through registers, by element-aligned loads, so
-// that any leading dimension works, and an operand whose k lies a line apart is turned on the way.  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
+// are multiplied: straight there where all of it is whole 16 bytes at addresses of that kind, an operand whose k lies a line apart as it is, to be
+// turned where it is read; else through registers, by element-aligned loads, so that any place and leading dimension works, and turned on the way.  LDS holds rows of 128 bytes whose eight 16-byte chunks are permuted (`place`), so that both the turned
 // stores and the operand loads of 32 rows touch every bank evenly.  The matrix instruction takes B's rows as its first operand: a lane
 // then has four neighbouring j of one i.  fp32 goes through the 32-bit instruction.  Sums are fp32; each C is rounded once, after the epilogue.
 // Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order (`plan_of`).
 //
 // What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 119 us, 1155 TFLOP/s (a large library product reaches
 // 1123 on this card); through registers 126, of which without loads 123, without stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's
-// clock falls under them).  fp32: 2048 x 4096 -> 4096 476 us, 144 TFLOP/s of 154; through registers 105 - 135.  4096 tokens, 4096 -> 9216 bf16, forward 308 - 317 us (2.25 rounds, and the
-// epilogue of each by itself), dX 284, dW 311, dz 56.
+// clock falls under them).  fp32: 2048 x 4096 -> 4096 480 us, 143 TFLOP/s of 154; through registers 105 - 135.  4096 tokens, 4096 -> 9216 bf16, forward 302 us (2.25 rounds, and the
+// epilogue of each by itself), dX 257, dW 273, dz 56.
 #include <algorithm>
 #include <type_traits>
 
@@ -322,6 +322,50 @@ __device__ __forceinline__ void arrived_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
+// An operand's way straight into LDS.  kTurn: a tile is kDepth lines of its kSide numbers, as they lie in memory; sixteen lanes exchange 16-bit numbers as they read them, and
+// fp32 is read number by number.  (Turned in registers, 4096 tokens, 4096 -> 9216 bf16: dX 278 us, dW 310; so 259 and 277.  1024 of 4096 -> 4096 fp32, dW 281 and 257.)
+template <class T, int kSide, int kThreads, bool kTurn, bool kFar>
+struct Direct {
+    static constexpr unsigned E = 16 / sizeof(T), kLines = 128 / sizeof(T), kOf = kSide * 8 / kThreads, kChunks = kTurn ? kSide / E : 8;
+    // Lines: the chunks of a line are permuted so that what a wave reads at once (16 bits: 64 bytes of four lines, fp32: 128 of two) lies in different banks.
+    static __device__ __forceinline__ unsigned turned(unsigned k) { return sizeof(T) == 4 ? (k & 4) << 1 : kSide == 64 ? (k & 2) << 1 : (k & 3) << 2; }
+    const T* from;  // the same for the whole wave
+    int64_t step;
+    uint32_t at[kOf];
+    __device__ __forceinline__ void start(const void* base, int64_t ld, int64_t first, int64_t most, int64_t k0) {
+        most -= first;
+        from = static_cast<const T*>(base) + (kTurn ? k0 * ld + first : first * ld + k0);
+        step = kTurn ? kLines * ld : kLines;
+#pragma unroll
+        for (unsigned n = 0; n < kOf; ++n) {  // a wave fills 64 neighbouring slots at a time; the lane asks for what has its place in its slot (the permutations are their own inverse)
+            const unsigned slot = threadIdx.x + n * kThreads, line = slot / kChunks, c = kTurn ? slot % kChunks ^ turned(line) : place<kFar>(line, slot % 8) % 8;
+            if (kTurn) at[n] = (line * (uint32_t)ld + (uint32_t)(c * E < most ? c * E : most - E)) * sizeof(T);
+            else at[n] = ((uint32_t)(line < most ? line : most - 1) * (uint32_t)ld + c * E) * sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void request(Chunk* to, bool more) {  // a tile, and on to the next
+#pragma unroll
+        for (unsigned n = 0; n < kOf; ++n) to_lds_directly(from, at[n], to + n * kThreads);
+        from += more ? step : 0;
+    }
+    // As multiply takes them: sixteen bytes of k, from `step` * 32 on, of the 32 numbers from `first` on.
+    static __device__ __forceinline__ Chunk across(const Chunk* tile, unsigned first, unsigned step) {
+        const unsigned lane = threadIdx.x & 63;
+        if constexpr (sizeof(T) == 4) {
+            const unsigned k = lane >> 5 << 2, c = first / E + (lane >> 2 & 7);
+            const float* p = reinterpret_cast<const float*>(tile + k * kChunks + (c ^ turned(k))) + (lane & 3) + step * 8 * kSide;
+            return __builtin_bit_cast(Chunk, F4{p[0], p[kSide], p[2 * kSide], p[3 * kSide]});
+        } else {  // sixteen lanes exchange sixteen numbers of four lines
+            typedef short S4 __attribute__((ext_vector_type(4)));
+            const unsigned k = (lane >> 5 << 3) + (lane >> 2 & 3), c = first / E + (lane >> 3 & 2) + (lane >> 1 & 1);
+            const auto* p = (const __attribute__((address_space(3))) S4*)(tile + k * kChunks + (c ^ turned(k))) + (lane & 1) + step * 4 * kSide;
+            auto* q = const_cast<__attribute__((address_space(3))) S4*>(p);
+            const S4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q + kSide);
+            return __builtin_bit_cast(Chunk, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
 // kStages: 0: two tiles in LDS, and the way there through registers.  Else so many tiles in LDS, all but one of them on their way straight from memory: no registers, no stores
 // to LDS among the reads of it, and more than one tile under way where a compute unit has a single workgroup, which else waits for memory at each step.
 template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0>
@@ -351,11 +395,17 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     // chunk 2 . step + (lane >> 5) of row lane & 31 of an even or odd 32 rows: the permutation is an exclusive or
     const unsigned at_lane = place<kFar>(lane & 31, lane >> 5);
     Chunk x[2][kTilesI], y[2][kTilesJ];
-    const auto operands = [&](const Chunk* half, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
+    const auto rows_a = [&](const Chunk* tile, unsigned step, Chunk(&u)[kTilesI]) {
 #pragma unroll
-        for (int k = 0; k < kTilesI; ++k) u[k] = half[(wave_i * kWideI + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_i * kTilesI + k) % 2 * 4 : 0))];
+        for (int k = 0; k < kTilesI; ++k) u[k] = tile[(wave_i * kWideI + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_i * kTilesI + k) % 2 * 4 : 0))];
+    };
+    const auto rows_b = [&](const Chunk* tile, unsigned step, Chunk(&v)[kTilesJ]) {
 #pragma unroll
-        for (int k = 0; k < kTilesJ; ++k) v[k] = half[(kI + wave_j * kWideJ + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_j * kTilesJ + k) % 2 * 4 : 0))];
+        for (int k = 0; k < kTilesJ; ++k) v[k] = tile[(kI + wave_j * kWideJ + k * 32) * 8 + (at_lane ^ 2 * step ^ (kFar ? (wave_j * kTilesJ + k) % 2 * 4 : 0))];
+    };
+    const auto operands = [&](const Chunk* tile, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
+        rows_a(tile, step, u);
+        rows_b(tile, step, v);
     };
     const auto products = [&](const Chunk(&u)[kTilesI], const Chunk(&v)[kTilesJ]) {
 #pragma unroll
@@ -366,45 +416,62 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     // Whole tiles.  While tile k is multiplied out of one half of LDS, tile k + 1 goes from registers into the other half and tile k + 2 is on its way from
     // memory; past the last one the last is read again, for nobody.  (Two or four tiles on their way gained nothing.)
     unsigned turn = 0;
-    const int64_t whole = way.inside(p) && remain > 0 ? remain / kDepth : 0;
+    const int64_t whole = (kStages || way.inside(p)) && remain > 0 ? remain / kDepth : 0;
     if constexpr (kStages > 0) {
-        // A wave fills 64 neighbouring slots at a time.  Slot s of a tile has row s / 8 of A, then of B, and of its chunks the one that `place` puts there; the lane asks for that one.
-        constexpr int kOf = (kI + kJ) * 8 / kThreads, kOfA = kI * 8 / kThreads, E = 16 / sizeof(T);
-        const T *from_a = static_cast<const T*>(p.a) + i0 * p.lda + k0, *from_b = static_cast<const T*>(p.b) + j0 * p.ldb + k0;
-        uint32_t at[kOf];
-#pragma unroll
-        for (int n = 0; n < kOf; ++n) {
-            const unsigned slot = threadIdx.x + (n < kOfA ? n : n - kOfA) * kThreads, row = slot / 8, c = place<kFar>(row, slot % 8) % 8;  // the permutation is its own inverse
-            const int64_t most = n < kOfA ? p.rows - i0 : p.columns - j0;
-            at[n] = ((uint32_t)(row < most ? row : most - 1) * (uint32_t)(n < kOfA ? p.lda : p.ldb) + c * E) * sizeof(T);
-        }
-        Chunk* const base = &room[0][0] + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
-        const auto request = [&](unsigned stage, int64_t step) {  // a tile, and `step` on to the next
-#pragma unroll
-            for (int n = 0; n < kOf; ++n) {
-                to_lds_directly(n < kOfA ? from_a : from_b, at[n], base + (stage * (kI + kJ) * 8 + n * kThreads));
-            }
-            from_a += step;
-            from_b += step;
+        using DirectA = Direct<T, kI, kThreads, kTurnA, kFar>;
+        using DirectB = Direct<T, kJ, kThreads, kTurnB, kFar>;
+        constexpr int kOf = DirectA::kOf + DirectB::kOf;
+        DirectA a;
+        DirectB b;
+        a.start(p.a, p.lda, i0, p.rows, k0);
+        b.start(p.b, p.ldb, j0, p.columns, k0);
+        const unsigned first = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
+        const auto request = [&](Chunk* to, bool more) {
+            a.request(to + first, more);
+            b.request(to + kI * 8 + first, more);
         };
-        if (whole) {
-            for (unsigned stage = 0; stage + 1 < kStages; ++stage) request(stage, stage + 1 < whole ? kDepth : 0);
+        const auto straight = [&](const Chunk* tile, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
+            if constexpr (!kTurnA) rows_a(tile, step, u);
+            if constexpr (!kTurnB) rows_b(tile, step, v);
+            if constexpr (kTurnA)
+#pragma unroll
+                for (int k = 0; k < kTilesI; ++k) u[k] = DirectA::across(tile, wave_i * kWideI + k * 32, step);
+            if constexpr (kTurnB)
+#pragma unroll
+                for (int k = 0; k < kTilesJ; ++k) v[k] = DirectB::across(tile + kI * 8, wave_j * kWideJ + k * 32, step);
+        };
+        if (whole) {  // past the last tile the last is read again, for nobody
+            for (unsigned stage = 0; stage + 1 < kStages; ++stage) request(room[stage], stage + 1 < whole);
             arrived_barrier<kOf*(kStages - 2)>();
-            operands(room[0], 0, x[0], y[0]);
+            straight(room[0], 0, x[0], y[0]);
             unsigned next = kStages - 1;  // the stage to fill: all waves are past the barrier behind their reads of it
-            for (int64_t k = 0; k < whole; ++k) {
-                const unsigned following = turn + 1 == kStages ? 0 : turn + 1;
+            // The tile that is filled is another than those that are read: without that said, the compiler waits for it to arrive before it reads across (dX of 1024 tokens of
+            // 4096 -> 4096 bf16 65 us for 48).  With two stages it is the following one, which is read behind the wait for it.
+            const auto multiplied = [&](Chunk* __restrict fill, const Chunk* __restrict tile, const Chunk* __restrict following, bool more) __attribute__((always_inline)) {
 #pragma unroll
                 for (unsigned step = 0; step < 4; ++step) {
                     if (step < 3) {
-                        operands(room[turn], step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
-                    } else {
+                        straight(tile, step + 1, x[(step + 1) & 1], y[(step + 1) & 1]);
+                    } else if (kStages > 2) {
                         arrived_barrier<kOf*(kStages - 2)>();
-                        operands(room[following], 0, x[0], y[0]);
+                        straight(following, 0, x[0], y[0]);
+                    } else {
+                        break;
                     }
-                    if (step == 0) request(next, k + kStages < whole ? kDepth : 0);
+                    if (step == 0) request(fill, more);
                     __builtin_amdgcn_sched_barrier(0);
                     products(x[step & 1], y[step & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            for (int64_t k = 0; k < whole; ++k) {
+                const unsigned following = turn + 1 == kStages ? 0 : turn + 1;
+                multiplied(room[next], room[turn], kStages > 2 ? room[following] : nullptr, k + kStages < whole);
+                if (kStages == 2) {
+                    arrived_barrier<0>();
+                    straight(room[following], 0, x[0], y[0]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    products(x[1], y[1]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 next = turn;
@@ -512,18 +579,16 @@ struct Plan {
 constexpr int64_t kComputeUnits = 256;
 
 template <class T>
-Plan plan_of(int64_t rows, int64_t columns, int64_t depth, int turned, bool may_cut) {
+Plan plan_of(int64_t rows, int64_t columns, int64_t depth, bool may_cut) {
     constexpr int64_t kDepth = 128 / sizeof(T);
     // Per k, in nanoseconds: what `at_once` workgroups on a compute unit take at least (a step's way through LDS and its barrier, whatever it multiplies), and what each
-    // adds once they share the matrix cores; by how many operands are turned.  Measured with 64 - 4096 tokens of 4096 -> 4096 and 9216 (16 bits), 256 - 1024 of 2048 and 4096 (fp32).
+    // adds once they share the matrix cores.  Measured with operands that go straight into LDS, where turned ones cost the same: 64 - 4096 tokens of 4096 -> 4096 and 9216 (16
+    // bits), 256 - 1024 of 2048 and 4096 (fp32), and their gradients.  Through registers all of it is slower, and turned ones by more.
     struct Size {
         int side, at_once;
         double alone, each;
     };
-    constexpr Size wide[3][3] = {{{256, 1, 21.7, 26.4}, {128, 2, 8.0, 7.8}, {64, 3, 2.8, 2.75}},
-                                 {{256, 1, 22.0, 31.5}, {128, 2, 10.8, 10.5}, {64, 4, 6.5, 3.9}},
-                                 {{256, 1, 24.0, 32.0}, {128, 2, 12.0, 11.0}, {64, 4, 7.0, 5.2}}};
-    constexpr Size exact[3][2] = {{{128, 2, 61.0, 62.0}, {64, 3, 18.0, 15.5}}, {{128, 2, 62.0, 64.0}, {64, 4, 19.0, 18.0}}, {{128, 2, 64.0, 66.0}, {64, 4, 20.0, 19.0}}};
+    constexpr Size wide[3] = {{256, 1, 21.5, 27.0}, {128, 2, 8.3, 7.8}, {64, 3, 2.8, 2.9}}, exact[2] = {{128, 2, 61.0, 62.0}, {64, 3, 18.0, 15.6}};
     const int64_t steps = (depth + kDepth - 1) / kDepth;
     const auto rounds = [&](const Size& size, int64_t workgroups, double k) {
         const int64_t most = (workgroups + kComputeUnits - 1) / kComputeUnits;
@@ -539,20 +604,20 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth, int turned, bool may_
         consider({size.side, 1, 0, false, 6.0 + rounds(size, tiles, (double)depth)});
         for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * tiles <= room; ++parts)  // written and read again, at 5 TB/s
             consider({size.side, parts, 0, false,
-                      9.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 5e6});
+                      8.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 5e6});
         if (!may_cut || tiles <= room || tiles > 16 * room) return;
         for (const bool by_rows : {false, true}) {
             const int64_t across = by_rows ? tiles_j : tiles_i, lines = tiles / room * room / across;  // whole lines of tiles
             if (lines < 1 || lines >= (by_rows ? tiles_i : tiles_j)) continue;
             const int64_t first = lines * size.side;
-            const Plan rest = plan_of<T>(by_rows ? rows - first : rows, by_rows ? columns : columns - first, depth, turned, false);
+            const Plan rest = plan_of<T>(by_rows ? rows - first : rows, by_rows ? columns : columns - first, depth, false);
             consider({size.side, 1, first, by_rows, 6.0 + rounds(size, lines * across, (double)depth) + rest.time});
         }
     };
     if constexpr (sizeof(T) == 2) {
-        for (const Size& size : wide[turned]) of(size);
+        for (const Size& size : wide) of(size);
     } else {
-        for (const Size& size : exact[turned]) of(size);
+        for (const Size& size : exact) of(size);
     }
     return best;
 }
@@ -578,12 +643,12 @@ struct Course {
     size_t bytes = 0;
 };
 template <class T>
-Course course_of(int64_t rows, int64_t columns, int64_t depth, int turned) {
+Course course_of(int64_t rows, int64_t columns, int64_t depth) {
     Course c;
-    c.head = plan_of<T>(rows, columns, depth, turned, true);
+    c.head = plan_of<T>(rows, columns, depth, true);
     if (c.head.first) {
         (c.head.rows ? rows : columns) -= c.head.first;
-        c.rest = plan_of<T>(rows, columns, depth, turned, false);
+        c.rest = plan_of<T>(rows, columns, depth, false);
     }
     c.bytes = parts_bytes<T>(c.head.first ? c.rest : c.head, rows, columns, depth);
     return c;
@@ -595,16 +660,22 @@ int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t
     parts_of<T>(p.depth, parts, &p.depth_of_part, &p.parts);
     const unsigned tiles = p.tiles_i * p.tiles_j;
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    const bool aligned = ((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)(p.lda * sizeof(T)) | (uintptr_t)(p.ldb * sizeof(T))) % 16 == 0;
-    const bool direct = aligned && p.lda < (INT64_C(1) << 21) && p.ldb < (INT64_C(1) << 21);  // a tile's offsets have 32 bits
+    // Straight into LDS go whole 16 bytes, and a tile's offsets have 32 bits.
+    constexpr int64_t E = 16 / sizeof(T);
+    const auto fits = [](const void* base, int64_t ld, int64_t across, bool turn) { return (uintptr_t)base % 16 == 0 && ld % E == 0 && ld < (INT64_C(1) << 21) && (!turn || across % E == 0); };
+    const bool direct = fits(p.a, p.lda, p.rows, turn_a) && fits(p.b, p.ldb, p.columns, turn_b);
     // One more tile under way where a compute unit has one workgroup (256 tokens of 4096 -> 4096 bf16, 64 x 64: 3 tiles in LDS 20.5 us, 4 17.6, 6 17.9; 1024 tokens, 128 x 128:
     // 2 55, 3 43, 4 43.5); where it has several, their number counts for more (512 tokens: 27.1, 28.3, 33.8; 2048 tokens: 68, 84, 84).
     constexpr int kStages = kI == 64 ? 3 : 2, kMore = kI == 256 ? kStages : kStages + 1;
-    if (direct && !turn_b && tiles * p.parts > kComputeUnits) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false, kStages><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else if (direct && !turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false, kMore><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else if (!turn_b) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, false><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else if (!turn_a) product_kernel<T, kI, kJ, kWavesI, kWavesJ, false, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
-    else product_kernel<T, kI, kJ, kWavesI, kWavesJ, true, true><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    const auto launch = [&](auto turned_a, auto turned_b) {
+        constexpr bool a = decltype(turned_a)::value, b = decltype(turned_b)::value;
+        if (!direct) product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b><<<tiles * p.parts, kThreads, 0, s>>>(p);
+        else if (tiles * p.parts > kComputeUnits) product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, kStages><<<tiles * p.parts, kThreads, 0, s>>>(p);
+        else product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, kMore><<<tiles * p.parts, kThreads, 0, s>>>(p);
+    };
+    if (!turn_b) launch(std::false_type(), std::false_type());
+    else if (!turn_a) launch(std::false_type(), std::true_type());
+    else launch(std::true_type(), std::true_type());
     if (int e = (int)hipGetLastError()) return e;
     if (p.parts > 1) parts_kernel<T, kI, kJ><<<dim3(kI * kJ / 1024, tiles), 256, 0, s>>>(p);
     return (int)hipGetLastError();
@@ -836,7 +907,7 @@ __global__ __launch_bounds__(1024) void bias_totals_kernel(const float* part, ui
 template <class T>
 Course linear_course(const LinearCall& c) {
     const bool columns = c.x.order == CER_ORDER_COLUMNS;
-    return course_of<T>(columns ? c.out : c.tokens, columns ? c.tokens : c.out, c.in, columns);
+    return course_of<T>(columns ? c.out : c.tokens, columns ? c.tokens : c.out, c.in);
 }
 template <class T>
 int64_t linear_bytes(const LinearCall& c) {
@@ -879,8 +950,8 @@ struct BackwardShape {
         tokens_of_part = std::max<int64_t>(1, (c.tokens + most - 1) / most), parts = (c.tokens + tokens_of_part - 1) / tokens_of_part;
         dz = act && (c.dx.data || c.dw) ? (size_t)c.tokens * c.out * sizeof(T) : 0;
         sums = c.dbias && parts > 1 && !columns ? (size_t)parts * c.out * 4 : 0;
-        if (c.dx.data && c.tokens) to_x = course_of<T>(columns ? c.in : c.tokens, columns ? c.tokens : c.in, c.out, columns ? 2 : 1);
-        if (c.dw) to_w = course_of<T>(c.out, c.in, c.tokens, columns ? 0 : 2);
+        if (c.dx.data && c.tokens) to_x = course_of<T>(columns ? c.in : c.tokens, columns ? c.tokens : c.in, c.out);
+        if (c.dw) to_w = course_of<T>(c.out, c.in, c.tokens);
         product = std::max(to_x.bytes, to_w.bytes);
     }
     int64_t bytes() const { return (int64_t)(Room::rounded(dz) + Room::rounded(sums) + Room::rounded(product)); }

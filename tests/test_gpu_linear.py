@@ -267,16 +267,46 @@ def test_where_the_operands_lie_changes_nothing(tokens, n, m, dtype):
     near(got[0], want, (n + 8) * 2.0 ** -23 * (x.double().abs() @ W.double().abs().t().contiguous()) + SMALLEST[dtype], HALF[dtype])
 
 
+@pytest.mark.parametrize("tokens,n,m", [(64, 72, 64), (128, 80, 128), (192, 72, 192), (328, 64, 456), (72, 1032, 1000), (520, 2056, 264), (200, 4104, 1032), (4168, 264, 1032), (264, 4616, 4104)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("columns", [False, True])
+def test_where_the_operands_of_gradients_lie_changes_nothing(tokens, n, m, dtype, columns):
+    """An operand that is turned where it is read, and one that is turned on its way."""
+    if columns and dtype != F32:
+        dtype = F32
+        tokens, n, m = n, tokens, m  # another order of the sizes instead of a type that has no columns
+    W, x, dy = numbers(1, m, n, dtype=dtype), numbers(2, *((n, tokens) if columns else (tokens, n)), dtype=dtype), numbers(3, *((m, tokens) if columns else (tokens, m)), dtype=dtype)
+    turned = (lambda t: t.t()) if columns else (lambda t: t)
+
+    def gradients(W, x, dy):
+        dx, dw = torch.empty_like(x), torch.empty_like(W)
+        B.linear_backward(W, turned(dy), X=turned(x), dX=turned(dx), dW=dw)
+        return turned(dx), dw
+
+    want = gradients(W, x, dy)
+    for other in ((at_offset(W, 1), x, dy), (W, at_offset(x, 3), dy), (W, x, at_offset(dy, 1))):
+        for a, b in zip(want, gradients(*other)):
+            assert torch.equal(a, b)
+    W, x, dy = W.double(), turned(x).double().contiguous(), turned(dy).double().contiguous()
+    near(want[0], dy @ W, (m + 8) * 2.0 ** -23 * (dy.abs() @ W.abs()) + SMALLEST[dtype], HALF[dtype])
+    d = dy.t().contiguous()
+    near(want[1], d @ x, (tokens + 8) * 2.0 ** -23 * (d.abs() @ x.abs()) + SMALLEST[dtype], HALF[dtype])
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("ld", [(1 << 21) - 8, 1 << 21, (1 << 21) + 8])
 def test_rows_far_apart(ld, dtype):
     tokens, n, m = 200, 264, 136
-    W, x = numbers(1, m, n, dtype=dtype), numbers(2, tokens, n, dtype=dtype)
+    W, x, dy = numbers(1, m, n, dtype=dtype), numbers(2, tokens, n, dtype=dtype), numbers(3, tokens, m, dtype=dtype)
     room = torch.empty((tokens, ld), dtype=dtype, device="cuda")
-    room[:, :n].copy_(x)
+    far = room[:, :n].copy_(x)
     want, got = (torch.empty((tokens, m), dtype=dtype, device="cuda") for _ in range(2))
     B.linear_matmul(W, x, want)
-    B.linear_matmul(W, room[:, :n], got)
+    B.linear_matmul(W, far, got)
+    assert torch.equal(want, got)
+    want, got = torch.empty_like(W), torch.empty_like(W)
+    B.linear_backward(W, dy, X=x, dW=want)
+    B.linear_backward(W, dy, X=far, dW=got)
     assert torch.equal(want, got)
 
 
