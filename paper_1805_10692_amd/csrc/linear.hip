@@ -311,10 +311,13 @@ __device__ __forceinline__ void tile_of(unsigned at, unsigned tiles_i, unsigned 
 // A barrier for LDS alone: __syncthreads would also wait for the loads from memory that are on their way for the tile after next.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// 16 bytes a lane from memory, `at` bytes behind `from`, into LDS from `to` on, lane after lane; `from` and `to` are the same for the whole wave.  Nothing waits for
+// 16 or 4 bytes a lane from memory, `at` bytes behind `from`, into LDS from `to` on, lane after lane; `from` and `to` are the same for the whole wave.  Nothing waits for
 // it but arrived_barrier.  (As a buffer's load: after the flat form the compiler lets every product wait for all operands that are being read; 512 tokens of 4096 -> 4096 28.1 -> 29.7 us.)
-__device__ __forceinline__ void to_lds_directly(const void* from, uint32_t at, Chunk* to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, -1, 0x00020000), (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+template <int kGrain>
+__device__ __forceinline__ void to_lds_directly(const void* from, uint32_t at, uint32_t* to) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, -1, 0x00020000);
+    if constexpr (kGrain == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 4, at, 0, 0, 0);
 }
 // All but the last kLater requests of the wave have arrived, and all waves are here.
 template <int kLater>
@@ -324,9 +327,9 @@ __device__ __forceinline__ void arrived_barrier() {
 
 // An operand's way straight into LDS.  kTurn: a tile is kDepth lines of its kSide numbers, as they lie in memory; sixteen lanes exchange 16-bit numbers as they read them, and
 // fp32 is read number by number.  (Turned in registers, 4096 tokens, 4096 -> 9216 bf16: dX 278 us, dW 310; so 259 and 277.  1024 of 4096 -> 4096 fp32, dW 281 and 257.)
-template <class T, int kSide, int kThreads, bool kTurn, bool kFar>
+template <class T, int kSide, int kThreads, bool kTurn, bool kFar, int kGrain>
 struct Direct {
-    static constexpr unsigned E = 16 / sizeof(T), kLines = 128 / sizeof(T), kOf = kSide * 8 / kThreads, kChunks = kTurn ? kSide / E : 8;
+    static constexpr unsigned E = 16 / sizeof(T), kLines = 128 / sizeof(T), kOf = kSide * 128 / kGrain / kThreads, kGrains = 16 / kGrain, kItems = kGrain / sizeof(T), kChunks = kTurn ? kSide / E : 8;
     // Lines: the chunks of a line are permuted so that what a wave reads at once (16 bits: 64 bytes of four lines, fp32: 128 of two) lies in different banks.
     static __device__ __forceinline__ unsigned turned(unsigned k) { return sizeof(T) == 4 ? (k & 4) << 1 : kSide == 64 ? (k & 2) << 1 : (k & 3) << 2; }
     const T* from;  // the same for the whole wave
@@ -338,14 +341,15 @@ struct Direct {
         step = kTurn ? kLines * ld : kLines;
 #pragma unroll
         for (unsigned n = 0; n < kOf; ++n) {  // a wave fills 64 neighbouring slots at a time; the lane asks for what has its place in its slot (the permutations are their own inverse)
-            const unsigned slot = threadIdx.x + n * kThreads, line = slot / kChunks, c = kTurn ? slot % kChunks ^ turned(line) : place<kFar>(line, slot % 8) % 8;
-            if (kTurn) at[n] = (line * (uint32_t)ld + (uint32_t)(c * E < most ? c * E : most - E)) * sizeof(T);
-            else at[n] = ((uint32_t)(line < most ? line : most - 1) * (uint32_t)ld + c * E) * sizeof(T);
+            const unsigned grain = threadIdx.x + n * kThreads, slot = grain / kGrains, line = slot / kChunks, c = kTurn ? slot % kChunks ^ turned(line) : place<kFar>(line, slot % 8) % 8;
+            const unsigned item = c * E + grain % kGrains * kItems;
+            if (kTurn) at[n] = (line * (uint32_t)ld + (uint32_t)(item < most ? item : most - kItems)) * sizeof(T);
+            else at[n] = ((uint32_t)(line < most ? line : most - 1) * (uint32_t)ld + item) * sizeof(T);
         }
     }
     __device__ __forceinline__ void request(Chunk* to, bool more) {  // a tile, and on to the next
 #pragma unroll
-        for (unsigned n = 0; n < kOf; ++n) to_lds_directly(from, at[n], to + n * kThreads);
+        for (unsigned n = 0; n < kOf; ++n) to_lds_directly<kGrain>(from, at[n], reinterpret_cast<uint32_t*>(to) + n * kThreads * (kGrain / 4));
         from += more ? step : 0;
     }
     // As multiply takes them: sixteen bytes of k, from `step` * 32 on, of the 32 numbers from `first` on.
@@ -368,7 +372,7 @@ struct Direct {
 
 // kStages: 0: two tiles in LDS, and the way there through registers.  Else so many tiles in LDS, all but one of them on their way straight from memory: no registers, no stores
 // to LDS among the reads of it, and more than one tile under way where a compute unit has a single workgroup, which else waits for memory at each step.
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0>
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0, int kGrain = 16>
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
@@ -418,14 +422,14 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     unsigned turn = 0;
     const int64_t whole = (kStages || way.inside(p)) && remain > 0 ? remain / kDepth : 0;
     if constexpr (kStages > 0) {
-        using DirectA = Direct<T, kI, kThreads, kTurnA, kFar>;
-        using DirectB = Direct<T, kJ, kThreads, kTurnB, kFar>;
+        using DirectA = Direct<T, kI, kThreads, kTurnA, kFar, kGrain>;
+        using DirectB = Direct<T, kJ, kThreads, kTurnB, kFar, kGrain>;
         constexpr int kOf = DirectA::kOf + DirectB::kOf;
         DirectA a;
         DirectB b;
         a.start(p.a, p.lda, i0, p.rows, k0);
         b.start(p.b, p.ldb, j0, p.columns, k0);
-        const unsigned first = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
+        const unsigned first = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * (4 * kGrain);  // chunks
         const auto request = [&](Chunk* to, bool more) {
             a.request(to + first, more);
             b.request(to + kI * 8 + first, more);
@@ -660,18 +664,28 @@ int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t
     parts_of<T>(p.depth, parts, &p.depth_of_part, &p.parts);
     const unsigned tiles = p.tiles_i * p.tiles_j;
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
-    // Straight into LDS go whole 16 bytes, and a tile's offsets have 32 bits.
-    constexpr int64_t E = 16 / sizeof(T);
-    const auto fits = [](const void* base, int64_t ld, int64_t across, bool turn) { return (uintptr_t)base % 16 == 0 && ld % E == 0 && ld < (INT64_C(1) << 21) && (!turn || across % E == 0); };
-    const bool direct = fits(p.a, p.lda, p.rows, turn_a) && fits(p.b, p.ldb, p.columns, turn_b);
+    // Straight into LDS go whole grains of 16 bytes, and a tile's offsets have 32 bits.  Numbers of fp32 go there by themselves where an operand is turned (1000 tokens, 2050 -> 2050: dX
+    // 120 -> 108 us, dW 100 -> 92); where none is, registers do as well (Y 117 -> 118, 657 tokens, 3563 -> 1475 108 -> 95), and pairs of 16 bits are slower (1000 tokens, Y 31, dX 36 -> 65, 67).
+    const auto fits = [](const void* base, int64_t ld, int64_t across, bool turn, int64_t grain) {
+        return (uintptr_t)base % grain == 0 && ld * sizeof(T) % grain == 0 && ld < (INT64_C(1) << 21) && (!turn || across * sizeof(T) % grain == 0);
+    };
+    const bool direct = fits(p.a, p.lda, p.rows, turn_a, 16) && fits(p.b, p.ldb, p.columns, turn_b, 16), by_numbers = fits(p.a, p.lda, p.rows, turn_a, 4) && fits(p.b, p.ldb, p.columns, turn_b, 4);
     // One more tile under way where a compute unit has one workgroup (256 tokens of 4096 -> 4096 bf16, 64 x 64: 3 tiles in LDS 20.5 us, 4 17.6, 6 17.9; 1024 tokens, 128 x 128:
     // 2 55, 3 43, 4 43.5); where it has several, their number counts for more (512 tokens: 27.1, 28.3, 33.8; 2048 tokens: 68, 84, 84).
     constexpr int kStages = kI == 64 ? 3 : 2, kMore = kI == 256 ? kStages : kStages + 1;
     const auto launch = [&](auto turned_a, auto turned_b) {
         constexpr bool a = decltype(turned_a)::value, b = decltype(turned_b)::value;
-        if (!direct) product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b><<<tiles * p.parts, kThreads, 0, s>>>(p);
-        else if (tiles * p.parts > kComputeUnits) product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, kStages><<<tiles * p.parts, kThreads, 0, s>>>(p);
-        else product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, kMore><<<tiles * p.parts, kThreads, 0, s>>>(p);
+        const bool several = tiles * p.parts > kComputeUnits;
+        const auto go = [&](auto stages, auto grain) { product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, decltype(stages)::value, decltype(grain)::value><<<tiles * p.parts, kThreads, 0, s>>>(p); };
+        using Few = std::integral_constant<int, kStages>;
+        using More = std::integral_constant<int, kMore>;
+        using Chunks = std::integral_constant<int, 16>;
+        if (direct) return several ? go(Few(), Chunks()) : go(More(), Chunks());
+        if constexpr (sizeof(T) == 4 && b) {
+            using Numbers = std::integral_constant<int, 4>;
+            if (by_numbers) return several ? go(Few(), Numbers()) : go(More(), Numbers());
+        }
+        go(std::integral_constant<int, 0>(), Chunks());
     };
     if (!turn_b) launch(std::false_type(), std::false_type());
     else if (!turn_a) launch(std::false_type(), std::true_type());
