@@ -372,7 +372,7 @@ struct Direct {
 
 // kStages: 0: two tiles in LDS, and the way there through registers.  Else so many tiles in LDS, all but one of them on their way straight from memory: no registers, no stores
 // to LDS among the reads of it, and more than one tile under way where a compute unit has a single workgroup, which else waits for memory at each step.
-template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0, int kGrain = 16>
+template <class T, int kI, int kJ, int kWavesI, int kWavesJ, bool kTurnA, bool kTurnB, int kStages = 0, int kGrainA = 16, int kGrainB = 16>
 __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product p) {
     constexpr int kThreads = 64 * kWavesI * kWavesJ, kWideI = kI / kWavesI, kWideJ = kJ / kWavesJ, kTilesI = kWideI / 32, kTilesJ = kWideJ / 32;
     constexpr int kPitch = kWideJ + 4;
@@ -422,17 +422,17 @@ __global__ __launch_bounds__(64 * kWavesI * kWavesJ) void product_kernel(Product
     unsigned turn = 0;
     const int64_t whole = (kStages || way.inside(p)) && remain > 0 ? remain / kDepth : 0;
     if constexpr (kStages > 0) {
-        using DirectA = Direct<T, kI, kThreads, kTurnA, kFar, kGrain>;
-        using DirectB = Direct<T, kJ, kThreads, kTurnB, kFar, kGrain>;
+        using DirectA = Direct<T, kI, kThreads, kTurnA, kFar, kGrainA>;
+        using DirectB = Direct<T, kJ, kThreads, kTurnB, kFar, kGrainB>;
         constexpr int kOf = DirectA::kOf + DirectB::kOf;
         DirectA a;
         DirectB b;
         a.start(p.a, p.lda, i0, p.rows, k0);
         b.start(p.b, p.ldb, j0, p.columns, k0);
-        const unsigned first = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * (4 * kGrain);  // chunks
+        const unsigned first = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 4;  // a wave's first chunk, for each byte of its grains
         const auto request = [&](Chunk* to, bool more) {
-            a.request(to + first, more);
-            b.request(to + kI * 8 + first, more);
+            a.request(to + first * kGrainA, more);
+            b.request(to + kI * 8 + first * kGrainB, more);
         };
         const auto straight = [&](const Chunk* tile, unsigned step, Chunk(&u)[kTilesI], Chunk(&v)[kTilesJ]) {
             if constexpr (!kTurnA) rows_a(tile, step, u);
@@ -587,7 +587,7 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth, bool may_cut) {
     constexpr int64_t kDepth = 128 / sizeof(T);
     // Per k, in nanoseconds: what `at_once` workgroups on a compute unit take at least (a step's way through LDS and its barrier, whatever it multiplies), and what each
     // adds once they share the matrix cores.  Measured with operands that go straight into LDS, where turned ones cost the same: 64 - 4096 tokens of 4096 -> 4096 and 9216 (16
-    // bits), 256 - 1024 of 2048 and 4096 (fp32), and their gradients.  Through registers all of it is slower, and turned ones by more.
+    // bits), 256 - 1024 of 2048 and 4096 (fp32), and their gradients.  Through registers all of it is slower, and turned ones by more; fp32 by numbers up to 81.
     struct Size {
         int side, at_once;
         double alone, each;
@@ -609,13 +609,16 @@ Plan plan_of(int64_t rows, int64_t columns, int64_t depth, bool may_cut) {
         for (int64_t parts = 2; parts <= 16 && parts * 4 <= steps && parts * tiles <= room; ++parts)  // written and read again, at 5 TB/s
             consider({size.side, parts, 0, false,
                       8.0 + rounds(size, tiles * parts, (double)((steps + parts - 1) / parts * kDepth)) + (double)(tiles * parts) * size.side * size.side * 8 / 5e6});
-        if (!may_cut || tiles <= room || tiles > 16 * room) return;
+        // Whole rounds by themselves and what is left with a plan of its own: a round is all that run at once, or (fp32, where each takes the matrix cores for as long as if it were
+        // alone) one workgroup on each compute unit: 1000 tokens, 2050 -> 2050 118 -> 100 us, dX 109 -> 95; of 16 bits 2100 tokens, 2048 -> 2048, dX 35 -> 40.
+        const int64_t round = sizeof(T) == 4 ? kComputeUnits : room;
+        if (!may_cut || tiles <= round || tiles > 16 * room) return;
         for (const bool by_rows : {false, true}) {
-            const int64_t across = by_rows ? tiles_j : tiles_i, lines = tiles / room * room / across;  // whole lines of tiles
+            const int64_t across = by_rows ? tiles_j : tiles_i, lines = tiles / round * round / across;  // whole lines of tiles
             if (lines < 1 || lines >= (by_rows ? tiles_i : tiles_j)) continue;
             const int64_t first = lines * size.side;
             const Plan rest = plan_of<T>(by_rows ? rows - first : rows, by_rows ? columns : columns - first, depth, false);
-            consider({size.side, 1, first, by_rows, 6.0 + rounds(size, lines * across, (double)depth) + rest.time});
+            consider({size.side, 1, first, by_rows, 10.0 + rounds(size, lines * across, (double)depth) + rest.time});
         }
     };
     if constexpr (sizeof(T) == 2) {
@@ -666,26 +669,31 @@ int launch_tiles(Product p, int64_t parts, bool turn_a, bool turn_b, hipStream_t
     constexpr int kThreads = 64 * kWavesI * kWavesJ;
     // Straight into LDS go whole grains of 16 bytes, and a tile's offsets have 32 bits.  Numbers of fp32 go there by themselves where an operand is turned (1000 tokens, 2050 -> 2050: dX
     // 120 -> 108 us, dW 100 -> 92); where none is, registers do as well (Y 117 -> 118, 657 tokens, 3563 -> 1475 108 -> 95), and pairs of 16 bits are slower (1000 tokens, Y 31, dX 36 -> 65, 67).
+    // Rows of numbers in tiles of 128 are slower, too (a tile of 999 tokens in columns, 2048 -> 4608, W by numbers 226 us, by 16 bytes and X by numbers 167).
     const auto fits = [](const void* base, int64_t ld, int64_t across, bool turn, int64_t grain) {
         return (uintptr_t)base % grain == 0 && ld * sizeof(T) % grain == 0 && ld < (INT64_C(1) << 21) && (!turn || across * sizeof(T) % grain == 0);
     };
-    const bool direct = fits(p.a, p.lda, p.rows, turn_a, 16) && fits(p.b, p.ldb, p.columns, turn_b, 16), by_numbers = fits(p.a, p.lda, p.rows, turn_a, 4) && fits(p.b, p.ldb, p.columns, turn_b, 4);
+    const bool chunks_a = fits(p.a, p.lda, p.rows, turn_a, 16), direct = chunks_a && fits(p.b, p.ldb, p.columns, turn_b, 16);
+    const bool by_numbers = fits(p.a, p.lda, p.rows, turn_a, 4) && fits(p.b, p.ldb, p.columns, turn_b, 4);
     // One more tile under way where a compute unit has one workgroup (256 tokens of 4096 -> 4096 bf16, 64 x 64: 3 tiles in LDS 20.5 us, 4 17.6, 6 17.9; 1024 tokens, 128 x 128:
     // 2 55, 3 43, 4 43.5); where it has several, their number counts for more (512 tokens: 27.1, 28.3, 33.8; 2048 tokens: 68, 84, 84).
     constexpr int kStages = kI == 64 ? 3 : 2, kMore = kI == 256 ? kStages : kStages + 1;
     const auto launch = [&](auto turned_a, auto turned_b) {
         constexpr bool a = decltype(turned_a)::value, b = decltype(turned_b)::value;
         const bool several = tiles * p.parts > kComputeUnits;
-        const auto go = [&](auto stages, auto grain) { product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, decltype(stages)::value, decltype(grain)::value><<<tiles * p.parts, kThreads, 0, s>>>(p); };
+        const auto go = [&](auto stages, auto grain_a, auto grain_b) {
+            product_kernel<T, kI, kJ, kWavesI, kWavesJ, a, b, decltype(stages)::value, decltype(grain_a)::value, decltype(grain_b)::value><<<tiles * p.parts, kThreads, 0, s>>>(p);
+        };
         using Few = std::integral_constant<int, kStages>;
         using More = std::integral_constant<int, kMore>;
         using Chunks = std::integral_constant<int, 16>;
-        if (direct) return several ? go(Few(), Chunks()) : go(More(), Chunks());
-        if constexpr (sizeof(T) == 4 && b) {
-            using Numbers = std::integral_constant<int, 4>;
-            if (by_numbers) return several ? go(Few(), Numbers()) : go(More(), Numbers());
-        }
-        go(std::integral_constant<int, 0>(), Chunks());
+        using Numbers = std::integral_constant<int, 4>;
+        if (direct) return several ? go(Few(), Chunks(), Chunks()) : go(More(), Chunks(), Chunks());
+        if constexpr (sizeof(T) == 4 && b && !a)
+            if (by_numbers && chunks_a) return several ? go(Few(), Chunks(), Numbers()) : go(More(), Chunks(), Numbers());
+        if constexpr (sizeof(T) == 4 && b && (a || kI == 64))
+            if (by_numbers) return several ? go(Few(), Numbers(), Numbers()) : go(More(), Numbers(), Numbers());
+        go(std::integral_constant<int, 0>(), Chunks(), Chunks());
     };
     if (!turn_b) launch(std::false_type(), std::false_type());
     else if (!turn_a) launch(std::false_type(), std::true_type());
