@@ -308,6 +308,11 @@ def test_rows_far_apart(ld, dtype):
     B.linear_backward(W, dy, X=x, dW=want)
     B.linear_backward(W, dy, X=far, dW=got)
     assert torch.equal(want, got)
+    far = room[:m, 8:n + 8].copy_(W)
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    B.linear_backward(W, dy, dX=want)
+    B.linear_backward(far, dy, dX=got)
+    assert torch.equal(want, got)
 
 
 @pytest.mark.parametrize("bias_type", [BF16, F16])
