@@ -593,8 +593,9 @@ int grad_clip(const cer_gradient_t* grads, int64_t count, float max_norm, float*
  * (linear: 2^24), features over 2^22 (block_norm: 32768), tokens . features or in . out over 2^40.
  *
  * workspace: device memory for a call's temporaries, 16-byte aligned, of linear_workspace_bytes() or block_workspace_bytes() bytes (which suffice for every call of
- * those sizes, type and order; block: with columns != 0 for F, Y or dY in columns), or NULL: a stream-ordered temporary.  With it a call only launches kernels; calls that
- * may run at once need one each.  A call that is recorded into a HIP graph has to bring it where it needs any (else CER_E_HIP).
+ * those sizes, type and order; block: with columns != 0 for F, Y or dY in columns), or NULL: a temporary of the call's own, on the null stream alone.  On any other stream,
+ * recorded into a HIP graph or not, a call has to bring it where it needs any (else CER_E_HIP, hipErrorNotSupported, and nothing is done).  With it a call only launches
+ * kernels; calls that may run at once need one each.
  */
 int64_t linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t type, int32_t order, int32_t backward);
 int64_t block_workspace_bytes(int64_t tokens, int64_t n, int32_t type, int32_t columns, int32_t backward);

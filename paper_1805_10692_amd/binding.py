@@ -250,7 +250,7 @@ else:
 #   grad_norm(grads, norm, stream=None)
 #   grad_clip(grads, max_norm, norm, outs=None, stream=None)
 # and those of a block around projections (activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'; gate: (n,) or (tokens, n); key: int64, (2,); workspace: float32,
-# linear_workspace_bytes() or block_workspace_bytes() / 4 numbers, needed while recorded into a graph):
+# linear_workspace_bytes() or block_workspace_bytes() / 4 numbers, needed, where that is not 0, on every stream but the null one, recorded or not):
 #   linear_matmul(W, X, Y, bias=None, residual=None, activation='none', pre=None, workspace=None, stream=None)
 #   linear_backward(W, dY, X=None, activation='none', pre=None, base=None, dX=None, dW=None, dbias=None, workspace=None, stream=None)
 #   block_norm(X, F, H, Y, gate=None, post_weight=None, pre_weight=None, scale=1.0, eps=1e-6, post=True, rstd_post=None, rstd_pre=None, workspace=None,
@@ -514,7 +514,7 @@ def _type_code(dtype) -> int:
 
 
 def linear_workspace_bytes(tokens: int, features_in: int, features_out: int, dtype, columns: bool = False, backward: bool = False) -> int:
-    """Size of the workspace with which linear_matmul (backward: linear_backward) allocates nothing."""
+    """Size of the workspace with which linear_matmul (backward: linear_backward) allocates nothing.  On streams other than the null one it is needed where this is not 0."""
     v = lib().linear_workspace_bytes(tokens, features_in, features_out, _type_code(dtype), int(columns), int(backward))
     if v < 0:
         raise CerError(int(v), "linear_workspace_bytes")
@@ -522,7 +522,8 @@ def linear_workspace_bytes(tokens: int, features_in: int, features_out: int, dty
 
 
 def block_workspace_bytes(tokens: int, n: int, dtype, columns: bool = False, backward: bool = False) -> int:
-    """Size of the workspace with which block_norm (backward: block_norm_backward) allocates nothing; dtype: of the residual stream, columns: F, Y or dY are in columns."""
+    """Size of the workspace with which block_norm (backward: block_norm_backward) allocates nothing; dtype: of the residual stream, columns: F, Y or dY are in columns.  On streams
+    other than the null one it is needed where this is not 0."""
     v = lib().block_workspace_bytes(tokens, n, _type_code(dtype), int(columns), int(backward))
     if v < 0:
         raise CerError(int(v), "block_workspace_bytes")

@@ -144,17 +144,14 @@ struct Temporary {
     int error = 0;
 };
 
-// All temporaries of a call in one: the caller's workspace, or one of the call's own.  A call that is being recorded has to bring its workspace.
+// All temporaries of a call in one: the caller's workspace, or, on the null stream, one of the call's own.  On any other stream, which may be one that is recorded or runs beside
+// others, a call that needs memory has to bring it: calls of these operators that allocated there were among those of a run that ended with a GPU fault of unknown cause.
 struct Room {
     static size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
-    Room(void* workspace, int64_t bytes, hipStream_t s) : own(workspace || !bytes || recorded(s) ? 0 : (size_t)bytes, s), at(static_cast<char*>(workspace ? workspace : own.p)) {
-        error = own.error ? own.error : bytes && !at ? (int)hipErrorStreamCaptureUnsupported : 0;
+    Room(void* workspace, int64_t bytes, hipStream_t s) : own(workspace || s ? 0 : (size_t)bytes, s), at(static_cast<char*>(workspace ? workspace : own.p)) {
+        error = own.error ? own.error : bytes && !at ? (int)hipErrorNotSupported : 0;
     }
-    static bool recorded(hipStream_t s) {
-        hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-        return s && (hipStreamIsCapturing(s, &st) != hipSuccess || st != hipStreamCaptureStatusNone);
-    }
-    float* take(size_t bytes) {  // 256-byte aligned, as the workspace is
+    float* take(size_t bytes) {  // apart by multiples of 256 bytes; aligned as the workspace is, to 16 at least
         if (!bytes) return nullptr;
         char* p = at;
         at += rounded(bytes);
