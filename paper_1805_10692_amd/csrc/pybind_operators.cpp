@@ -441,20 +441,17 @@ struct Workspace {
     int64_t numbers = 0;
     bool of(PyObject* o, Device& dev) { return !o || flat_of(o, "workspace", dev, CER_TYPE_F32, -1, &at, nullptr, &numbers); }
 };
-// Matrices that a call wants in one order: a single token's or feature's is both, so that those of them that have a choice follow one that has none.
+// Matrices that a call wants in one order.  A single token's or feature's order is both, as long as its numbers lie side by side: those that have a choice follow one that has
+// none -- one of several tokens and features, or one whose numbers lie apart (a token of a batch in columns, a feature of one in rows).
 template <int kMany>
 void one_order(cer_tokens_t* const (&m)[kMany], const int64_t (&features)[kMany], int64_t tokens) {
-    const cer_tokens_t* lead = nullptr;
-    for (int k = 0; k < kMany && !lead; ++k)
-        if (m[k]->data && tokens > 1 && features[k] > 1) lead = m[k];
-    if (!lead) {  // vectors of one token or of one feature: rows
-        for (int k = 0; k < kMany; ++k) {
-            const cer_tokens_t rows{nullptr, 0, 0, CER_ORDER_ROWS};
-            same_order(m[k], rows, tokens, features[k]);
-        }
-        return;
+    const cer_tokens_t rows{nullptr, 0, 0, CER_ORDER_ROWS}, *lead = &rows;
+    for (int k = kMany; k-- > 0;) {
+        const bool token = tokens == 1, feature = features[k] == 1, apart = m[k]->ld != 1 && (token ? m[k]->order == CER_ORDER_COLUMNS : feature && m[k]->order == CER_ORDER_ROWS);
+        if (m[k]->data && ((!token && !feature) || apart)) lead = m[k];
     }
-    for (int k = 0; k < kMany; ++k) same_order(m[k], *lead, tokens, features[k]);
+    const cer_tokens_t as = *lead;
+    for (int k = 0; k < kMany; ++k) same_order(m[k], as, tokens, features[k]);
 }
 
 PyObject* py_linear_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
@@ -573,7 +570,8 @@ PyObject* py_block_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t na
         !tokens_of(a[kDX], "dX", dev, &dx, &tokens, &n) || !tokens_of(a[kDF], "dF", dev, &df, &tokens, &n))
         return nullptr;
     if (a[kDSum] && !tokens_of(a[kDSum], "dsum", dev, &dsum, &tokens, &n)) return nullptr;
-    for (cer_tokens_t* m : {&dy, &h, &o, &dx, &df, &dsum}) Gate::rows(m, tokens, n);
+    for (cer_tokens_t* m : {&dy, &h, &dx, &dsum}) Gate::rows(m, tokens, n);
+    one_order<2>({&o, &df}, {n, n}, tokens);
     Gate gate, dgate;
     if (!gate.of(a[kGate], "gate", dev, -1, tokens, n) || !dgate.of(a[kDGate], "dgate", dev, CER_TYPE_F32, tokens, n)) return nullptr;
     if (a[kDGate] && (!dgate.vector) != (!gate.vector)) return fail("dgate", "must have gate's shape"), nullptr;
