@@ -644,8 +644,8 @@ int linear_backward(const void* W, int64_t ldw, int32_t type, int64_t tokens, in
  *   dgate, dgate_vector, dpost_weight, dpre_weight (the last three fp32): wanted where not NULL;  dgate only with gate, dgate_vector with gate_vector.
  *   No output may be an input's place.
  *
- * Rows alone: one launch forward; backward one (two over 6144 features of 16 bits or 8192 of fp32), and another where sums over the tokens are wanted, with a
- * temporary of up to 512 . n floats.  A matrix in columns costs a temporary of its size and, on either side of the work, a launch.
+ * Rows alone: one launch forward; backward one (two over 6144 features of H's 16 bits or 8192 of fp32, with a temporary of 2 floats a token), and another where sums over the
+ * tokens are wanted, with a temporary of up to 512 . n floats.  A matrix in columns costs a temporary of its size and, on either side of the work, a launch.
  */
 int block_norm(const cer_tokens_t* X, const cer_tokens_t* F, const cer_tokens_t* H, const cer_tokens_t* Y, int64_t tokens, int64_t n, const cer_tokens_t* gate,
                const void* gate_vector, int32_t gate_type, const void* post_weight, int32_t post_type, const void* pre_weight, int32_t pre_type, float scale,

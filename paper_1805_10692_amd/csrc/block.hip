@@ -487,10 +487,11 @@ struct BackShape {
     int64_t tokens_of_part;
     size_t turned, room, means;
     BackShape(const BlockBackwardCall& c) : w(c.n, c.h.type == CER_TYPE_F32 ? 4 : 8) {
-        // 1024 threads with eight features each spill: 2048 x 8192 bf16 80 us here, 72 in strips; with four or eight of fp32 they do not, or hardly (2000 x 7680: 94 us, 110).
-        inside = w.threads <= kFewThreads ? w.chunks == 1 : c.h.type == CER_TYPE_F32 && c.n <= 8192;
+        // 1024 threads with eight features each spill: 2048 x 8192 bf16 80 us here, 72 in strips; with four or eight of fp32 they do not
+        // (2000 x 4608 57 us, 81 in strips; 4096 x 6144 127 and 212; 2000 x 7680 88 and 110).
+        inside = c.n <= (c.h.type == CER_TYPE_F32 ? 8192 : 6144);
         sums[0] = c.dpre_weight != nullptr, sums[1] = c.dpost_weight || c.dgate_vector;
-        groups = inside && w.threads <= kFewThreads ? (unsigned)std::max<int64_t>(1, std::min<int64_t>(kFewThreads / w.threads, (c.tokens + 255) / 256)) : 1;
+        groups = inside && w.chunks == 1 && w.threads <= kFewThreads ? (unsigned)std::max<int64_t>(1, std::min<int64_t>(kFewThreads / w.threads, (c.tokens + 255) / 256)) : 1;
         tokens_of_part = std::max<int64_t>(1, (c.tokens + 63) / 64);
         parts = (unsigned)(inside ? std::min<int64_t>((c.tokens + groups - 1) / groups, 256) : (c.tokens + tokens_of_part - 1) / tokens_of_part);
         turned = (size_t)c.tokens * c.n * 4;
