@@ -609,7 +609,7 @@ int64_t block_workspace_bytes(int64_t tokens, int64_t n, int32_t type, int32_t c
  *   activation  CER_ACTIVATION_*: none, max(z, 0), z (1 + erf(z / sqrt 2)) / 2, the same with tanh(sqrt(2/pi) (z + 0.044715 z^3)) for erf, z / (1 + exp(-z)).
  *         An infinite z has the function's limit (-inf: 0).
  *
- * linear_backward -- with dZ = dY . activation'(pre), 0 where that is 0 whatever dY is (rounded to the type before the products):
+ * linear_backward -- with dZ = dY . activation'(pre), 0 where that is 0 whatever dY is (rounded to the type before the products; over the largest number of fp16: infinite):
  *   dX = base (NULL: 0; may be dX's own place) + W^T dZ;  dW = sum_t dZ_t x_t^T;  dbias = sum_t dZ_t (fp32, from the unrounded dZ).
  *   dX, dW, dbias: any may be NULL.  residual's gradient is dY itself.
  *   pre   what linear_matmul wrote (relu: its Y does as well, without a residual); NULL for CER_ACTIVATION_NONE

@@ -13,10 +13,11 @@
 // then has four neighbouring j of one i.  fp32 goes through the 32-bit instruction.  Sums are fp32; each C is rounded once, after the epilogue.
 // Where the tiles are too few for the chip the contraction is cut into parts, which a second launch adds up in their order (`plan_of`).
 //
-// What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 119 us, 1155 TFLOP/s (a large library product reaches
-// 1123 on this card); through registers 126, of which without loads 123, without stores to LDS either 111, without reading LDS 106, products and barriers alone 89 (the chip's
-// clock falls under them).  fp32: 2048 x 4096 -> 4096 480 us, 143 TFLOP/s of 154; through registers 105 - 135.  4096 tokens, 4096 -> 9216 bf16, forward 302 us (2.25 rounds, and the
-// epilogue of each by itself), dX 257, dW 273, dz 56.
+// What bounds it: the matrix cores and the way through LDS.  4096 x 4096 -> 4096 bf16 in one round of 256 tiles of 256 x 256: 113 us, 1214 TFLOP/s, over 300 calls on the same inputs,
+// 121 over 20 (a library product of that size 111 and 117); through registers 126 where the direct way took 119, of which without loads 123, without stores to LDS either 111,
+// without reading LDS 106, products and barriers alone 89 (the chip's clock falls under them).  fp32: 2048 x 4096 -> 4096 491 us, 140 TFLOP/s of 154, 553 over 20; through registers 105 - 135.
+// 4096 tokens, 4096 -> 9216 bf16: forward 310 us on new inputs in each call, 288 on the same ones (2.25 rounds, and the epilogue of each by itself); backward 600, of which dX 267,
+// dW 279, dz 53, db 5.
 #include <algorithm>
 #include <type_traits>
 
@@ -49,7 +50,7 @@ __device__ __forceinline__ float normal_share(float z) { return 0.5f * erfcf(-kH
 __device__ __forceinline__ float tanh_argument(float z) { return 2.f * kTanhFactor * z * fmaf(kTanhCube * z, z, 1.f); }
 // z . share; a share of 0 has its limit for an infinite z.
 __device__ __forceinline__ float part_of(float z, float share) { return share == 0.f ? 0.f : z * share; }
-// z / (1 + 2^-t)
+// z / (1 + 2^-t); may be 0 from where 2^-t passes 2^126 (silu: z below -87.3, where it is over -1.1e-36)
 __device__ __forceinline__ float share_of(float z, float t) { return part_of(z, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-t))); }
 constexpr float kLog2E = 1.4426950408889634f;
 
@@ -826,7 +827,7 @@ __global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
     }
 }
 // Two tiles of 16 tokens only where W is short: there the other kernel's two launches take longer (32 tokens, 640 -> 640 bf16: 6.8 against 11.1 us; 9216 -> 4096 33 against 22).
-// Few rows of a long W leave most compute units without a workgroup (one token, 12800 -> 640: 18 us against 15 in parts).
+// Few rows of a long W leave most compute units without a workgroup (one token, 12800 -> 640: 18 us against 10 in parts).
 bool few_tokens(int64_t tokens, int64_t in, int64_t out, int64_t item) {
     const bool brief = in * item <= 48 * 128;
     return tokens <= (brief ? 32 : 16) && (brief || out >= 2048);
@@ -958,6 +959,9 @@ int linear_of(const LinearCall& c, hipStream_t s) {
 }
 
 // What a backward call needs and how it goes about the gradient of z.
+// dz is kept in the activations' type: both products take it as an operand of the matrix instruction.  In 16 bits that costs half a step of each dz, which the gradients show (4096
+// tokens, 4096 -> 9216 bf16: off by 2.3e-3 of their size, 1.7e-3 with dz in 32 bits, which is their own rounding); two pieces of 16 bits would keep it, and double dX's and dW's 546 us.
+// db is summed before dz is rounded.
 template <class T>
 struct BackwardShape {
     static constexpr int V = 16 / sizeof(T);
