@@ -6,6 +6,7 @@
 
 W is dense and trained; V is quantized, kept in CER form and frozen.  Everything between the norms is in columns, cer_matmul's order; the residual
 stream x -> h is in rows.  y is what the next block reads.  A step goes back the same way, with the same dropout mask formed again from its key.
+Calls that need memory take temporaries of their own: on the null stream.  On another one they take a workspace (binding.linear_workspace_bytes, block_workspace_bytes).
 """
 import os
 import sys
